@@ -264,6 +264,46 @@ int bb_debug_wide_format(bb_ctx* ctx, int on);
 int bb_gemm_static(const float* A_dev, const uint16_t* W_dev, float* C_dev, int M, int N, int K, int split_k,
                    void* hip_stream);
 
+/* ---- 8-bit integer operators ---------------------------------------------------------------------
+ * Rows quantised to int8 with one fp32 scale each, and the product of such rows with such weights.  No context is
+ * needed; all work is enqueued on hip_stream (a hipStream_t of the current device, NULL = its default stream); nothing is
+ * allocated, memset or synchronised, so every call may be captured into a graph.  Pointers are device memory, aligned to their
+ * element's size; ld* is the distance between rows in elements (ignored for a single row): rows of an output must not overlap
+ * (ld >= columns), those of an input may, and nothing between the columns and ld is read or written.  Rows that are 16-byte aligned are
+ * fastest.  Malformed arguments: BB_EINVAL; a HIP error: BB_EHIP (no context, hence no bb_last_error text).  No rows: BB_OK,
+ * nothing is launched. */
+#define BB_F32  0
+#define BB_BF16 1
+#define BB_F16  2
+#define BB_QUANTIZE_MAX_ROWS 0x7FFFFFFF
+
+/* q[r][c] = rint(127 x[r][c] / max_c |x[r][c]|) (ties to even), scale[r] = max_c |x[r][c]| / 127, so that
+ * q * scale stands for x.  A row of zeros has scale 0; a row that holds a NaN or an infinity has scale NaN and codes 0.
+ * x of `type` (BB_F32, BB_BF16, BB_F16).  Quantises activations per token and weights ([out][in]) per output channel. */
+int bb_quantize_rows(const void* x_dev, long ldx, int8_t* q_dev, long ldq, float* scale_dev, long rows, int cols, int type,
+                     void* hip_stream);
+
+/* h = x + residual, rounded to `type` and stored in residual_out (may be residual or x themselves); then the rows of
+ * y = h / sqrt(mean_c h^2 + eps) * gain quantised as above, y unrounded.  Without a residual (both residual pointers NULL) h = x.
+ * gain: [cols]; x, residual, residual_out, gain of the same type.  eps >= 0. */
+int bb_rmsnorm_quantize(const void* x_dev, long ldx, const void* residual_dev, long ldr, void* residual_out_dev, long ldo,
+                        const void* gain_dev, float eps, int8_t* q_dev, long ldq, float* scale_dev, long rows, int cols, int type,
+                        void* hip_stream);
+
+/* The rows of y = gate / (1 + exp(-gate)) * up (fp32, unrounded) quantised as above; gate and up of the same type. */
+int bb_swiglu_quantize(const void* gate_dev, long ldg, const void* up_dev, long ldu, int8_t* q_dev, long ldq, float* scale_dev,
+                       long rows, int cols, int type, void* hip_stream);
+
+/* C[m][n] = (sum_k A[m][k] W[n][k]) * a_scale[m] * w_scale[n] + bias[n]: the sum exact in int32 (hence K <=
+ * BB_GEMM_INT8_MAX_K), the scaling in fp32, C rounded to c_type.  A [M][K], W [N][K] int8, scales and bias (may be NULL) fp32.
+ * workspace_dev: at least bb_gemm_int8_workspace_bytes(M, N, K) bytes, 16-byte aligned (may be NULL if that is 0), used by this
+ * call alone until its work is done; BB_ENOMEM if it is smaller. */
+#define BB_GEMM_INT8_MAX_K 131071
+size_t bb_gemm_int8_workspace_bytes(int M, int N, int K);
+int bb_gemm_int8(const int8_t* A_dev, long lda, const float* a_scale_dev, const int8_t* W_dev, long ldw, const float* w_scale_dev,
+                 const float* bias_dev, void* C_dev, long ldc, int c_type, int M, int N, int K, void* workspace_dev,
+                 size_t workspace_bytes, void* hip_stream);
+
 /* Tests: on != 0 makes every later forward also store the fp32 logits of the rows that receive them (view's
  * logits_dev); off (the default) the logits exist only in the registers of the LM-head GEMM. */
 int bb_debug_keep_logits(bb_ctx* ctx, int on);

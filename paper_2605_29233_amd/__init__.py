@@ -4,4 +4,4 @@ The binding only marshals arguments; every step of the path runs in the library'
 PyTorch is used for the device workspace allocation and the stream handle.
 """
 from .binding import (BlockBatch, Limits, BranchState, RequestStats, StepView, BBError, lib_path, load_library,
-                      BB_INIT, BB_PERIODIC)  # noqa: F401
+                      BB_INIT, BB_PERIODIC, quantize_rows, rmsnorm_quantize, swiglu_quantize, gemm_int8)  # noqa: F401

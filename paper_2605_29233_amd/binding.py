@@ -64,7 +64,8 @@ def lib_path():
 _LIB = None
 EXPORTS = ("bb_workspace_bytes", "bb_create", "bb_destroy", "bb_last_error", "bb_load_weights", "bb_request_open",
            "bb_request_close", "bb_refresh", "bb_denoise_step", "bb_merge_commit", "bb_get_tokens", "bb_get_stats",
-           "bb_get_view", "bb_set_state", "bb_get_kv", "bb_set_kv", "bb_read_device", "bb_synchronize", "bb_debug_gemm", "bb_debug_gemm_wide", "bb_debug_wide_format", "bb_profile_enable", "bb_profile_read", "bb_debug_set_gemm_plan", "bb_debug_gemm_plan", "bb_debug_attention_plan", "bb_debug_copy16", "bb_generate", "bb_kv_diag_scratch_bytes", "bb_kv_diagnostics", "bb_gemm_static", "bb_debug_mfma_rate", "bb_debug_keep_logits")
+           "bb_get_view", "bb_set_state", "bb_get_kv", "bb_set_kv", "bb_read_device", "bb_synchronize", "bb_debug_gemm", "bb_debug_gemm_wide", "bb_debug_wide_format", "bb_profile_enable", "bb_profile_read", "bb_debug_set_gemm_plan", "bb_debug_gemm_plan", "bb_debug_attention_plan", "bb_debug_copy16", "bb_generate", "bb_kv_diag_scratch_bytes", "bb_kv_diagnostics", "bb_gemm_static", "bb_debug_mfma_rate", "bb_debug_keep_logits",
+           "bb_quantize_rows", "bb_rmsnorm_quantize", "bb_swiglu_quantize", "bb_gemm_int8", "bb_gemm_int8_workspace_bytes")
 KERNEL_CLASSES = ("gemm_skinny", "gemm_wide", "attention", "glue", "policy")
 
 
@@ -117,6 +118,13 @@ def load_library():
         lib.bb_debug_keep_logits.argtypes = [C.c_void_p, C.c_int]
         lib.bb_debug_mfma_rate.argtypes = [C.c_void_p, C.POINTER(C.c_double)]
         lib.bb_gemm_static.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p]
+        ptr, i64, i32 = C.c_void_p, C.c_long, C.c_int
+        lib.bb_quantize_rows.argtypes = [ptr, i64, ptr, i64, ptr, i64, i32, i32, ptr]
+        lib.bb_rmsnorm_quantize.argtypes = [ptr, i64, ptr, i64, ptr, i64, ptr, C.c_float, ptr, i64, ptr, i64, i32, i32, ptr]
+        lib.bb_swiglu_quantize.argtypes = [ptr, i64, ptr, i64, ptr, i64, ptr, i64, i32, i32, ptr]
+        lib.bb_gemm_int8.argtypes = [ptr, i64, ptr, ptr, i64, ptr, ptr, ptr, i64, i32, i32, i32, i32, ptr, C.c_size_t, ptr]
+        lib.bb_gemm_int8_workspace_bytes.argtypes = [i32, i32, i32]
+        lib.bb_gemm_int8_workspace_bytes.restype = C.c_size_t
         _LIB = lib
     return _LIB
 
@@ -143,6 +151,151 @@ def gemm_plan(M, N, K, wide=True, fusable=False):
     if rc != 0:
         raise ValueError(f"bb_debug_gemm_plan({M}, {N}, {K}) -> {rc}")
     return dict(split_k=out[0], chunks_per_split=out[1], nt=out[2], mt=out[3], workgroups=out[4])
+
+
+# ---- 8-bit integer operators --------------------------------------------------------------------
+_TYPES = None           # torch dtype -> BB_F32, BB_BF16, BB_F16
+
+
+def _types():
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    return _TYPES
+
+
+def _rows(t, name, dtype, shape, device):
+    """Row distance of a 2-D operand whose rows are contiguous; refuses any other."""
+    if t.dtype != dtype or t.device != device or t.shape != shape:
+        raise BBError(f"{name}: expected {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if shape[1] > 1 and t.stride(1) != 1:
+        raise BBError(f"{name}: the elements of a row must be contiguous")
+    return t.stride(0)
+
+
+def _vector(t, name, dtype, n, device):
+    if t.dtype != dtype or t.device != device or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise BBError(f"{name}: expected contiguous {dtype} ({n},) on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+class _On:
+    """The device and stream of a call: tensors made inside belong to that stream."""
+
+    def __init__(self, device, stream):
+        import torch
+        if device.type != "cuda":
+            raise BBError(f"tensors must be on the GPU, got {device} (there is no CPU fallback)")
+        if stream is not None and stream.device != device:
+            raise BBError(f"the stream is of {stream.device}, the tensors are on {device}")
+        self._guard = torch.cuda.stream(stream) if stream is not None else \
+            torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
+        self.handle = (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+
+    def __enter__(self):
+        if self._guard is not None:
+            self._guard.__enter__()
+        return self.handle
+
+    def __exit__(self, *a):
+        if self._guard is not None:
+            self._guard.__exit__(*a)
+
+
+def _quantized(x, out, scale):
+    """Checks of what the three quantisers share; (q, its row distance, scale), made here where not given."""
+    import torch
+    if x.dim() != 2 or x.dtype not in _types():
+        raise BBError(f"expected a 2-D tensor of float32, bfloat16 or float16, got {x.dtype} {tuple(x.shape)}")
+    rows, cols = x.shape
+    if out is None:         # (rows at multiples of 16 bytes, as the product reads them fastest)
+        out = torch.empty(rows, (cols + 15) // 16 * 16, dtype=torch.int8, device=x.device)[:, :cols]
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    ldq = _rows(out, "out", torch.int8, x.shape, x.device)
+    _vector(scale, "scale", torch.float32, rows, x.device)
+    return out, ldq, scale
+
+
+def _done(rc, what):
+    if rc != 0:
+        raise BBError(f"{what}: {_ERR.get(rc, rc)}")
+
+
+def quantize_rows(x, out=None, scale=None, stream=None):
+    """bb_quantize_rows on torch CUDA tensors: x [rows][cols] fp32, bf16 or fp16 -> (q int8 [rows][cols], scale fp32
+    [rows]) with q * scale standing for x.  q and scale are written in place where given.  The call is enqueued on
+    `stream` (default: the current stream of x's device), on which what it makes is allocated too."""
+    lib = load_library()
+    with _On(x.device, stream) as st:
+        out, ldq, scale = _quantized(x, out, scale)
+        rows, cols = x.shape
+        _done(lib.bb_quantize_rows(x.data_ptr(), _rows(x, "x", x.dtype, x.shape, x.device), out.data_ptr(), ldq, scale.data_ptr(),
+                                   rows, cols, _types()[x.dtype], st), "bb_quantize_rows")
+    return out, scale
+
+
+def rmsnorm_quantize(x, gain, eps, residual=None, residual_out=None, out=None, scale=None, stream=None):
+    """bb_rmsnorm_quantize: h = x + residual -> residual_out (default: residual itself, in place), then RMSNorm(h) * gain
+    with int8 rows; returns (q, scale).  Without a residual h = x.  gain has x's type.  Stream as in quantize_rows."""
+    lib = load_library()
+    with _On(x.device, stream) as st:
+        out, ldq, scale = _quantized(x, out, scale)
+        rows, cols = x.shape
+        res = h = None
+        ldr = ldh = 0
+        if residual is not None:
+            h = residual if residual_out is None else residual_out
+            ldr, ldh = _rows(residual, "residual", x.dtype, x.shape, x.device), _rows(h, "residual_out", x.dtype, x.shape, x.device)
+            res, h = residual.data_ptr(), h.data_ptr()
+        elif residual_out is not None:
+            raise BBError("residual_out without a residual")
+        _done(lib.bb_rmsnorm_quantize(x.data_ptr(), _rows(x, "x", x.dtype, x.shape, x.device), res, ldr, h, ldh,
+                                      _vector(gain, "gain", x.dtype, cols, x.device), eps, out.data_ptr(), ldq, scale.data_ptr(),
+                                      rows, cols, _types()[x.dtype], st), "bb_rmsnorm_quantize")
+    return out, scale
+
+
+def swiglu_quantize(gate, up, out=None, scale=None, stream=None):
+    """bb_swiglu_quantize: SiLU(gate) * up with int8 rows; returns (q, scale).  gate and up may be the two halves of one
+    tensor's columns.  Stream as in quantize_rows."""
+    lib = load_library()
+    with _On(gate.device, stream) as st:
+        out, ldq, scale = _quantized(gate, out, scale)
+        rows, cols = gate.shape
+        _done(lib.bb_swiglu_quantize(gate.data_ptr(), _rows(gate, "gate", gate.dtype, gate.shape, gate.device), up.data_ptr(),
+                                     _rows(up, "up", gate.dtype, gate.shape, gate.device), out.data_ptr(), ldq, scale.data_ptr(),
+                                     rows, cols, _types()[gate.dtype], st), "bb_swiglu_quantize")
+    return out, scale
+
+
+def gemm_int8(a, a_scale, w, w_scale, bias=None, out=None, dtype=None, stream=None):
+    """bb_gemm_int8: out[m][n] = (sum_k a[m][k] w[n][k]) * a_scale[m] * w_scale[n] + bias[n]; a [M][K], w [N][K] int8,
+    scales and bias fp32.  out: fp32, bf16 or fp16 [M][N], made here (of `dtype`, default bf16) where not given.  Stream as in
+    quantize_rows; the workspace is allocated on it for this call alone."""
+    import torch
+    lib = load_library()
+    dev = a.device
+    with _On(dev, stream) as st:
+        if a.dim() != 2 or w.dim() != 2:
+            raise BBError(f"expected 2-D operands, got {tuple(a.shape)} and {tuple(w.shape)}")
+        (M, K), N = a.shape, w.shape[0]
+        lda, ldw = _rows(a, "a", torch.int8, a.shape, dev), _rows(w, "w", torch.int8, torch.Size((N, K)), dev)
+        sa, sw = _vector(a_scale, "a_scale", torch.float32, M, dev), _vector(w_scale, "w_scale", torch.float32, N, dev)
+        b = None if bias is None else _vector(bias, "bias", torch.float32, N, dev)
+        if out is None:
+            out = torch.empty(M, N, dtype=dtype or torch.bfloat16, device=dev)
+        elif dtype is not None and out.dtype != dtype:
+            raise BBError(f"out has {out.dtype}, dtype says {dtype}")
+        if out.dtype not in _types():
+            raise BBError(f"out: expected float32, bfloat16 or float16, got {out.dtype}")
+        ldc = _rows(out, "out", out.dtype, torch.Size((M, N)), dev)
+        nbytes = lib.bb_gemm_int8_workspace_bytes(M, N, K)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+        _done(lib.bb_gemm_int8(a.data_ptr(), lda, sa, w.data_ptr(), ldw, sw, b, out.data_ptr(), ldc, _types()[out.dtype], M, N, K,
+                               ws.data_ptr() if nbytes else None, nbytes, st), "bb_gemm_int8")
+    return out
 
 
 class StepView:
