@@ -296,10 +296,13 @@ int bb_swiglu_quantize(const void* gate_dev, long ldg, const void* up_dev, long 
 
 /* C[m][n] = (sum_k A[m][k] W[n][k]) * a_scale[m] * w_scale[n] + bias[n]: the sum exact in int32 (hence K <=
  * BB_GEMM_INT8_MAX_K), the scaling in fp32, C rounded to c_type.  A [M][K], W [N][K] int8, scales and bias (may be NULL) fp32.
- * workspace_dev: at least bb_gemm_int8_workspace_bytes(M, N, K) bytes, 16-byte aligned (may be NULL if that is 0), used by this
- * call alone until its work is done; BB_ENOMEM if it is smaller. */
+ * M and N at most BB_GEMM_INT8_MAX_ROWS.
+ * workspace_dev: at least bb_gemm_int8_workspace_bytes(M, N, K, aligned) bytes, 16-byte aligned (may be NULL if that is 0), used
+ * by this call alone until its work is done; BB_ENOMEM if it is smaller.  aligned: nonzero if A_dev, W_dev, lda and ldw are multiples of 16
+ * (and lda, ldw at most 2^23; the ld of a single row counts as 0).  Operands that are not are slower. */
 #define BB_GEMM_INT8_MAX_K 131071
-size_t bb_gemm_int8_workspace_bytes(int M, int N, int K);
+#define BB_GEMM_INT8_MAX_ROWS (1 << 30)
+size_t bb_gemm_int8_workspace_bytes(int M, int N, int K, int aligned);
 int bb_gemm_int8(const int8_t* A_dev, long lda, const float* a_scale_dev, const int8_t* W_dev, long ldw, const float* w_scale_dev,
                  const float* bias_dev, void* C_dev, long ldc, int c_type, int M, int N, int K, void* workspace_dev,
                  size_t workspace_bytes, void* hip_stream);

@@ -123,7 +123,7 @@ def load_library():
         lib.bb_rmsnorm_quantize.argtypes = [ptr, i64, ptr, i64, ptr, i64, ptr, C.c_float, ptr, i64, ptr, i64, i32, i32, ptr]
         lib.bb_swiglu_quantize.argtypes = [ptr, i64, ptr, i64, ptr, i64, ptr, i64, i32, i32, ptr]
         lib.bb_gemm_int8.argtypes = [ptr, i64, ptr, ptr, i64, ptr, ptr, ptr, i64, i32, i32, i32, i32, ptr, C.c_size_t, ptr]
-        lib.bb_gemm_int8_workspace_bytes.argtypes = [i32, i32, i32]
+        lib.bb_gemm_int8_workspace_bytes.argtypes = [i32, i32, i32, i32]
         lib.bb_gemm_int8_workspace_bytes.restype = C.c_size_t
         _LIB = lib
     return _LIB
@@ -291,9 +291,11 @@ def gemm_int8(a, a_scale, w, w_scale, bias=None, out=None, dtype=None, stream=No
         if out.dtype not in _types():
             raise BBError(f"out: expected float32, bfloat16 or float16, got {out.dtype}")
         ldc = _rows(out, "out", out.dtype, torch.Size((M, N)), dev)
-        nbytes = lib.bb_gemm_int8_workspace_bytes(M, N, K)
+        pa, pw = a.data_ptr(), w.data_ptr()
+        lda, ldw = lda if M > 1 else 0, ldw if N > 1 else 0
+        nbytes = lib.bb_gemm_int8_workspace_bytes(M, N, K, int((pa | pw | lda | ldw) % 16 == 0 and lda <= 1 << 23 and ldw <= 1 << 23))
         ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-        _done(lib.bb_gemm_int8(a.data_ptr(), lda, sa, w.data_ptr(), ldw, sw, b, out.data_ptr(), ldc, _types()[out.dtype], M, N, K,
+        _done(lib.bb_gemm_int8(pa, lda, sa, pw, ldw, sw, b, out.data_ptr(), ldc, _types()[out.dtype], M, N, K,
                                ws.data_ptr() if nbytes else None, nbytes, st), "bb_gemm_int8")
     return out
 

@@ -2,13 +2,13 @@
 // the row itself (bb_quantize_rows), RMSNorm of it with the residual's addition (bb_rmsnorm_quantize) or SiLU(gate) * up
 // (bb_swiglu_quantize).
 //
-// The codes are those of the formula whatever the launch: the norm's 1 / rms is a positive factor of the whole row and falls out of
-// y / max |y|, so they depend on p = h * gain alone, which a double holds exactly; 127 p / max |p| is formed in double too, as a
-// product with 127 / max |p| and, within 1e-12 of a border between two codes, again as a correctly rounded quotient (a border that
-// is met exactly, like half the maximum, is thereby seen as one).  SiLU is computed in fp32: its y is off by a few 2^-24 and a code
-// can so differ by one where y is that near to a border.  Sums of squares are in double.
+// The codes are those of the formula in 64 bits whatever the launch.  The norm's 1 / rms is a positive factor of the whole row and falls out
+// of y / max |y|, so they depend on p = h * gain alone, which a double holds exactly.  Values are kept in fp32 (v), which for 16-bit types is p
+// itself, else off by V_ERR at most; t = v * (127 / max) is off by 127 (V_ERR + 2^-23).  Only where t is that near to a border between two
+// codes (a few elements in 10^5) is the value taken again, in double, and the quotient correctly rounded, so that a border that is met
+// exactly (half the maximum is 63.5) is seen as one.  So is the maximum itself where fp32 does not hold it.  Sums of squares are in double.
 //
-// What bounds it: memory.  A row is read once and kept in registers (as it came) between the maximum and the codes.
+// What bounds it: memory.  A row is read once and its values stay in registers between the maximum and the codes.
 #include "bb_internal.h"
 #include <algorithm>
 #include <type_traits>
@@ -38,23 +38,54 @@ template <class T> static __device__ __forceinline__ T narrow(float v) {
     } else return (T)v;
 }
 
-// Eight consecutive elements; any alignment that the type itself has (the hardware takes such loads and stores).
-template <class T> struct Eight { T e[8]; };
-template <class T> static __device__ __forceinline__ Eight<T> load8(const T* p) { Eight<T> r; __builtin_memcpy(&r, p, sizeof(r)); return r; }
-template <class T> static __device__ __forceinline__ Eight<T> load8(const T* p, int n) {
-    Eight<T> r;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) r.e[j] = j < n ? p[j] : T{};
-    return r;
+// Eight consecutive elements as they lie in memory, taken apart only where they are used: loads of several groups are then on their way together.
+template <class T> struct Eight {
+    static constexpr int WORDS = 8 * (int)sizeof(T) / 16;
+    u32x4 w[WORDS];
+    __device__ __forceinline__ float get(int j) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[j >> 2][j & 3]);
+        else if constexpr (std::is_same_v<T, bf16_t>) return __uint_as_float(j & 1 ? w[0][j >> 1] & 0xFFFF0000u : w[0][j >> 1] << 16);
+        else return (float)__builtin_bit_cast(half_t, (uint16_t)(w[0][j >> 1] >> (16 * (j & 1))));
+    }
+    __device__ __forceinline__ void set(int j, float v) {
+        const T n = narrow<T>(v);
+        if constexpr (sizeof(T) == 4) w[j >> 2][j & 3] = __float_as_uint(n);
+        else {
+            const unsigned b = __builtin_bit_cast(uint16_t, n);
+            w[0][j >> 1] = j & 1 ? (w[0][j >> 1] & 0xFFFFu) | b << 16 : (w[0][j >> 1] & 0xFFFF0000u) | b;
+        }
+    }
+    // any alignment that the type itself has
+    __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(w, p, sizeof(w)); }
+    __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, w, sizeof(w)); }
+};
+
+// x / (1 + exp(-x)).  exp(-x) = 2^(-x log2 e): the product in two parts, the second (its rounding, and what a float of log2 e leaves out)
+// as a factor 1 + part ln 2.  Halves of a last place: 1 for the product's parts, 2 each for the hardware's exp2 and reciprocal, 1 each for the
+// factor, the sum, the product with x: 8, and 1 for the product with `up`.
+static __device__ __forceinline__ float silu(float x) {
+    constexpr float L = -1.44269504088896340736f, L_REST = (float)(-1.44269504088896340736 - (double)L);
+    const float hi = x * L, lo = fmaf(x, L_REST, fmaf(x, L, -hi)), e0 = __builtin_amdgcn_exp2f(hi);
+    const float e = fabsf(hi) < 126.0f ? fmaf(e0, lo * 0.693147180559945309417f, e0) : e0;     // (beyond, infinity times a small part)
+    return x * __builtin_amdgcn_rcpf(1.0f + e);
 }
 
-struct RowSums { double top, ss; bool bad; };
+// What a row's values are, at column c, in 64 bits, from memory (h once it is written).
+template <int OP, class T> static __device__ __forceinline__ double exact_value(const QuantArgs& a, long row, int c) {
+    const double x = widen((OP == QOP_NORM && a.x2 ? (const T*)a.h + row * a.ldh : (const T*)a.x + row * a.ldx)[c]);
+    if constexpr (OP == QOP_NORM) return x * (double)widen(((const T*)a.gain)[c]);
+    if constexpr (OP == QOP_SWIGLU) return x / (1.0 + exp(-x)) * (double)widen(((const T*)a.x2 + row * a.ldx2)[c]);
+    return x;
+}
 
 // THREADS lanes share a row (64: a wave each, four rows a workgroup).  G: groups of eight columns a thread keeps, group i of thread t
-// being number t + i THREADS of the row; G = 0: rows of more than 32768 columns, read a second time for the codes.
+// being number t + i THREADS of the row; G = 0: longer rows, read again for the codes.  Of the up to seven columns that make no group thread t takes one.
 template <int OP, class T, int THREADS, int G>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel(QuantArgs a) {
     constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1, KEEP = G ? G : 1;
+    constexpr bool TOP_IN_DOUBLE = OP == QOP_NORM && std::is_same_v<T, float>;      // v does not hold the maximum, but its factors are at hand
+    // 2^-24: one rounding; SiLU * up: 9 of them, allowed 16
+    constexpr float V_ERR = OP == QOP_SWIGLU ? 0x1p-20f : 0x1p-24f, NEAR = 0.5f - 127.0f * (V_ERR + 0x1p-22f);
     const int t = threadIdx.x % THREADS;
     const long row = (long)blockIdx.x * ROWS + threadIdx.x / THREADS;
     if (ROWS > 1 && row >= a.rows) return;                  // (whole waves; no barrier follows where rows share a workgroup)
@@ -62,104 +93,202 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
     const T* x2 = a.x2 ? (const T*)a.x2 + row * a.ldx2 : nullptr;
     const T* gain = (const T*)a.gain;
     T* h = (T*)a.h + row * a.ldh;
-    const int cols = a.cols, groups = (cols + 7) >> 3;
+    const int cols = a.cols, groups = cols >> 3, c_tail = groups * 8 + t;
+    const bool tail = t < (cols & 7);
 
-    Eight<T> kx[KEEP], kx2[OP == QOP_SWIGLU ? KEEP : 1], kg[OP == QOP_NORM ? KEEP : 1];
-    auto fetch = [&](int i, int g, bool again) {
-        const int c = g * 8, n = cols - c;
-        auto get = [&](const T* p) { return n >= 8 ? load8(p + c) : load8(p + c, n); };
-        kx[i] = get(OP == QOP_NORM && again && x2 ? h : x);
-        if constexpr (OP == QOP_SWIGLU) kx2[i] = get(x2);
+    float v[KEEP][8], v_tail = 0.f;
+    double ss = 0.0, top2 = 0.0;
+    unsigned top_bits = 0u;                                 // as whole numbers |v| are in order, infinity and NaN at the end
+    Eight<T> kx[KEEP], ky[OP == QOP_ROWS ? 1 : KEEP], kr[OP == QOP_NORM ? KEEP : 1];
+    auto fetch = [&](int i, int g, bool again) {            // (nothing that would make a load wait for the one before it)
+        const int c = g * 8;
+        kx[i].load((OP == QOP_NORM && again && x2 ? h : x) + c);
+        if constexpr (OP == QOP_SWIGLU) ky[i].load(x2 + c);
         if constexpr (OP == QOP_NORM) {
-            kg[i] = get(gain);
+            ky[i].load(gain + c);
+            if (x2 && !again) kr[i].load(x2 + c);
+        }
+    };
+    auto value = [&](float f, float w) {
+        float y = f;
+        if constexpr (OP == QOP_NORM) {
+            y = f * w;
+            ss = fma((double)f, (double)f, ss);
+            if constexpr (TOP_IN_DOUBLE) top2 = fmax(top2, fabs((double)f * (double)w));
+        }
+        if constexpr (OP == QOP_SWIGLU) y = silu(f) * w;
+        top_bits = max(top_bits, __float_as_uint(y) & 0x7FFFFFFFu);
+        return y;
+    };
+    auto values = [&](int i, int g, bool again) {
+        if constexpr (OP == QOP_NORM)
             if (x2 && !again) {
-                const Eight<T> r = get(x2);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) kx[i].e[j] = narrow<T>(widen(kx[i].e[j]) + widen(r.e[j]));
-                if (n >= 8) __builtin_memcpy(h + c, &kx[i], sizeof(kx[i]));
-                else for (int j = 0; j < n; ++j) h[c + j] = kx[i].e[j];
+                for (int j = 0; j < 8; ++j) kx[i].set(j, kx[i].get(j) + kr[i].get(j));
+                kx[i].store(h + g * 8);
             }
-        }
-    };
-    auto value = [&](int i, int j) -> double {
-        const float v = widen(kx[i].e[j]);
-        if constexpr (OP == QOP_ROWS) return v;
-        if constexpr (OP == QOP_NORM) return (double)v * (double)widen(kg[i].e[j]);
-        if constexpr (OP == QOP_SWIGLU) return v / (1.0f + expf(-v)) * widen(kx2[i].e[j]);
-    };
-    RowSums s = {0.0, 0.0, false};
-    auto look = [&](int i) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const double y = fabs(value(i, j));
-            s.bad |= !(y < INFINITY);
-            s.top = fmax(s.top, y);
-            if constexpr (OP == QOP_NORM) { const double v = widen(kx[i].e[j]); s.ss = fma(v, v, s.ss); }
-        }
+        for (int j = 0; j < 8; ++j) v[i][j] = value(kx[i].get(j), OP == QOP_ROWS ? 0.f : ky[OP == QOP_ROWS ? 0 : i].get(j));
     };
     if constexpr (G > 0) {
 #pragma unroll
         for (int i = 0; i < G; ++i) if (t + i * THREADS < groups) fetch(i, t + i * THREADS, false);
-#pragma unroll
-        for (int i = 0; i < G; ++i) if (t + i * THREADS < groups) look(i);
-    } else
-        for (int g = t; g < groups; g += THREADS) { fetch(0, g, false); look(0); }
-
-    int bad = s.bad;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        s.top = fmax(s.top, __shfl_xor(s.top, o, 64));
-        if constexpr (OP == QOP_NORM) s.ss += __shfl_xor(s.ss, o, 64);
-        bad |= __shfl_xor(bad, o, 64);
     }
-    if constexpr (THREADS > 64) {
-        __shared__ double tops[THREADS / 64], sums[THREADS / 64];
-        __shared__ int bads[THREADS / 64];
-        if ((t & 63) == 0) { tops[t >> 6] = s.top; sums[t >> 6] = s.ss; bads[t >> 6] = bad; }
-        __syncthreads();
-        s.top = 0.0; s.ss = 0.0; bad = 0;
-#pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w) { s.top = fmax(s.top, tops[w]); s.ss += sums[w]; bad |= bads[w]; }
+    if (tail) {
+        float f = widen(x[c_tail]);
+        if constexpr (OP == QOP_NORM)
+            if (x2) {
+                const T n = narrow<T>(f + widen(x2[c_tail]));
+                h[c_tail] = n;
+                f = widen(n);
+            }
+        v_tail = value(f, OP == QOP_NORM ? widen(gain[c_tail]) : OP == QOP_SWIGLU ? widen(x2[c_tail]) : 0.f);
     }
-    // a row that holds a NaN or an infinity has the scale NaN (and codes 0); one of zeros the scale 0
-    if constexpr (OP == QOP_NORM) bad |= !(s.ss < INFINITY);
-    if (t == 0) {
-        const double rms = OP == QOP_NORM ? sqrt(s.ss / cols + a.eps) : 1.0;
-        a.scale[row] = bad ? NAN : s.top == 0.0 ? 0.0f : (float)(s.top / rms / 127.0);
-    }
-    const bool none = bad || s.top == 0.0;
-    const double per = none ? 0.0 : 127.0 / s.top;
-    int8_t* q = a.q + row * a.ldq;
-    auto codes = [&](int i, int g) {
-        const int c = g * 8, n = cols - c;
-        unsigned out[2] = {0u, 0u};
+    if constexpr (G > 0) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const double p = none ? 0.0 : value(i, j), u = p * per;
-            double r = rint(u);
-            if (fabs(u - r) > 0.5 - 1e-12) r = rint(127.0 * p / s.top);
-            out[j >> 2] |= ((unsigned)(int)r & 0xFFu) << (8 * (j & 3));
+        for (int i = 0; i < G; ++i) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+            if (t + i * THREADS < groups) values(i, t + i * THREADS, false);
         }
-        if (n >= 8) __builtin_memcpy(q + c, out, 8);
-        else for (int j = 0; j < n; ++j) q[c + j] = (int8_t)(out[j >> 2] >> (8 * (j & 3)));
+    } else
+        for (int g = t; g < groups; g += THREADS) { fetch(0, g, false); values(0, g, false); }
+
+    // ---- the row's maximum (and sum of squares) ----------------------------------------------------------------------------------------
+    __shared__ double sh_ss[16], sh_top[16];
+    __shared__ unsigned sh_bits[16];
+    auto reduce = [&]() {
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            top_bits = max(top_bits, (unsigned)__shfl_xor((int)top_bits, o, 64));
+            if constexpr (OP == QOP_NORM) ss += __shfl_xor(ss, o, 64);
+            if constexpr (TOP_IN_DOUBLE) top2 = fmax(top2, __shfl_xor(top2, o, 64));
+        }
+        if constexpr (THREADS > 64) {
+            if ((t & 63) == 0) { sh_bits[t >> 6] = top_bits; if (OP == QOP_NORM) sh_ss[t >> 6] = ss; if (TOP_IN_DOUBLE) sh_top[t >> 6] = top2; }
+            __syncthreads();
+            ss = 0.0;
+#pragma unroll
+            for (int w = 0; w < THREADS / 64; ++w) {
+                top_bits = max(top_bits, sh_bits[w]);
+                if constexpr (OP == QOP_NORM) ss += sh_ss[w];
+                if constexpr (TOP_IN_DOUBLE) top2 = fmax(top2, sh_top[w]);
+            }
+        }
+    };
+    auto reduce_top = [&](double d) {                       // the maximum of d over the row
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) d = fmax(d, __shfl_xor(d, o, 64));
+        if constexpr (THREADS > 64) {
+            __syncthreads();
+            if ((t & 63) == 0) sh_top[t >> 6] = d;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < THREADS / 64; ++w) d = fmax(d, sh_top[w]);
+        }
+        return d;
+    };
+    reduce();
+    double top = TOP_IN_DOUBLE ? top2 : (double)__uint_as_float(top_bits);
+    // Rows so large or small that fp32 products would not do (and those that hold an infinity or a NaN): everything in double.
+    const bool hard = !(top_bits > 0x0D800000u && top_bits < 0x71800000u);     // 2^-100, 2^100
+    bool bad = false;
+    if (hard && top_bits != 0u) {
+        double d = 0.0;
+        int b = 0;
+        for (int c = t; c < cols; c += THREADS) {
+            const double y = fabs(exact_value<OP, T>(a, row, c));
+            b |= !(y < INFINITY);
+            d = fmax(d, y);
+        }
+        top = reduce_top(b ? INFINITY : d);
+        bad = !(top < INFINITY);
+    } else if (OP == QOP_SWIGLU && top_bits != 0u) {        // the largest of those that may be the maximum
+        double d = 0.0;
+        const float least = (float)top * (1.0f - 4.0f * V_ERR);
+        auto look = [&](int i, int g) {
+            float m = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(v[i][j]));
+            if (m >= least)
+#pragma unroll 1
+                for (int j = 0; j < 8; ++j) d = fmax(d, fabs(exact_value<OP, T>(a, row, g * 8 + j)));
+        };
+        if constexpr (G > 0) {
+#pragma unroll
+            for (int i = 0; i < G; ++i) look(i, t + i * THREADS);       // (groups that do not exist hold zeros)
+        } else
+            for (int g = t; g < groups; g += THREADS) { fetch(0, g, true); values(0, g, true); look(0, g); }
+        if (fabsf(v_tail) >= least) d = fmax(d, fabs(exact_value<OP, T>(a, row, c_tail)));
+        top = reduce_top(d);
+    }
+    if constexpr (OP == QOP_NORM) bad |= !(ss < INFINITY);
+    // a row that holds a NaN or an infinity has the scale NaN (and codes 0); one of zeros the scale 0
+    if (t == 0) {
+        const double rms = OP == QOP_NORM ? sqrt(ss / cols + a.eps) : 1.0;
+        a.scale[row] = bad ? NAN : top == 0.0 ? 0.0f : (float)(top / rms / 127.0);
+    }
+
+    // ---- the codes ---------------------------------------------------------------------------------------------------------------------
+    const bool none = bad || top == 0.0;
+    const float per = none || hard ? 0.0f : 127.0f / (float)top;     // (the rounding of top, the quotient and the product: under 2^-22)
+    int8_t* q = a.q + row * a.ldq;
+    // adding 1.5 * 2^23 rounds to a whole number, whose low byte is the code; far: how near to a border, half at most
+    auto code_bits = [&](float y, float& far) {
+        const float u = y * per, r = u + 12582912.0f;
+        far = fmaxf(far, fabsf(u - (r - 12582912.0f)));
+        return __float_as_uint(r);
+    };
+    auto exact_code = [&](int c) { return (int)rint(127.0 * exact_value<OP, T>(a, row, c) / top); };
+    auto codes = [&](int i, int g) {
+        unsigned bits[8], out[2];
+        float far = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) bits[j] = code_bits(v[i][j], far);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            out[k] = __builtin_amdgcn_perm(bits[4 * k + 1], bits[4 * k], 0x0C0C0400u) | __builtin_amdgcn_perm(bits[4 * k + 3], bits[4 * k + 2], 0x04000C0Cu);
+        if (none) out[0] = out[1] = 0u;
+        else if (hard || far > NEAR) {
+            unsigned long long o = 0;
+#pragma unroll 1
+            for (int j = 7; j >= 0; --j) o = o << 8 | (unsigned)(exact_code(g * 8 + j) & 0xFF);
+            out[0] = (unsigned)o; out[1] = (unsigned)(o >> 32);
+        }
+        __builtin_memcpy(q + g * 8, out, 8);
     };
     if constexpr (G > 0) {
 #pragma unroll
         for (int i = 0; i < G; ++i) if (t + i * THREADS < groups) codes(i, t + i * THREADS);
     } else
-        for (int g = t; g < groups; g += THREADS) { fetch(0, g, true); codes(0, g); }
+        for (int g = t; g < groups; g += THREADS) { fetch(0, g, true); values(0, g, true); codes(0, g); }
+    if (tail) {
+        float far = 0.f;
+        const unsigned b = code_bits(v_tail, far);
+        q[c_tail] = (int8_t)(none ? 0 : hard || far > NEAR ? exact_code(c_tail) : (int)(b & 0xFFu));
+    }
 }
 
+template <int OP, class T, int THREADS, int G> static void launch_body(const QuantArgs& a, hipStream_t s) {
+    constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1;
+    quantize_kernel<OP, T, THREADS, G><<<dim3((unsigned)((a.rows + ROWS - 1) / ROWS)), THREADS < 256 ? 256 : THREADS, 0, s>>>(a);
+}
+// Lanes per row: with many rows as few as keep a row in registers without costing occupancy (fewer partial sums to put together), with few
+// rows as many as shorten one row's time.  us, bf16, rows 20480 x 4096: 256 lanes 71, 512 88; 6143 x 12288: 256 lanes 68, 512 62, 1024 77,
+// (SwiGLU 133, 150, 205); 120 x 12288: 1024 lanes 6.5, 512 7.4, 256 9.8; 20480 x 512: 64 lanes 14, 256 22.
 template <int OP, class T> static void launch_quantize(const QuantArgs& a, hipStream_t s) {
-    const int groups = (a.cols + 7) / 8;
-#define QLAUNCH(THREADS, G) quantize_kernel<OP, T, THREADS, G><<<dim3((unsigned)((a.rows + (THREADS < 256 ? 256 / THREADS : 1) - 1) / (THREADS < 256 ? 256 / THREADS : 1))), THREADS < 256 ? 256 : THREADS, 0, s>>>(a)
-    if (groups <= 64) QLAUNCH(64, 1);
-    else if (groups <= 256) QLAUNCH(256, 1);
-    else if (groups <= 512) QLAUNCH(256, 2);
-    else if (groups <= 1024) QLAUNCH(1024, 1);
-    else if (groups <= 4096) QLAUNCH(1024, 4);
-    else QLAUNCH(1024, 0);
-#undef QLAUNCH
+    const int groups = a.cols / 8;
+    const bool many = a.rows >= 1024;
+    if (groups <= 64) launch_body<OP, T, 64, 1>(a, s);
+    else if (groups <= 128 && many) launch_body<OP, T, 64, 2>(a, s);
+    else if (groups <= 256) launch_body<OP, T, 256, 1>(a, s);
+    else if (groups <= 512) { if (many) launch_body<OP, T, 256, 2>(a, s); else launch_body<OP, T, 512, 1>(a, s); }
+    else if (groups <= 1024) { if (many) launch_body<OP, T, 256, 4>(a, s); else launch_body<OP, T, 1024, 1>(a, s); }
+    else if (groups <= 1536 && many) launch_body<OP, T, 256, 6>(a, s);
+    else if (groups <= 2048 && !many) launch_body<OP, T, 1024, 2>(a, s);
+    else if (groups <= 2560 && many) launch_body<OP, T, 512, 5>(a, s);
+    else if (groups <= 4096) launch_body<OP, T, 1024, 4>(a, s);
+    else launch_body<OP, T, 1024, 0>(a, s);
 }
 
 template <int OP> static int quantize(int type, const QuantArgs& a, hipStream_t s) {

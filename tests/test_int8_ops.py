@@ -2,9 +2,7 @@
 SwiGLU), the int8 product, a feed-forward made of them, their refusals and what they leave alone.
 
 Tolerances, all derived: a scale is one fp32 rounding of the exact value (2^-24 relative; 2^-23 allows the double chain's own
-errors next to a rounding border).  Codes of the plain rows and the norm equal the formula's.  SiLU(g) * u in fp32 is off by at most
-8 roundings' worth (expf 2 units in the last place = 4 half units, the sum, the quotient and the product one half unit each, rounded
-up): 2^-21 relative, as is the row's maximum, so a code's real value is off by at most 127 * 2^-20.  The product: an exact integer
+errors next to a rounding border).  Codes equal the formula's.  The product: an exact integer
 rounded to fp32, two products and a sum in fp32 (2^-24 each of the running value), then one rounding to the output's type."""
 import pytest
 import torch
@@ -116,14 +114,7 @@ def test_rmsnorm_quantize_equals_the_formula(rows, cols, dtype, residual):
 
 def check_swiglu(q, scale, gate, up):
     g = gate.double()
-    y = g / (1 + torch.exp(-g)) * up.double()
-    top = y.abs().amax(1, keepdim=True)
-    want = (top / 127)[:, 0]
-    assert ((scale.cpu().double() - want).abs() <= 2.0 ** -20 * want + 2.0 ** -149).all()
-    live = (top > 0)[:, 0]
-    off = (q.cpu().double() - 127 * y / top)[live].abs()
-    assert off.numel() == 0 or off.max() <= 0.5 + 127 * 2.0 ** -20
-    assert (q.cpu()[~live] == 0).all()
+    check_codes(q, scale, g / (1 + torch.exp(-g)) * up.double())
 
 
 @pytest.mark.gpu
@@ -363,7 +354,14 @@ def test_the_library_refuses_malformed_arguments_on_the_host():
                dict(ldw=-1), dict(ldc=31), dict(sa=p + 1), dict(sw=p + 2), dict(bias=p + 1), dict(C=p + 1), dict(C=p + 2, type=0)):
         assert gemm(**kw) == -1, kw
     assert gemm(M=0) == 0 and gemm(N=0, ldc=0) == 0
-    assert isinstance(lib.bb_gemm_int8_workspace_bytes(-1, 5, 5), int) and lib.bb_gemm_int8_workspace_bytes(0, 0, 0) == 0
+    # a workspace that is missing, too small or misaligned
+    big = dict(M=120, N=4096, K=12288, lda=12288, ldw=12288, ldc=4096)
+    need = lib.bb_gemm_int8_workspace_bytes(120, 4096, 12288, 1)
+    assert need > 0 and gemm(**big) == -3 and gemm(**big, ws=p, nws=need - 1) == -3 and gemm(**big, ws=p + 8, nws=need) == -1
+    odd = lib.bb_gemm_int8_workspace_bytes(120, 4096, 12288, 0)
+    assert odd >= need + (120 + 4096) * 12288 and gemm(**dict(big, lda=12289), ws=p, nws=odd - 1) == -3
+    for sizes in ((-1, 5, 5), (0, 0, 0), (0, 8, 8), (5, 5, 0), (5, 5, 131072), ((1 << 30) + 1, 5, 5)):
+        assert lib.bb_gemm_int8_workspace_bytes(*sizes, 1) == 0 and lib.bb_gemm_int8_workspace_bytes(*sizes, 0) == 0
 
 
 @pytest.mark.gpu
