@@ -154,68 +154,67 @@ def gemm_plan(M, N, K, wide=True, fusable=False):
 
 
 # ---- 8-bit integer operators --------------------------------------------------------------------
+# (what these calls do on the host counts where a kernel takes a few microseconds: no objects made, checks in one place each)
 _TYPES = None           # torch dtype -> BB_F32, BB_BF16, BB_F16
 
 
-def _types():
+def _type(dtype, what):
     global _TYPES
     if _TYPES is None:
         import torch
         _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-    return _TYPES
+    t = _TYPES.get(dtype)
+    if t is None:
+        raise BBError(f"{what}: expected float32, bfloat16 or float16, got {dtype}")
+    return t
 
 
-def _rows(t, name, dtype, shape, device):
-    """Row distance of a 2-D operand whose rows are contiguous; refuses any other."""
-    if t.dtype != dtype or t.device != device or t.shape != shape:
-        raise BBError(f"{name}: expected {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    if shape[1] > 1 and t.stride(1) != 1:
-        raise BBError(f"{name}: the elements of a row must be contiguous")
-    return t.stride(0)
+def _ld(t, what, dtype, shape, device):
+    """Row distance of a matrix whose rows are contiguous; refuses any other."""
+    if t.dtype is not dtype or t.shape != shape or t.device != device:
+        raise BBError(f"{what}: expected {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1:
+        raise BBError(f"{what}: the elements of a row must be contiguous")
+    return ld
 
 
-def _vector(t, name, dtype, n, device):
-    if t.dtype != dtype or t.device != device or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
-        raise BBError(f"{name}: expected contiguous {dtype} ({n},) on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+def _vec(t, what, dtype, n, device):
+    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != n or t.device != device or (n > 1 and t.stride(0) != 1):
+        raise BBError(f"{what}: expected contiguous {dtype} ({n},) on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-class _On:
-    """The device and stream of a call: tensors made inside belong to that stream."""
-
-    def __init__(self, device, stream):
-        import torch
-        if device.type != "cuda":
-            raise BBError(f"tensors must be on the GPU, got {device} (there is no CPU fallback)")
-        if stream is not None and stream.device != device:
+def _elsewhere(device, stream):
+    """None if a call on this device and stream can go ahead as things are, else the context it has to run in (in which what
+    it allocates belongs to that stream)."""
+    import torch
+    if device.type != "cuda":
+        raise BBError(f"tensors must be on the GPU, got {device} (there is no CPU fallback)")
+    if stream is not None:
+        if stream.device != device:
             raise BBError(f"the stream is of {stream.device}, the tensors are on {device}")
-        self._guard = torch.cuda.stream(stream) if stream is not None else \
-            torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
-        self.handle = (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+        return torch.cuda.stream(stream)
+    return None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
-    def __enter__(self):
-        if self._guard is not None:
-            self._guard.__enter__()
-        return self.handle
 
-    def __exit__(self, *a):
-        if self._guard is not None:
-            self._guard.__exit__(*a)
+def _raw_stream(device):
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device.index)     # (torch.cuda.current_stream without its 2 us)
 
 
 def _quantized(x, out, scale):
-    """Checks of what the three quantisers share; (q, its row distance, scale), made here where not given."""
+    """Outputs of the three quantisers, made where not given: (q, its row distance, scale, address of scale)."""
     import torch
-    if x.dim() != 2 or x.dtype not in _types():
-        raise BBError(f"expected a 2-D tensor of float32, bfloat16 or float16, got {x.dtype} {tuple(x.shape)}")
+    dev = x.device
+    if x.dim() != 2:
+        raise BBError(f"expected a matrix, got {tuple(x.shape)}")
     rows, cols = x.shape
     if out is None:         # (rows at multiples of 16 bytes, as the product reads them fastest)
-        out = torch.empty(rows, (cols + 15) // 16 * 16, dtype=torch.int8, device=x.device)[:, :cols]
+        out = torch.empty(rows, (cols + 15) // 16 * 16, dtype=torch.int8, device=dev)[:, :cols]
     if scale is None:
-        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
-    ldq = _rows(out, "out", torch.int8, x.shape, x.device)
-    _vector(scale, "scale", torch.float32, rows, x.device)
-    return out, ldq, scale
+        scale = torch.empty(rows, dtype=torch.float32, device=dev)
+    return out, _ld(out, "out", torch.int8, x.shape, dev), scale, _vec(scale, "scale", torch.float32, rows, dev)
 
 
 def _done(rc, what):
@@ -227,76 +226,89 @@ def quantize_rows(x, out=None, scale=None, stream=None):
     """bb_quantize_rows on torch CUDA tensors: x [rows][cols] fp32, bf16 or fp16 -> (q int8 [rows][cols], scale fp32
     [rows]) with q * scale standing for x.  q and scale are written in place where given.  The call is enqueued on
     `stream` (default: the current stream of x's device), on which what it makes is allocated too."""
-    lib = load_library()
-    with _On(x.device, stream) as st:
-        out, ldq, scale = _quantized(x, out, scale)
-        rows, cols = x.shape
-        _done(lib.bb_quantize_rows(x.data_ptr(), _rows(x, "x", x.dtype, x.shape, x.device), out.data_ptr(), ldq, scale.data_ptr(),
-                                   rows, cols, _types()[x.dtype], st), "bb_quantize_rows")
+    dev = x.device
+    ctx = _elsewhere(dev, stream)
+    if ctx is not None:
+        with ctx:
+            return quantize_rows(x, out, scale)
+    out, ldq, scale, ps = _quantized(x, out, scale)
+    rows, cols = x.shape
+    _done(load_library().bb_quantize_rows(x.data_ptr(), _ld(x, "x", x.dtype, x.shape, dev), out.data_ptr(), ldq, ps, rows, cols, _type(x.dtype, "x"),
+                                          _raw_stream(dev)), "bb_quantize_rows")
     return out, scale
 
 
 def rmsnorm_quantize(x, gain, eps, residual=None, residual_out=None, out=None, scale=None, stream=None):
     """bb_rmsnorm_quantize: h = x + residual -> residual_out (default: residual itself, in place), then RMSNorm(h) * gain
     with int8 rows; returns (q, scale).  Without a residual h = x.  gain has x's type.  Stream as in quantize_rows."""
-    lib = load_library()
-    with _On(x.device, stream) as st:
-        out, ldq, scale = _quantized(x, out, scale)
-        rows, cols = x.shape
-        res = h = None
-        ldr = ldh = 0
-        if residual is not None:
-            h = residual if residual_out is None else residual_out
-            ldr, ldh = _rows(residual, "residual", x.dtype, x.shape, x.device), _rows(h, "residual_out", x.dtype, x.shape, x.device)
-            res, h = residual.data_ptr(), h.data_ptr()
-        elif residual_out is not None:
-            raise BBError("residual_out without a residual")
-        _done(lib.bb_rmsnorm_quantize(x.data_ptr(), _rows(x, "x", x.dtype, x.shape, x.device), res, ldr, h, ldh,
-                                      _vector(gain, "gain", x.dtype, cols, x.device), eps, out.data_ptr(), ldq, scale.data_ptr(),
-                                      rows, cols, _types()[x.dtype], st), "bb_rmsnorm_quantize")
+    dev = x.device
+    ctx = _elsewhere(dev, stream)
+    if ctx is not None:
+        with ctx:
+            return rmsnorm_quantize(x, gain, eps, residual, residual_out, out, scale)
+    out, ldq, scale, ps = _quantized(x, out, scale)
+    dtype, shape = x.dtype, x.shape
+    rows, cols = shape
+    res = h = None
+    ldr = ldh = 0
+    if residual is not None:
+        if residual_out is None:
+            residual_out = residual
+        ldr, ldh = _ld(residual, "residual", dtype, shape, dev), _ld(residual_out, "residual_out", dtype, shape, dev)
+        res, h = residual.data_ptr(), residual_out.data_ptr()
+    elif residual_out is not None:
+        raise BBError("residual_out without a residual")
+    _done(load_library().bb_rmsnorm_quantize(x.data_ptr(), _ld(x, "x", dtype, shape, dev), res, ldr, h, ldh, _vec(gain, "gain", dtype, cols, dev), eps,
+                                             out.data_ptr(), ldq, ps, rows, cols, _type(dtype, "x"), _raw_stream(dev)), "bb_rmsnorm_quantize")
     return out, scale
 
 
 def swiglu_quantize(gate, up, out=None, scale=None, stream=None):
     """bb_swiglu_quantize: SiLU(gate) * up with int8 rows; returns (q, scale).  gate and up may be the two halves of one
     tensor's columns.  Stream as in quantize_rows."""
-    lib = load_library()
-    with _On(gate.device, stream) as st:
-        out, ldq, scale = _quantized(gate, out, scale)
-        rows, cols = gate.shape
-        _done(lib.bb_swiglu_quantize(gate.data_ptr(), _rows(gate, "gate", gate.dtype, gate.shape, gate.device), up.data_ptr(),
-                                     _rows(up, "up", gate.dtype, gate.shape, gate.device), out.data_ptr(), ldq, scale.data_ptr(),
-                                     rows, cols, _types()[gate.dtype], st), "bb_swiglu_quantize")
+    dev = gate.device
+    ctx = _elsewhere(dev, stream)
+    if ctx is not None:
+        with ctx:
+            return swiglu_quantize(gate, up, out, scale)
+    out, ldq, scale, ps = _quantized(gate, out, scale)
+    dtype, shape = gate.dtype, gate.shape
+    rows, cols = shape
+    _done(load_library().bb_swiglu_quantize(gate.data_ptr(), _ld(gate, "gate", dtype, shape, dev), up.data_ptr(), _ld(up, "up", dtype, shape, dev),
+                                            out.data_ptr(), ldq, ps, rows, cols, _type(dtype, "gate"), _raw_stream(dev)), "bb_swiglu_quantize")
     return out, scale
 
 
 def gemm_int8(a, a_scale, w, w_scale, bias=None, out=None, dtype=None, stream=None):
     """bb_gemm_int8: out[m][n] = (sum_k a[m][k] w[n][k]) * a_scale[m] * w_scale[n] + bias[n]; a [M][K], w [N][K] int8,
     scales and bias fp32.  out: fp32, bf16 or fp16 [M][N], made here (of `dtype`, default bf16) where not given.  Stream as in
-    quantize_rows; the workspace is allocated on it for this call alone."""
+    quantize_rows; a workspace, where the product needs one, is allocated on it for this call alone."""
     import torch
-    lib = load_library()
     dev = a.device
-    with _On(dev, stream) as st:
-        if a.dim() != 2 or w.dim() != 2:
-            raise BBError(f"expected 2-D operands, got {tuple(a.shape)} and {tuple(w.shape)}")
-        (M, K), N = a.shape, w.shape[0]
-        lda, ldw = _rows(a, "a", torch.int8, a.shape, dev), _rows(w, "w", torch.int8, torch.Size((N, K)), dev)
-        sa, sw = _vector(a_scale, "a_scale", torch.float32, M, dev), _vector(w_scale, "w_scale", torch.float32, N, dev)
-        b = None if bias is None else _vector(bias, "bias", torch.float32, N, dev)
-        if out is None:
-            out = torch.empty(M, N, dtype=dtype or torch.bfloat16, device=dev)
-        elif dtype is not None and out.dtype != dtype:
-            raise BBError(f"out has {out.dtype}, dtype says {dtype}")
-        if out.dtype not in _types():
-            raise BBError(f"out: expected float32, bfloat16 or float16, got {out.dtype}")
-        ldc = _rows(out, "out", out.dtype, torch.Size((M, N)), dev)
-        pa, pw = a.data_ptr(), w.data_ptr()
-        lda, ldw = lda if M > 1 else 0, ldw if N > 1 else 0
-        nbytes = lib.bb_gemm_int8_workspace_bytes(M, N, K, int((pa | pw | lda | ldw) % 16 == 0 and lda <= 1 << 23 and ldw <= 1 << 23))
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-        _done(lib.bb_gemm_int8(pa, lda, sa, pw, ldw, sw, b, out.data_ptr(), ldc, _types()[out.dtype], M, N, K,
-                               ws.data_ptr() if nbytes else None, nbytes, st), "bb_gemm_int8")
+    ctx = _elsewhere(dev, stream)
+    if ctx is not None:
+        with ctx:
+            return gemm_int8(a, a_scale, w, w_scale, bias, out, dtype)
+    if a.dim() != 2 or w.dim() != 2:
+        raise BBError(f"expected matrices, got {tuple(a.shape)} and {tuple(w.shape)}")
+    (M, K), N, i8, f32 = a.shape, w.shape[0], torch.int8, torch.float32
+    lda, ldw = _ld(a, "a", i8, (M, K), dev), _ld(w, "w", i8, (N, K), dev)
+    sa, sw = _vec(a_scale, "a_scale", f32, M, dev), _vec(w_scale, "w_scale", f32, N, dev)
+    b = None if bias is None else _vec(bias, "bias", f32, N, dev)
+    if out is None:
+        out = torch.empty(M, N, dtype=dtype or torch.bfloat16, device=dev)
+    elif dtype is not None and out.dtype is not dtype:
+        raise BBError(f"out has {out.dtype}, dtype says {dtype}")
+    ct = _type(out.dtype, "out")
+    ldc = _ld(out, "out", out.dtype, (M, N), dev)
+    pa, pw, lib = a.data_ptr(), w.data_ptr(), load_library()
+    if M == 1:
+        lda = 0
+    if N == 1:
+        ldw = 0
+    nbytes = lib.bb_gemm_int8_workspace_bytes(M, N, K, (pa | pw | lda | ldw) % 16 == 0 and lda <= 1 << 23 and ldw <= 1 << 23)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    _done(lib.bb_gemm_int8(pa, lda, sa, pw, ldw, sw, b, out.data_ptr(), ldc, ct, M, N, K, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(dev)), "bb_gemm_int8")
     return out
 
 
