@@ -264,6 +264,16 @@ int bb_debug_wide_format(bb_ctx* ctx, int on);
 int bb_gemm_static(const float* A_dev, const uint16_t* W_dev, float* C_dev, int M, int N, int K, int split_k,
                    void* hip_stream);
 
+/* Layer GEMMs in 8-bit integers: from the next forward on every layer's projections run as int8 products (bb_gemm_int8
+ * below) of rows quantised per token, where they are made (norm, attention, SwiGLU), with weights quantised per output
+ * channel; embeddings, norms, attention, K,V and the LM head stay as they are.  A block step then streams a byte per weight instead of two.
+ * mem_dev: device memory of at least bb_int8_layers_bytes(ctx), 256-byte aligned, which the context uses until it is destroyed or the
+ * call is made again (mem_dev == NULL: the format is switched off); a call that takes memory away waits for the stream first.  The codes are made from the loaded weights by
+ * the next forward, and again after bb_load_weights.  The tuning knobs of the other formats (bb_debug_set_gemm_plan,
+ * bb_debug_wide_format) have no effect meanwhile. */
+size_t bb_int8_layers_bytes(bb_ctx* ctx);
+int bb_int8_layers(bb_ctx* ctx, void* mem_dev, size_t bytes);
+
 /* ---- 8-bit integer operators ---------------------------------------------------------------------
  * Rows quantised to int8 with one fp32 scale each, and the product of such rows with such weights.  No context is
  * needed; all work is enqueued on hip_stream (a hipStream_t of the current device, NULL = its default stream); nothing is

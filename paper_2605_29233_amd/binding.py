@@ -65,7 +65,7 @@ _LIB = None
 EXPORTS = ("bb_workspace_bytes", "bb_create", "bb_destroy", "bb_last_error", "bb_load_weights", "bb_request_open",
            "bb_request_close", "bb_refresh", "bb_denoise_step", "bb_merge_commit", "bb_get_tokens", "bb_get_stats",
            "bb_get_view", "bb_set_state", "bb_get_kv", "bb_set_kv", "bb_read_device", "bb_synchronize", "bb_debug_gemm", "bb_debug_gemm_wide", "bb_debug_wide_format", "bb_profile_enable", "bb_profile_read", "bb_debug_set_gemm_plan", "bb_debug_gemm_plan", "bb_debug_attention_plan", "bb_debug_copy16", "bb_generate", "bb_kv_diag_scratch_bytes", "bb_kv_diagnostics", "bb_gemm_static", "bb_debug_mfma_rate", "bb_debug_keep_logits",
-           "bb_quantize_rows", "bb_rmsnorm_quantize", "bb_swiglu_quantize", "bb_gemm_int8", "bb_gemm_int8_workspace_bytes")
+           "bb_quantize_rows", "bb_rmsnorm_quantize", "bb_swiglu_quantize", "bb_gemm_int8", "bb_gemm_int8_workspace_bytes", "bb_int8_layers", "bb_int8_layers_bytes")
 KERNEL_CLASSES = ("gemm_skinny", "gemm_wide", "attention", "glue", "policy")
 
 
@@ -125,6 +125,9 @@ def load_library():
         lib.bb_gemm_int8.argtypes = [ptr, i64, ptr, ptr, i64, ptr, ptr, ptr, i64, i32, i32, i32, i32, ptr, C.c_size_t, ptr]
         lib.bb_gemm_int8_workspace_bytes.argtypes = [i32, i32, i32, i32]
         lib.bb_gemm_int8_workspace_bytes.restype = C.c_size_t
+        lib.bb_int8_layers_bytes.argtypes = [ptr]
+        lib.bb_int8_layers_bytes.restype = C.c_size_t
+        lib.bb_int8_layers.argtypes = [ptr, ptr, C.c_size_t]
         _LIB = lib
     return _LIB
 
@@ -393,7 +396,7 @@ class BlockBatch:
         if self._ctx:
             self.lib.bb_destroy(self._ctx)
             self._ctx = C.c_void_p()
-            self._ws = None
+            self._ws = self._i8 = None
 
     def __del__(self):
         try:
@@ -411,6 +414,19 @@ class BlockBatch:
             rows, cols = (t.shape[0], t.shape[1]) if t.dim() == 2 else (1, t.numel())
             bt = bb_tensor(name.encode(), C.c_void_p(t.data_ptr()), int(t.is_cuda), rows, cols)
             self._chk(self.lib.bb_load_weights(self._ctx, C.byref(bt), 1), f"bb_load_weights({name})")
+
+    def int8_layers(self, on=True):
+        """bb_int8_layers: the layers' products in 8-bit integers from the next forward on (memory for the codes is allocated here),
+        or, with on=False, as before."""
+        import torch
+        mem, n, base = None, 0, None
+        if on:
+            n = self.lib.bb_int8_layers_bytes(self._ctx)
+            mem = torch.empty(n + 256, dtype=torch.uint8, device=self.device)
+            torch.cuda.current_stream(self.device).synchronize()        # (what used that memory before it was freed may still run there)
+            base = C.c_void_p((mem.data_ptr() + 255) // 256 * 256)
+        self._chk(self.lib.bb_int8_layers(self._ctx, base, n), "bb_int8_layers")
+        self._i8 = mem          # (released only once the library has let go of it)
 
     def request_open(self, prompt, gen_len, block_sizes):
         p = np.ascontiguousarray(prompt, dtype=np.int32)

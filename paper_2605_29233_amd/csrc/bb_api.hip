@@ -18,6 +18,10 @@ struct LayerW {
     float *g_attn, *g_ffn, *bqkv;       // fp32
 };
 
+// The int8 layers' own memory (bb_int8_layers): weights as codes with a scale per row, the codes of the rows on their way into a product.
+struct Int8Matrix { int8_t* q; float* scale; };
+struct Int8Layer { Int8Matrix qkv, o, gu, down; bool stale; };       // stale: the weights were loaded after the codes were made
+
 struct HostReq { int in_use, L_p, G, L, N, blocks[BB_MAX_BRANCHES], initialised; };
 
 struct bb_ctx {
@@ -42,6 +46,8 @@ struct bb_ctx {
     std::string err;
     int last_forward_rows, last_lm_cap;
     int wide_off;                       // tests: the layer GEMMs use two bf16 terms like the LM head (bb_debug_wide_format)
+    std::vector<Int8Layer> i8;          // empty: off
+    int8_t* i8_rows; float* i8_scales; char* i8_part; size_t i8_part_bytes;
     int keep_logits;                    // tests: the LM head also stores its fp32 logits (bb_debug_keep_logits)
     // per-launch event timing (bb_profile_*)
     int prof_on;
@@ -385,6 +391,7 @@ static int load_one(bb_ctx* c, const bb_tensor& t) {
         }
     } else return fail(c, BB_EINVAL, "unknown tensor " + name);
     if (!ok) return fail(c, BB_EINVAL, "shape mismatch for " + name);
+    if (slot >= 3 && !c->i8.empty()) c->i8[(slot - 3) / 12].stale = true;
     HIPCHK(c, hipGetLastError());
     if (!t.on_device) HIPCHK(c, hipStreamSynchronize(c->stream));      // staging is reused by the next tensor
     c->loaded[slot] = 1;
@@ -460,6 +467,104 @@ static int check_reqs(bb_ctx* c, const int* ids, int n, bool need_init) {
     return BB_OK;
 }
 
+// ---- int8 layers ------------------------------------------------------------------------------------
+static void int8_layout(const bb_ctx* c, char* base, size_t* total, std::vector<Int8Layer>* layers, int8_t** rows, float** scales, char** part, size_t* part_bytes) {
+    const bb_model_cfg& m = c->m; const Dev& D = c->D;
+    const int nq = m.n_q_heads * m.head_dim, rows_pad = (D.rows_cap + 31) / 32 * 32;
+    Bump b{base, 0};
+    auto matrix = [&](int N, int K) { Int8Matrix x; x.q = b.take<int8_t>((size_t)N * K); x.scale = b.take<float>(N); return x; };
+    layers->resize(m.n_layers);
+    for (auto& L : *layers) { L.qkv = matrix(D.nqkv, m.d_model); L.o = matrix(m.d_model, nq); L.gu = matrix(2 * m.d_ffn, m.d_model); L.down = matrix(m.d_model, m.d_ffn); L.stale = true; }
+    *rows = b.take<int8_t>((size_t)rows_pad * std::max(std::max(m.d_model, m.d_ffn), nq));
+    *scales = b.take<float>(rows_pad);
+    *part_bytes = 0;                    // (k is split where there are few rows; a product that finds less room than it would take splits less)
+    for (int r = 32; r <= std::min(rows_pad, 1024); r += 32)
+        for (const auto& s : {std::make_pair(D.nqkv, m.d_model), std::make_pair(m.d_model, nq), std::make_pair(2 * m.d_ffn, m.d_model), std::make_pair(m.d_model, m.d_ffn)})
+            *part_bytes = std::max(*part_bytes, gemm_int8_partial_bytes(r, s.first, s.second));
+    *part = b.take<char>(*part_bytes);
+    *total = align_up(b.off, 256);
+}
+
+static size_t bb_int8_layers_bytes_impl(bb_ctx* c) {
+    std::vector<Int8Layer> layers; int8_t* rows; float* scales; char* part; size_t part_bytes, total = 0;
+    int8_layout(c, nullptr, &total, &layers, &rows, &scales, &part, &part_bytes);
+    return total;
+}
+
+static int bb_int8_layers_impl(bb_ctx* c, void* mem, size_t bytes) {
+    if (!c) return BB_EINVAL;
+    if (!mem) {
+        HIPCHK(c, hipStreamSynchronize(c->stream));
+        c->i8.clear();
+        return BB_OK;
+    }
+    if (reinterpret_cast<uintptr_t>(mem) % 256) return fail(c, BB_EINVAL, "the int8 layers' memory must be 256-byte aligned");
+    if (bytes < bb_int8_layers_bytes_impl(c)) return fail(c, BB_ENOMEM, "less memory than bb_int8_layers_bytes");
+    if (!c->i8.empty()) HIPCHK(c, hipStreamSynchronize(c->stream));     // (the memory given before is the caller's again)
+    std::vector<Int8Layer> layers;
+    size_t total = 0;
+    int8_layout(c, (char*)mem, &total, &layers, &c->i8_rows, &c->i8_scales, &c->i8_part, &c->i8_part_bytes);
+    c->i8.swap(layers);
+    return BB_OK;
+}
+
+// The codes of one layer's matrices from their tiled bf16 copies (exact), as many rows at a time as the staging buffer holds.
+static int int8_weights(bb_ctx* c, int li) {
+    const bb_model_cfg& m = c->m;
+    const LayerW& W = c->layers[li];
+    Int8Layer& L = c->i8[li];
+    auto matrix = [&](const u32x4* tiles, const Int8Matrix& x, int N, int K, int interleaved) {
+        const int step = (int)std::min<size_t>(N, c->stage_bytes / ((size_t)K * 2));
+        int rc = BB_OK;
+        for (int r = 0; r < N && rc == BB_OK; r += step) {
+            const int n = std::min(step, N - r);
+            launch_untile_weights(tiles, K, interleaved, r, n, (uint16_t*)c->stage, c->stream);
+            rc = bb_quantize_rows(c->stage, K, x.q + (size_t)r * K, K, x.scale + r, n, K, BB_BF16, c->stream);
+        }
+        return rc;
+    };
+    const int nq = m.n_q_heads * m.head_dim;
+    int rc = matrix(W.wqkv, L.qkv, c->D.nqkv, m.d_model, 0);
+    if (rc == BB_OK) rc = matrix(W.wo, L.o, m.d_model, nq, 0);
+    if (rc == BB_OK) rc = matrix(W.wgu, L.gu, 2 * m.d_ffn, m.d_model, m.d_ffn);
+    if (rc == BB_OK) rc = matrix(W.wdown, L.down, m.d_model, m.d_ffn, 0);
+    if (rc != BB_OK) return fail(c, rc, "quantising the weights failed");
+    L.stale = false;
+    return BB_OK;
+}
+
+// All layers of a forward with int8 products: each projection's input rows quantised where they are made, weights as codes per output channel,
+// fp32 out.  Leaves the last down projection's output in c->part, as the plain layers do with one partial result.
+static int int8_layers(bb_ctx* c, int rows_cap, int mode, int seg_base, int n_segs, int max_seg_rows, int max_pages, int seg_tiles, int gk) {
+    const bb_model_cfg& m = c->m; const Dev& D = c->D; hipStream_t s = c->stream;
+    const int d = m.d_model, nq = m.n_q_heads * m.head_dim, f = m.d_ffn, mt = (rows_cap + 31) / 32;
+    for (int li = 0; li < m.n_layers; ++li)
+        if (c->i8[li].stale) { const int rc = int8_weights(c, li); if (rc != BB_OK) return rc; }
+    auto gemm = [&](const Int8Matrix& W, float* out, int N, int K) {
+        PROF(gk, (double)N * K, 2.0 * rows_cap * (double)N * K);
+        launch_gemm_int8(c->i8_rows, K, c->i8_scales, W.q, K, W.scale, out, N, rows_cap, N, K, c->i8_part, c->i8_part_bytes, D.counts, s);
+    };
+    for (int li = 0; li < m.n_layers; ++li) {
+        const LayerW& W = c->layers[li];
+        const Int8Layer& Q = c->i8[li];
+        { PROF(BB_K_GLUE, 0, 0);
+          if (li == 0) launch_embed(D, c->emb, c->h, rows_cap, s);
+          launch_rmsnorm_quantize(li == 0 ? c->h : c->part, li == 0 ? nullptr : c->h, W.g_attn, m.rms_eps, c->i8_rows, d, c->i8_scales, rows_cap, d, D.counts, s); }
+        c->prof_chain = true;
+        gemm(Q.qkv, c->qkv, D.nqkv, d);
+        { PROF(BB_K_GLUE, 0, 0); launch_qkv_epilogue(D, c->qkv, 1, 0, m.qkv_bias ? W.bqkv : nullptr, c->Q, li, rows_cap, nullptr, 0, s); }
+        if (mode == 2 && li == m.n_layers - 1) break;
+        { PROF(BB_K_ATTENTION, 0, 0); launch_attention(D, c->Q, c->Apk, li, mt, max_seg_rows, seg_base, n_segs, max_pages, seg_tiles, c->attn_part, c->attn_part_elems, 0, s); }
+        { PROF(BB_K_GLUE, 0, 0); launch_panel_quantize(c->Apk, mt, c->i8_rows, nq, c->i8_scales, rows_cap, nq, D.counts, s); }
+        gemm(Q.o, c->part, d, nq);
+        { PROF(BB_K_GLUE, 0, 0); launch_rmsnorm_quantize(c->part, c->h, W.g_ffn, m.rms_eps, c->i8_rows, d, c->i8_scales, rows_cap, d, D.counts, s); }
+        gemm(Q.gu, c->gu, 2 * f, d);
+        { PROF(BB_K_GLUE, 0, 0); launch_swiglu_quantize(c->gu, c->gu + f, 2L * f, c->i8_rows, f, c->i8_scales, rows_cap, f, D.counts, s); }
+        gemm(Q.down, c->part, d, f);
+    }
+    return BB_OK;
+}
+
 // ---- the forward -----------------------------------------------------------------------------------
 // mode 0: block step with LM head; 1: initial full forward with LM head over lm_cap rows
 // (results broadcast to all branches); 2: cache-only refresh (stops after the last K,V write).
@@ -499,6 +604,11 @@ static int forward(bb_ctx* c, int rows_cap, int lm_cap, int mode, int seg_base, 
     c->prof_chain = false;              // the first launch records its own start
     int s_down = 0;
     const size_t pstride = (size_t)rows_pad * d;
+    if (!c->i8.empty()) {
+        const int rc = int8_layers(c, rows_cap, mode, seg_base, n_segs, max_seg_rows, max_pages, seg_tiles, gk);
+        if (rc != BB_OK) return rc;
+        s_down = m.n_layers > 0;
+    } else
     for (int li = 0; li < m.n_layers; ++li) {
         const LayerW& W = c->layers[li];
         // few rows: the norm's scale is applied after the projection (see residual_pack_kernel)
@@ -1099,6 +1209,14 @@ extern "C" int bb_debug_attention_plan(const bb_model_cfg* model, const bb_limit
         out[0] = p.n_splits; out[1] = p.waves;
         return BB_OK;
     } catch (...) { return BB_ENOMEM; }
+}
+
+extern "C" size_t bb_int8_layers_bytes(bb_ctx* c) {
+    try { return c ? bb_int8_layers_bytes_impl(c) : 0; } catch (...) { return 0; }
+}
+
+extern "C" int bb_int8_layers(bb_ctx* c, void* mem_dev, size_t bytes) {
+    BB_GUARD(c, bb_int8_layers_impl(c, mem_dev, bytes));
 }
 
 extern "C" int bb_debug_wide_format(bb_ctx* c, int on) {

@@ -270,3 +270,18 @@ void launch_write_kv(const Dev& D, int phys_table_row_slot, int branch, int laye
 void launch_kv_sqdist(const Dev& D, int gbr_a, int gbr_b, const half_t* snapK, const half_t* snapV, int snap_rows, int b_row,
                       int n_pages_used, double* out, hipStream_t s);
 void launch_kv_snapshot(const Dev& D, int gbr, half_t* snapK, half_t* snapV, int snap_rows, int row, int n_pages_used, hipStream_t s);
+
+// ---- int8 layers (quantize.hip, gemm_int8.hip): the launches behind the 8-bit operators, on the rows of a forward of which *live count --------------
+// residual (null: x alone) += x, then the RMSNorm of it
+void launch_rmsnorm_quantize(const float* x, float* residual, const float* gain, float eps, int8_t* q, long ldq, float* scale, long rows, int cols,
+                             const int* live, hipStream_t s);
+void launch_swiglu_quantize(const float* gate, const float* up, long ld, int8_t* q, long ldq, float* scale, long rows, int cols, const int* live, hipStream_t s);
+void launch_panel_quantize(const u32x4* Apk, int mt_total, int8_t* q, long ldq, float* scale, long rows, int cols, const int* live, hipStream_t s);
+void launch_gemm_int8(const int8_t* A, long lda, const float* sa, const int8_t* W, long ldw, const float* sw, float* C, long ldc, int M, int N, int K,
+                      void* ws, size_t ws_bytes, const int* live, hipStream_t s);
+size_t gemm_int8_partial_bytes(int M, int N, int K);
+// h = the token embeddings of the packed rows
+void launch_embed(const Dev& D, const uint16_t* emb, float* h, int rows_cap, hipStream_t s);
+// Rows row0 .. row0 + n of a matrix from its tiled bf16 copy, row-major.  interleaved > 0: the fused gate/up matrix of that many features, whose rows
+// are asked for as all of gate, then all of up.
+void launch_untile_weights(const u32x4* tiles, int K, int interleaved, int row0, int n, uint16_t* dst, hipStream_t s);

@@ -251,6 +251,19 @@ void launch_rmsnorm_pack(const Dev& D, float* h, const float* partial, int n_par
         rmsnorm_pack_kernel<256><<<mt_total * 32, 256, 0, s>>>(D, h, partial, n_partial, partial_stride, gain, Apk, mt_total, gather, bcast, wide, emb);
 }
 
+// The embeddings as a launch of their own (the int8 layers' norm does not gather).
+__global__ __launch_bounds__(256) void embed_kernel(Dev D, const uint16_t* __restrict__ emb, float* __restrict__ h) {
+    const int row = blockIdx.x;
+    if (row >= D.counts[0]) return;
+    for (int k8 = threadIdx.x; k8 < D.d >> 3; k8 += 256) {
+        float4 a, b;
+        load_stream8(D, nullptr, emb, row, k8, a, b);
+        reinterpret_cast<float4*>(h + (size_t)row * D.d)[2 * k8] = a;
+        reinterpret_cast<float4*>(h + (size_t)row * D.d)[2 * k8 + 1] = b;
+    }
+}
+void launch_embed(const Dev& D, const uint16_t* emb, float* h, int rows_cap, hipStream_t s) { embed_kernel<<<rows_cap, 256, 0, s>>>(D, emb, h); }
+
 // Few rows (block steps): the norm's row-wide sum would leave one workgroup per row with the whole row's partial tiles
 // to read, and half the CUs idle.  RMSNorm's scale is one number per row and commutes with the projection that follows:
 // (x / rms(x) * gain) W^T = (x * gain) W^T / rms(x).  So this kernel only adds the split-K partials to the residual,

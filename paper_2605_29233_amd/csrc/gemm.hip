@@ -624,6 +624,24 @@ void launch_tile_weights(const uint16_t* src, int rows, int K, u32x4* dst, int d
                                                                     interleave, (K + 63) / 64 * 4);
 }
 
+__global__ void untile_weights_kernel(const u32x4* __restrict__ tiles, int k8s, int ksteps_pad, int interleaved, int row0, int n, u32x4* __restrict__ dst) {
+    const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= (size_t)n * k8s) return;
+    int r = row0 + (int)(i / k8s);
+    const int k8 = (int)(i % k8s);
+    if (interleaved) {
+        const int up = r >= interleaved;
+        r -= up * interleaved;
+        r = r / 32 * 64 + r % 32 + 32 * up;
+    }
+    dst[i] = tiles[tileW_u4(r, k8, ksteps_pad)];
+}
+
+void launch_untile_weights(const u32x4* tiles, int K, int interleaved, int row0, int n, uint16_t* dst, hipStream_t s) {
+    const size_t pieces = (size_t)n * (K / 8);
+    untile_weights_kernel<<<(unsigned)((pieces + 255) / 256), 256, 0, s>>>(tiles, K / 8, (K + 63) / 64 * 4, interleaved, row0, n, reinterpret_cast<u32x4*>(dst));
+}
+
 // fp32 row-major [M][K] -> packed hi/lo fragments; rows >= M and columns >= K (padding to whole chunks) are zero.
 __global__ void pack_rows_kernel(const float* __restrict__ A, int M, int K, u32x4* __restrict__ Apk, int mt_total) {
     size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;

@@ -20,6 +20,7 @@ struct GemmInt8Args {
     const int8_t *A, *W; const float *sa, *sw, *bias; void* C;
     long lda, ldw, ldc;
     int M, N, K, type;
+    const int* live;                // rows of A that count, on the device (null: all M; only the tiled kernel is asked for fewer)
 };
 
 // Four consecutive columns of a row of C, as far as they exist.
@@ -171,6 +172,12 @@ template <int BM, int BN> static __device__ __forceinline__ Item item_of(const T
     return it;
 }
 
+static __device__ __forceinline__ void only_live(TiledArgs& ta, int bm) {
+    if (!ta.g.live) return;
+    ta.g.M = __builtin_amdgcn_readfirstlane(min(ta.g.M, *ta.g.live));
+    ta.tiles_m = (ta.g.M + bm - 1) / bm;
+}
+
 template <int R, int T, int WM, int NS, int PER_CU>
 __global__ __launch_bounds__(256, PER_CU) void gemm_int8_tiled_kernel(TiledArgs ta) {
     constexpr int WN = 4 / WM, FA = R * WM, FW = T * WN, BM = 16 * FA, BN = 16 * FW, U = 2 * (FA + FW), L = U / 4, LA = FA / 2, SLOT = U * 1024;
@@ -178,6 +185,7 @@ __global__ __launch_bounds__(256, PER_CU) void gemm_int8_tiled_kernel(TiledArgs 
     constexpr int SM = (BM + 63) / 64 * 64, SN = (BN + 63) / 64 * 64, SCALES = SM + 2 * SN;        // scales of an item: rows', columns', biases
     __shared__ __attribute__((aligned(16))) char lds[NS * SLOT + (NS + 2) * SCALES * 4];
     float* const scales = reinterpret_cast<float*>(lds + NS * SLOT);
+    only_live(ta, BM);
     const GemmInt8Args& a = ta.g;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
     const int wm = wave % WM, wn = wave / WM;
@@ -336,9 +344,11 @@ template <int R, int T, int WM>
 __global__ __launch_bounds__(256) void gemm_int8_join_kernel(TiledArgs ta) {
     constexpr int WN = 4 / WM;
     __shared__ __attribute__((aligned(16))) float scales[4][2][16 * T];
+    only_live(ta, 16 * R * WM);
     const GemmInt8Args& a = ta.g;
     const int sub = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), idx = blockIdx.x * 4 + sub, lane = threadIdx.x & 63;
     const int tiles = ta.tiles_m * ta.tiles_n, wave = idx / R % 4, r = idx % R;
+    if (idx >= tiles * 4 * R) return;
     const Item it = item_of<16 * R * WM, 16 * T * WN>(ta, idx / (4 * R));
     const int m = it.m0 + (wave % WM * R + r) * 16, n = it.n0 + wave / WM * T * 16;
     if (m >= a.M || n >= a.N) return;                       // (whole waves, and no barrier below)
@@ -390,7 +400,7 @@ static const Int8Body i8_bodies[] = {
 };
 #define I8_MAX_PARTIAL ((size_t)1 << 28)
 struct Int8Plan { int body, split; size_t partial_bytes; };
-static Int8Plan int8_plan(int M, int N, int K) {
+static Int8Plan int8_plan(int M, int N, int K, size_t most = I8_MAX_PARTIAL) {
     Int8Plan best{0, 1, 0};
     float best_cost = INFINITY;
     const int chunks = (K + 127) / 128;
@@ -400,7 +410,7 @@ static Int8Plan int8_plan(int M, int N, int K) {
         const size_t tiles = ((size_t)M + b.bm - 1) / b.bm * (((size_t)N + b.bn - 1) / b.bn);
         for (int split : {1, 2, 3, 4, 6, 8, 12, 16}) {
             const size_t items = tiles * split, partial = split > 1 ? items * b.bm * b.bn * 4 : 0;
-            if (split > 1 && (split > chunks || partial > I8_MAX_PARTIAL)) break;
+            if (split > 1 && (split > chunks || partial > most)) break;
             const float per = (float)((items + 255) / 256), rounds = ceilf(per / b.per_cu), c = (float)((chunks + split - 1) / split);
             const float main = b.start + rounds * b.round + rounds * c * b.chunk + per / b.per_cu * c * b.shared;
             float cost = sqrtf(sqrtf(main * main * main * main + stream * stream * stream * stream));
@@ -410,6 +420,25 @@ static Int8Plan int8_plan(int M, int N, int K) {
     }
     return best;
 }
+
+static void launch_plan(const GemmInt8Args& a, const Int8Plan& p, void* workspace_dev, hipStream_t s) {
+    switch (p.body) {
+        case 0: launch_tiled<8, 8, 2, 2, 1>(a, p.split, workspace_dev, s); break;
+        case 1: launch_tiled<8, 6, 2, 2, 1>(a, p.split, workspace_dev, s); break;
+        case 2: launch_tiled<4, 4, 2, 2, 2>(a, p.split, workspace_dev, s); break;
+        case 3: launch_tiled<4, 2, 2, 3, 2>(a, p.split, workspace_dev, s); break;
+        case 4: launch_tiled<2, 2, 2, 4, 2>(a, p.split, workspace_dev, s); break;
+        default: launch_tiled<1, 1, 2, 4, 3>(a, p.split, workspace_dev, s); break;
+    }
+}
+
+// The layers of a forward: aligned operands, fp32 out, as many splits as the workspace has room for.
+void launch_gemm_int8(const int8_t* A, long lda, const float* sa, const int8_t* W, long ldw, const float* sw, float* C, long ldc, int M, int N, int K,
+                      void* ws, size_t ws_bytes, const int* live, hipStream_t s) {
+    GemmInt8Args a{A, W, sa, sw, nullptr, C, lda, ldw, ldc, M, N, K, BB_F32, live};
+    launch_plan(a, int8_plan(M, N, K, std::min(ws_bytes, I8_MAX_PARTIAL)), ws, s);
+}
+size_t gemm_int8_partial_bytes(int M, int N, int K) { return int8_plan(M, N, K).partial_bytes; }
 
 // Rows that are not 16-byte aligned: up to I8_ANY_ROWS rows of A the kernel for any alignment (M = 64, 24576 x 4096 matrix: X us against
 // Y with aligned copies), above aligned copies of both operands in the workspace and the tiled kernel.
@@ -440,7 +469,7 @@ extern "C" int bb_gemm_int8(const int8_t* A_dev, long lda, const float* a_scale_
     const size_t need = bb_gemm_int8_workspace_bytes(M, N, K, aligned);
     if (need > 0 && (!workspace_dev || (uintptr_t)workspace_dev % 16)) return workspace_bytes < need ? BB_ENOMEM : BB_EINVAL;
     if (workspace_bytes < need) return BB_ENOMEM;
-    GemmInt8Args a{A_dev, W_dev, a_scale_dev, w_scale_dev, bias_dev, C_dev, lda, ldw, ldc, M, N, K, c_type};
+    GemmInt8Args a{A_dev, W_dev, a_scale_dev, w_scale_dev, bias_dev, C_dev, lda, ldw, ldc, M, N, K, c_type, nullptr};
     if (K < 16 || (!aligned && !copies(M, K, aligned))) {
         const int tiles_n = (N + 63) / 64;
         gemm_int8_any_kernel<<<(unsigned)((size_t)tiles_n * ((M + 63) / 64)), 256, 0, s>>>(a, tiles_n);
@@ -460,13 +489,6 @@ extern "C" int bb_gemm_int8(const int8_t* A_dev, long lda, const float* a_scale_
         a.A = copy(A_dev, lda, M); a.lda = per_row * 16L;
         a.W = copy(W_dev, ldw, N); a.ldw = per_row * 16L;
     }
-    switch (p.body) {
-        case 0: launch_tiled<8, 8, 2, 2, 1>(a, p.split, workspace_dev, s); break;
-        case 1: launch_tiled<8, 6, 2, 2, 1>(a, p.split, workspace_dev, s); break;
-        case 2: launch_tiled<4, 4, 2, 2, 2>(a, p.split, workspace_dev, s); break;
-        case 3: launch_tiled<4, 2, 2, 3, 2>(a, p.split, workspace_dev, s); break;
-        case 4: launch_tiled<2, 2, 2, 4, 2>(a, p.split, workspace_dev, s); break;
-        default: launch_tiled<1, 1, 2, 4, 3>(a, p.split, workspace_dev, s); break;
-    }
+    launch_plan(a, p, workspace_dev, s);
     return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
 }

@@ -18,6 +18,7 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 #define QOP_ROWS 0
 #define QOP_NORM 1
 #define QOP_SWIGLU 2
+#define QOP_PANEL 3             // rows of a packed activation panel of two bf16 terms (what attention leaves for the output projection)
 
 struct QuantArgs {
     const void *x, *x2, *gain;      // NORM: x2 = residual (or null); SWIGLU: x = gate, x2 = up
@@ -26,6 +27,8 @@ struct QuantArgs {
     long ldx, ldx2, ldh, ldq;
     long rows; int cols;
     double eps;
+    const int* live;                // rows that count, on the device (null: all)
+    int mt_total;                   // PANEL
 };
 
 struct bf16_t { uint16_t v; };
@@ -72,6 +75,10 @@ static __device__ __forceinline__ float silu(float x) {
 
 // What a row's values are, at column c, in 64 bits, from memory (h once it is written).
 template <int OP, class T> static __device__ __forceinline__ double exact_value(const QuantArgs& a, long row, int c) {
+    if constexpr (OP == QOP_PANEL) {
+        auto term = [&](int t) { return (double)widen(((const T*)((const u32x4*)a.x + packA_u4((int)row, c >> 3, a.mt_total, t)))[c & 7]); };
+        return term(0) + term(1);
+    }
     const double x = widen((OP == QOP_NORM && a.x2 ? (const T*)a.h + row * a.ldh : (const T*)a.x + row * a.ldx)[c]);
     if constexpr (OP == QOP_NORM) return x * (double)widen(((const T*)a.gain)[c]);
     if constexpr (OP == QOP_SWIGLU) return x / (1.0 + exp(-x)) * (double)widen(((const T*)a.x2 + row * a.ldx2)[c]);
@@ -88,7 +95,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
     constexpr float V_ERR = OP == QOP_SWIGLU ? 0x1p-20f : 0x1p-24f, NEAR = 0.5f - 127.0f * (V_ERR + 0x1p-22f);
     const int t = threadIdx.x % THREADS;
     const long row = (long)blockIdx.x * ROWS + threadIdx.x / THREADS;
-    if (ROWS > 1 && row >= a.rows) return;                  // (whole waves; no barrier follows where rows share a workgroup)
+    if ((ROWS > 1 && row >= a.rows) || (a.live && row >= *a.live)) return;          // (whole waves; no barrier follows where rows share a workgroup)
     const T* x = (const T*)a.x + row * a.ldx;
     const T* x2 = a.x2 ? (const T*)a.x2 + row * a.ldx2 : nullptr;
     const T* gain = (const T*)a.gain;
@@ -102,6 +109,11 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
     Eight<T> kx[KEEP], ky[OP == QOP_ROWS ? 1 : KEEP], kr[OP == QOP_NORM ? KEEP : 1];
     auto fetch = [&](int i, int g, bool again) {            // (nothing that would make a load wait for the one before it)
         const int c = g * 8;
+        if constexpr (OP == QOP_PANEL) {
+            kx[i].load((const T*)((const u32x4*)a.x + packA_u4((int)row, g, a.mt_total, 0)));
+            ky[i].load((const T*)((const u32x4*)a.x + packA_u4((int)row, g, a.mt_total, 1)));
+            return;
+        }
         kx[i].load((OP == QOP_NORM && again && x2 ? h : x) + c);
         if constexpr (OP == QOP_SWIGLU) ky[i].load(x2 + c);
         if constexpr (OP == QOP_NORM) {
@@ -117,6 +129,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
             if constexpr (TOP_IN_DOUBLE) top2 = fmax(top2, fabs((double)f * (double)w));
         }
         if constexpr (OP == QOP_SWIGLU) y = silu(f) * w;
+        if constexpr (OP == QOP_PANEL) y = f + w;           // (exact: 16 bits and the sign)
         top_bits = max(top_bits, __float_as_uint(y) & 0x7FFFFFFFu);
         return y;
     };
@@ -309,6 +322,25 @@ static bool refuse_out(const void* q, long ldq, const void* scale, long rows, in
 }
 static bool refuse_rows(const void* p, int type, long rows, long ld) {
     return !p || (uintptr_t)p % (type == BB_F32 ? 4 : 2) || (rows > 1 && ld < 0);
+}
+
+// The layers of a forward: fp32 rows, of which *live count.
+void launch_rmsnorm_quantize(const float* x, float* residual, const float* gain, float eps, int8_t* q, long ldq, float* scale, long rows, int cols,
+                             const int* live, hipStream_t s) {
+    QuantArgs a{};
+    a.x = x; a.ldx = cols; a.x2 = residual; a.ldx2 = cols; a.h = residual; a.ldh = cols; a.gain = gain; a.eps = eps;
+    a.q = q; a.ldq = ldq; a.scale = scale; a.rows = rows; a.cols = cols; a.live = live;
+    launch_quantize<QOP_NORM, float>(a, s);
+}
+void launch_swiglu_quantize(const float* gate, const float* up, long ld, int8_t* q, long ldq, float* scale, long rows, int cols, const int* live, hipStream_t s) {
+    QuantArgs a{};
+    a.x = gate; a.ldx = ld; a.x2 = up; a.ldx2 = ld; a.q = q; a.ldq = ldq; a.scale = scale; a.rows = rows; a.cols = cols; a.live = live;
+    launch_quantize<QOP_SWIGLU, float>(a, s);
+}
+void launch_panel_quantize(const u32x4* Apk, int mt_total, int8_t* q, long ldq, float* scale, long rows, int cols, const int* live, hipStream_t s) {
+    QuantArgs a{};
+    a.x = Apk; a.mt_total = mt_total; a.q = q; a.ldq = ldq; a.scale = scale; a.rows = rows; a.cols = cols; a.live = live;
+    launch_quantize<QOP_PANEL, bf16_t>(a, s);
 }
 
 extern "C" int bb_quantize_rows(const void* x_dev, long ldx, int8_t* q_dev, long ldq, float* scale_dev, long rows, int cols, int type, void* hip_stream) {
