@@ -157,15 +157,23 @@ def gemm_plan(M, N, K, wide=True, fusable=False):
 
 
 # ---- 8-bit integer operators --------------------------------------------------------------------
-# (what these calls do on the host counts where a kernel takes a few microseconds: no objects made, checks in one place each)
-_TYPES = None           # torch dtype -> BB_F32, BB_BF16, BB_F16
+# (what these calls do on the host counts where a kernel takes a few microseconds: no objects made, nothing looked up twice)
+_TYPES = {}             # torch dtype -> BB_F32, BB_BF16, BB_F16
+_torch = _here = _raw_stream = _I8 = _F32 = None
+
+
+def _ready():
+    """What the calls below use of torch (imported with the first of them)."""
+    global _torch, _here, _raw_stream, _I8, _F32
+    import torch
+    load_library()
+    _TYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    _I8, _F32, _here = torch.int8, torch.float32, torch.cuda.current_device
+    _raw_stream = torch._C._cuda_getCurrentRawStream        # (torch.cuda.current_stream without its 2 us)
+    _torch = torch
 
 
 def _type(dtype, what):
-    global _TYPES
-    if _TYPES is None:
-        import torch
-        _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
     t = _TYPES.get(dtype)
     if t is None:
         raise BBError(f"{what}: expected float32, bfloat16 or float16, got {dtype}")
@@ -188,69 +196,57 @@ def _vec(t, what, dtype, n, device):
     return t.data_ptr()
 
 
-def _elsewhere(device, stream):
-    """None if a call on this device and stream can go ahead as things are, else the context it has to run in (in which what
-    it allocates belongs to that stream)."""
-    import torch
+def _elsewhere(device, stream, call):
+    """A call on another stream than the current one, or another device: what it allocates then belongs to that stream."""
     if device.type != "cuda":
         raise BBError(f"tensors must be on the GPU, got {device} (there is no CPU fallback)")
-    if stream is not None:
-        if stream.device != device:
-            raise BBError(f"the stream is of {stream.device}, the tensors are on {device}")
-        return torch.cuda.stream(stream)
-    return None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    if stream is not None and stream.device != device:
+        raise BBError(f"the stream is of {stream.device}, the tensors are on {device}")
+    with _torch.cuda.device(device) if stream is None else _torch.cuda.stream(stream):
+        return call()
 
 
-def _raw_stream(device):
-    import torch
-    return torch._C._cuda_getCurrentRawStream(device.index)     # (torch.cuda.current_stream without its 2 us)
-
-
-def _quantized(x, out, scale):
+def _quantized(shape, dev, out, scale):
     """Outputs of the three quantisers, made where not given: (q, its row distance, scale, address of scale)."""
-    import torch
-    dev = x.device
-    if x.dim() != 2:
-        raise BBError(f"expected a matrix, got {tuple(x.shape)}")
-    rows, cols = x.shape
+    if len(shape) != 2:
+        raise BBError(f"expected a matrix, got {tuple(shape)}")
+    rows, cols = shape
     if out is None:         # (rows at multiples of 16 bytes, as the product reads them fastest)
-        out = torch.empty(rows, (cols + 15) // 16 * 16, dtype=torch.int8, device=dev)[:, :cols]
+        out = _torch.empty(rows, (cols + 15) // 16 * 16, dtype=_I8, device=dev)[:, :cols]
     if scale is None:
-        scale = torch.empty(rows, dtype=torch.float32, device=dev)
-    return out, _ld(out, "out", torch.int8, x.shape, dev), scale, _vec(scale, "scale", torch.float32, rows, dev)
+        scale = _torch.empty(rows, dtype=_F32, device=dev)
+    return out, _ld(out, "out", _I8, shape, dev), scale, _vec(scale, "scale", _F32, rows, dev)
 
 
 def _done(rc, what):
-    if rc != 0:
-        raise BBError(f"{what}: {_ERR.get(rc, rc)}")
+    raise BBError(f"{what}: {_ERR.get(rc, rc)}")
 
 
 def quantize_rows(x, out=None, scale=None, stream=None):
     """bb_quantize_rows on torch CUDA tensors: x [rows][cols] fp32, bf16 or fp16 -> (q int8 [rows][cols], scale fp32
     [rows]) with q * scale standing for x.  q and scale are written in place where given.  The call is enqueued on
     `stream` (default: the current stream of x's device), on which what it makes is allocated too."""
-    dev = x.device
-    ctx = _elsewhere(dev, stream)
-    if ctx is not None:
-        with ctx:
-            return quantize_rows(x, out, scale)
-    out, ldq, scale, ps = _quantized(x, out, scale)
-    rows, cols = x.shape
-    _done(load_library().bb_quantize_rows(x.data_ptr(), _ld(x, "x", x.dtype, x.shape, dev), out.data_ptr(), ldq, ps, rows, cols, _type(x.dtype, "x"),
-                                          _raw_stream(dev)), "bb_quantize_rows")
+    if _torch is None:
+        _ready()
+    dev, dtype, shape = x.device, x.dtype, x.shape
+    if stream is not None or dev.index is None or dev.index != _here():
+        return _elsewhere(dev, stream, lambda: quantize_rows(x, out, scale))
+    out, ldq, scale, ps = _quantized(shape, dev, out, scale)
+    rc = _LIB.bb_quantize_rows(x.data_ptr(), _ld(x, "x", dtype, shape, dev), out.data_ptr(), ldq, ps, shape[0], shape[1], _type(dtype, "x"), _raw_stream(dev.index))
+    if rc:
+        _done(rc, "bb_quantize_rows")
     return out, scale
 
 
 def rmsnorm_quantize(x, gain, eps, residual=None, residual_out=None, out=None, scale=None, stream=None):
     """bb_rmsnorm_quantize: h = x + residual -> residual_out (default: residual itself, in place), then RMSNorm(h) * gain
     with int8 rows; returns (q, scale).  Without a residual h = x.  gain has x's type.  Stream as in quantize_rows."""
-    dev = x.device
-    ctx = _elsewhere(dev, stream)
-    if ctx is not None:
-        with ctx:
-            return rmsnorm_quantize(x, gain, eps, residual, residual_out, out, scale)
-    out, ldq, scale, ps = _quantized(x, out, scale)
-    dtype, shape = x.dtype, x.shape
+    if _torch is None:
+        _ready()
+    dev, dtype, shape = x.device, x.dtype, x.shape
+    if stream is not None or dev.index is None or dev.index != _here():
+        return _elsewhere(dev, stream, lambda: rmsnorm_quantize(x, gain, eps, residual, residual_out, out, scale))
+    out, ldq, scale, ps = _quantized(shape, dev, out, scale)
     rows, cols = shape
     res = h = None
     ldr = ldh = 0
@@ -261,24 +257,26 @@ def rmsnorm_quantize(x, gain, eps, residual=None, residual_out=None, out=None, s
         res, h = residual.data_ptr(), residual_out.data_ptr()
     elif residual_out is not None:
         raise BBError("residual_out without a residual")
-    _done(load_library().bb_rmsnorm_quantize(x.data_ptr(), _ld(x, "x", dtype, shape, dev), res, ldr, h, ldh, _vec(gain, "gain", dtype, cols, dev), eps,
-                                             out.data_ptr(), ldq, ps, rows, cols, _type(dtype, "x"), _raw_stream(dev)), "bb_rmsnorm_quantize")
+    rc = _LIB.bb_rmsnorm_quantize(x.data_ptr(), _ld(x, "x", dtype, shape, dev), res, ldr, h, ldh, _vec(gain, "gain", dtype, cols, dev), eps,
+                                  out.data_ptr(), ldq, ps, rows, cols, _type(dtype, "x"), _raw_stream(dev.index))
+    if rc:
+        _done(rc, "bb_rmsnorm_quantize")
     return out, scale
 
 
 def swiglu_quantize(gate, up, out=None, scale=None, stream=None):
     """bb_swiglu_quantize: SiLU(gate) * up with int8 rows; returns (q, scale).  gate and up may be the two halves of one
     tensor's columns.  Stream as in quantize_rows."""
-    dev = gate.device
-    ctx = _elsewhere(dev, stream)
-    if ctx is not None:
-        with ctx:
-            return swiglu_quantize(gate, up, out, scale)
-    out, ldq, scale, ps = _quantized(gate, out, scale)
-    dtype, shape = gate.dtype, gate.shape
-    rows, cols = shape
-    _done(load_library().bb_swiglu_quantize(gate.data_ptr(), _ld(gate, "gate", dtype, shape, dev), up.data_ptr(), _ld(up, "up", dtype, shape, dev),
-                                            out.data_ptr(), ldq, ps, rows, cols, _type(dtype, "gate"), _raw_stream(dev)), "bb_swiglu_quantize")
+    if _torch is None:
+        _ready()
+    dev, dtype, shape = gate.device, gate.dtype, gate.shape
+    if stream is not None or dev.index is None or dev.index != _here():
+        return _elsewhere(dev, stream, lambda: swiglu_quantize(gate, up, out, scale))
+    out, ldq, scale, ps = _quantized(shape, dev, out, scale)
+    rc = _LIB.bb_swiglu_quantize(gate.data_ptr(), _ld(gate, "gate", dtype, shape, dev), up.data_ptr(), _ld(up, "up", dtype, shape, dev), out.data_ptr(), ldq, ps,
+                                 shape[0], shape[1], _type(dtype, "gate"), _raw_stream(dev.index))
+    if rc:
+        _done(rc, "bb_swiglu_quantize")
     return out, scale
 
 
@@ -286,32 +284,33 @@ def gemm_int8(a, a_scale, w, w_scale, bias=None, out=None, dtype=None, stream=No
     """bb_gemm_int8: out[m][n] = (sum_k a[m][k] w[n][k]) * a_scale[m] * w_scale[n] + bias[n]; a [M][K], w [N][K] int8,
     scales and bias fp32.  out: fp32, bf16 or fp16 [M][N], made here (of `dtype`, default bf16) where not given.  Stream as in
     quantize_rows; a workspace, where the product needs one, is allocated on it for this call alone."""
-    import torch
+    if _torch is None:
+        _ready()
     dev = a.device
-    ctx = _elsewhere(dev, stream)
-    if ctx is not None:
-        with ctx:
-            return gemm_int8(a, a_scale, w, w_scale, bias, out, dtype)
+    if stream is not None or dev.index is None or dev.index != _here():
+        return _elsewhere(dev, stream, lambda: gemm_int8(a, a_scale, w, w_scale, bias, out, dtype))
     if a.dim() != 2 or w.dim() != 2:
         raise BBError(f"expected matrices, got {tuple(a.shape)} and {tuple(w.shape)}")
-    (M, K), N, i8, f32 = a.shape, w.shape[0], torch.int8, torch.float32
-    lda, ldw = _ld(a, "a", i8, (M, K), dev), _ld(w, "w", i8, (N, K), dev)
-    sa, sw = _vec(a_scale, "a_scale", f32, M, dev), _vec(w_scale, "w_scale", f32, N, dev)
-    b = None if bias is None else _vec(bias, "bias", f32, N, dev)
+    (M, K), N = a.shape, w.shape[0]
+    lda, ldw = _ld(a, "a", _I8, (M, K), dev), _ld(w, "w", _I8, (N, K), dev)
+    sa, sw = _vec(a_scale, "a_scale", _F32, M, dev), _vec(w_scale, "w_scale", _F32, N, dev)
+    b = None if bias is None else _vec(bias, "bias", _F32, N, dev)
     if out is None:
-        out = torch.empty(M, N, dtype=dtype or torch.bfloat16, device=dev)
+        out = _torch.empty(M, N, dtype=dtype or _torch.bfloat16, device=dev)
     elif dtype is not None and out.dtype is not dtype:
         raise BBError(f"out has {out.dtype}, dtype says {dtype}")
     ct = _type(out.dtype, "out")
     ldc = _ld(out, "out", out.dtype, (M, N), dev)
-    pa, pw, lib = a.data_ptr(), w.data_ptr(), load_library()
+    pa, pw = a.data_ptr(), w.data_ptr()
     if M == 1:
         lda = 0
     if N == 1:
         ldw = 0
-    nbytes = lib.bb_gemm_int8_workspace_bytes(M, N, K, (pa | pw | lda | ldw) % 16 == 0 and lda <= 1 << 23 and ldw <= 1 << 23)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-    _done(lib.bb_gemm_int8(pa, lda, sa, pw, ldw, sw, b, out.data_ptr(), ldc, ct, M, N, K, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(dev)), "bb_gemm_int8")
+    nbytes = _LIB.bb_gemm_int8_workspace_bytes(M, N, K, (pa | pw | lda | ldw) % 16 == 0 and lda <= 1 << 23 and ldw <= 1 << 23)
+    ws = _torch.empty(nbytes, dtype=_torch.uint8, device=dev) if nbytes else None
+    rc = _LIB.bb_gemm_int8(pa, lda, sa, pw, ldw, sw, b, out.data_ptr(), ldc, ct, M, N, K, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(dev.index))
+    if rc:
+        _done(rc, "bb_gemm_int8")
     return out
 
 

@@ -5,8 +5,8 @@
 // The codes are those of the formula in 64 bits whatever the launch.  The norm's 1 / rms is a positive factor of the whole row and falls out
 // of y / max |y|, so they depend on p = h * gain alone, which a double holds exactly.  Values are kept in fp32 (v), which for 16-bit types is p
 // itself, else off by V_ERR at most; t = v * (127 / max) is off by 127 (V_ERR + 2^-23).  Only where t is that near to a border between two
-// codes (a few elements in 10^5) is the value taken again, in double, and the quotient correctly rounded, so that a border that is met
-// exactly (half the maximum is 63.5) is seen as one.  So is the maximum itself where fp32 does not hold it.  Sums of squares are in double.
+// codes is it taken again, in double (from memory where v does not hold it, a few elements in 10^5), so that a border that is met exactly (half the
+// maximum is 63.5) is seen as one.  So is the maximum itself where fp32 does not hold it.  Sums of squares are in double.
 //
 // What bounds it: memory.  A row is read once and its values stay in registers between the maximum and the codes.
 #include "bb_internal.h"
@@ -90,6 +90,7 @@ template <int OP, class T> static __device__ __forceinline__ double exact_value(
 template <int OP, class T, int THREADS, int G>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel(QuantArgs a) {
     constexpr int ROWS = THREADS < 256 ? 256 / THREADS : 1, KEEP = G ? G : 1;
+    constexpr bool V_EXACT = OP == QOP_ROWS || OP == QOP_PANEL || (OP == QOP_NORM && sizeof(T) == 2);
     constexpr bool TOP_IN_DOUBLE = OP == QOP_NORM && std::is_same_v<T, float>;      // v does not hold the maximum, but its factors are at hand
     // 2^-24: one rounding; SiLU * up: 9 of them, allowed 16
     constexpr float V_ERR = OP == QOP_SWIGLU ? 0x1p-20f : 0x1p-24f, NEAR = 0.5f - 127.0f * (V_ERR + 0x1p-22f);
@@ -220,12 +221,11 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
         double d = 0.0;
         const float least = (float)top * (1.0f - 4.0f * V_ERR);
         auto look = [&](int i, int g) {
-            float m = 0.f;
+            unsigned near = 0u;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(v[i][j]));
-            if (m >= least)
+            for (int j = 0; j < 8; ++j) near |= fabsf(v[i][j]) >= least ? 1u << j : 0u;
 #pragma unroll 1
-                for (int j = 0; j < 8; ++j) d = fmax(d, fabs(exact_value<OP, T>(a, row, g * 8 + j)));
+            for (; near; near &= near - 1u) d = fmax(d, fabs(exact_value<OP, T>(a, row, g * 8 + __ffs((int)near) - 1)));
         };
         if constexpr (G > 0) {
 #pragma unroll
@@ -246,27 +246,45 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
     const bool none = bad || top == 0.0;
     const float per = none || hard ? 0.0f : 127.0f / (float)top;     // (the rounding of top, the quotient and the product: under 2^-22)
     int8_t* q = a.q + row * a.ldq;
-    // adding 1.5 * 2^23 rounds to a whole number, whose low byte is the code; far: how near to a border, half at most
+    // adding 1.5 * 2^23 rounds to a whole number, whose low byte is the code; far: how far from it, half at a border
     auto code_bits = [&](float y, float& far) {
         const float u = y * per, r = u + 12582912.0f;
-        far = fmaxf(far, fabsf(u - (r - 12582912.0f)));
+        far = fabsf(u - (r - 12582912.0f));
         return __float_as_uint(r);
     };
-    auto exact_code = [&](int c) { return (int)rint(127.0 * exact_value<OP, T>(a, row, c) / top); };
+    auto exact_code = [&](double y) { return (unsigned)(int)rint(127.0 * y / top) & 0xFFu; };
+    // For a y that v holds: which side of the border next to u it is on.  Both products are exact.  (16-bit types meet borders often: of
+    // normal bf16 values one in 600 is half the row's maximum.)
+    auto side_of_border = [&](float y) {
+        const float u = y * per, r = rintf(u), border = r + (u > r ? 0.5f : -0.5f);
+        const double l = 127.0 * (double)y, b = (double)border * top;
+        const float below = border - 0.5f, above = border + 0.5f;
+        const float code = l > b ? above : l < b ? below : rintf(border);
+        return (unsigned)(int)code & 0xFFu;
+    };
     auto codes = [&](int i, int g) {
         unsigned bits[8], out[2];
-        float far = 0.f;
+        float far[8], most = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) bits[j] = code_bits(v[i][j], far);
+        for (int j = 0; j < 8; ++j) { bits[j] = code_bits(v[i][j], far[j]); most = fmaxf(most, far[j]); }
+        unsigned again = 0u;            // the codes to take from the values in memory
+        if (hard && !none) again = 0xFFu;
+        else if (most > NEAR && !none) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (V_EXACT) { if (far[j] > NEAR) bits[j] = side_of_border(v[i][j]); }
+                else again |= far[j] > NEAR ? 1u << j : 0u;
+            }
+        }
 #pragma unroll
         for (int k = 0; k < 2; ++k)
             out[k] = __builtin_amdgcn_perm(bits[4 * k + 1], bits[4 * k], 0x0C0C0400u) | __builtin_amdgcn_perm(bits[4 * k + 3], bits[4 * k + 2], 0x04000C0Cu);
         if (none) out[0] = out[1] = 0u;
-        else if (hard || far > NEAR) {
-            unsigned long long o = 0;
 #pragma unroll 1
-            for (int j = 7; j >= 0; --j) o = o << 8 | (unsigned)(exact_code(g * 8 + j) & 0xFF);
-            out[0] = (unsigned)o; out[1] = (unsigned)(o >> 32);
+        for (; again; again &= again - 1u) {
+            const int j = __ffs((int)again) - 1, at = 8 * (j & 3);
+            const unsigned code = exact_code(exact_value<OP, T>(a, row, g * 8 + j)) << at, mask = ~(0xFFu << at);
+            if (j < 4) out[0] = (out[0] & mask) | code; else out[1] = (out[1] & mask) | code;
         }
         __builtin_memcpy(q + g * 8, out, 8);
     };
@@ -276,9 +294,9 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
     } else
         for (int g = t; g < groups; g += THREADS) { fetch(0, g, true); values(0, g, true); codes(0, g); }
     if (tail) {
-        float far = 0.f;
+        float far;
         const unsigned b = code_bits(v_tail, far);
-        q[c_tail] = (int8_t)(none ? 0 : hard || far > NEAR ? exact_code(c_tail) : (int)(b & 0xFFu));
+        q[c_tail] = (int8_t)(none ? 0u : hard || far > NEAR ? exact_code(exact_value<OP, T>(a, row, c_tail)) : b & 0xFFu);
     }
 }
 
@@ -287,8 +305,8 @@ template <int OP, class T, int THREADS, int G> static void launch_body(const Qua
     quantize_kernel<OP, T, THREADS, G><<<dim3((unsigned)((a.rows + ROWS - 1) / ROWS)), THREADS < 256 ? 256 : THREADS, 0, s>>>(a);
 }
 // Lanes per row: with many rows as few as keep a row in registers without costing occupancy (fewer partial sums to put together), with few
-// rows as many as shorten one row's time.  us, bf16, rows 20480 x 4096: 256 lanes 71, 512 88; 6143 x 12288: 256 lanes 68, 512 62, 1024 77,
-// (SwiGLU 133, 150, 205); 120 x 12288: 1024 lanes 6.5, 512 7.4, 256 9.8; 20480 x 512: 64 lanes 14, 256 22.
+// rows as many as shorten one row's time.  us, bf16 rows: 20480 x 4096 256 lanes 47, 512 54, 64 53; 6143 x 12288 256 lanes 45, 512 43, 1024 47
+// (SwiGLU 83, 95, 129); 120 x 12288 1024 lanes 5.1, 512 6.0, 256 8.3; 20480 x 512 64 lanes 9.6, 256 17.
 template <int OP, class T> static void launch_quantize(const QuantArgs& a, hipStream_t s) {
     const int groups = a.cols / 8;
     const bool many = a.rows >= 1024;
