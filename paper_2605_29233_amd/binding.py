@@ -211,8 +211,9 @@ def _quantized(shape, dev, out, scale):
     if len(shape) != 2:
         raise BBError(f"expected a matrix, got {tuple(shape)}")
     rows, cols = shape
-    if out is None:         # (rows at multiples of 16 bytes, as the product reads them fastest)
-        out = _torch.empty(rows, (cols + 15) // 16 * 16, dtype=_I8, device=dev)[:, :cols]
+    if out is None:         # (rows at multiples of a cache line, as the product reads them fastest; short ones of 16 bytes, which it wants at least)
+        unit = 128 if cols > 512 else 16
+        out = _torch.empty(rows, (cols + unit - 1) // unit * unit, dtype=_I8, device=dev)[:, :cols]
     if scale is None:
         scale = _torch.empty(rows, dtype=_F32, device=dev)
     return out, _ld(out, "out", _I8, shape, dev), scale, _vec(scale, "scale", _F32, rows, dev)

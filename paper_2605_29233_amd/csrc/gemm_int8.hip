@@ -3,7 +3,7 @@
 // The sum is exact (int32; K <= 131071 keeps it below 2^31 even for codes of -128), so results do not depend on the tile, the split
 // of k or the order; it is rounded to fp32 once, scaled in fp32 and rounded to C's type.
 //
-// MFMA operands: the matrix cores take 16 rows x 64 k, lane l holding the 16 bytes k = 16 (l / 16) .. + 15 of row l % 16, so row-major
+// The operands: the matrix cores take 16 rows x 64 k, lane l holding the 16 bytes k = 16 (l / 16) .. + 15 of row l % 16, so row-major
 // operands need no re-tiling: 16-byte pieces of their rows are what a lane wants.  W is the first operand: a lane then holds four
 // consecutive columns of one row of C.
 #include "bb_internal.h"
@@ -22,23 +22,6 @@ struct GemmInt8Args {
     int M, N, K, type;
     const int* live;                // rows of A that count, on the device (null: all M; only the tiled kernel is asked for fewer)
 };
-
-// Four consecutive columns of a row of C, as far as they exist.
-static __device__ __forceinline__ void store_c4(const GemmInt8Args& a, int m, int n, const i32x4& acc) {
-    if (m >= a.M || n >= a.N) return;
-    const float sa = a.sa[m];
-    const int cnt = min(4, a.N - n);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        if (r >= cnt) break;
-        float v = (float)acc[r] * sa * a.sw[n + r];
-        if (a.bias) v += a.bias[n + r];
-        const size_t at = (size_t)m * a.ldc + n + r;
-        if (a.type == BB_F32) ((float*)a.C)[at] = v;
-        else if (a.type == BB_F16) ((half_t*)a.C)[at] = (half_t)v;
-        else ((__bf16*)a.C)[at] = (__bf16)v;
-    }
-}
 
 // Which column of a wave's 16 T row i of MFMA tile t is: of a pair of tiles a lane, which holds rows 4 (lane / 16) .. + 3 of each, gets eight columns
 // in a row, which it stores whole.  (The last of an odd number of tiles: as they come.)
@@ -93,52 +76,37 @@ template <int T, int R> static __device__ __forceinline__ void store_tile(const 
     if (a.type == BB_F32) as(0.f); else if (a.type == BB_F16) as((half_t)0); else as((__bf16)0.f);
 }
 
-// 16 bytes of a row from k on; zeros past its end.  Any alignment.
+// 16 bytes of a row from k on; zeros past its end.  Any alignment.  A piece that the end cuts is shifted down out of the row's last 16 bytes, so
+// that every lane makes one load and none waits for another's (K >= 16).
 static __device__ __forceinline__ u32x4 load16(const int8_t* row, int k, int K) {
-    u32x4 v = {0u, 0u, 0u, 0u};
-    if (k + 16 <= K) __builtin_memcpy(&v, row + k, 16);
-    else
-#pragma unroll 1
-        for (int j = 0; j < 16; ++j)
-            if (k + j < K) v[j >> 2] |= (unsigned)(uint8_t)row[k + j] << (8 * (j & 3));
-    return v;
+    typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
+    const int from = min(k, K - 16);
+    u64x2 w;
+    __builtin_memcpy(&w, row + from, 16);
+    int sh = 8 * min(k - from, 16);                         // 0: whole; 128: nothing left
+    const bool upper = sh >= 64;
+    unsigned long long lo = upper ? w[1] : w[0], hi = upper ? 0 : w[1];
+    sh -= upper ? 64 : 0;
+    const bool none = sh >= 64;
+    sh = none ? 0 : sh;
+    lo = lo >> sh | hi << 1 << (63 - sh);
+    hi >>= sh;
+    return __builtin_bit_cast(u32x4, u64x2{none ? 0 : lo, none ? 0 : hi});
 }
-
-// Any alignment, any K: 64 x 64 of C per workgroup, 64 k at a time through registers and LDS (rows 80 bytes apart: 16 lanes' pieces fall
-// into different banks); four waves of 32 x 32.
-__global__ __launch_bounds__(256) void gemm_int8_any_kernel(GemmInt8Args a, int tiles_n) {
-    __shared__ __attribute__((aligned(16))) char lds[2][64 * 80];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, c16 = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x % tiles_n * 64, m0 = blockIdx.x / tiles_n * 64;
-    const int wn = (wave & 1) * 32, wm = (wave >> 1) * 32;
-    const int8_t* wrow = a.W + min(n0 + (t >> 2), a.N - 1) * a.ldw;
-    const int8_t* arow = a.A + min(m0 + (t >> 2), a.M - 1) * a.lda;
-    i32x4 acc[2][2] = {};
-    u32x4 w = load16(wrow, (t & 3) * 16, a.K), b = load16(arow, (t & 3) * 16, a.K);
-    for (int k = 0; k < a.K; k += 64) {
-        __syncthreads();
-        *reinterpret_cast<u32x4*>(&lds[0][(t >> 2) * 80 + (t & 3) * 16]) = w;
-        *reinterpret_cast<u32x4*>(&lds[1][(t >> 2) * 80 + (t & 3) * 16]) = b;
-        __syncthreads();
-        if (k + 64 < a.K) {
-            w = load16(wrow, k + 64 + (t & 3) * 16, a.K);
-            b = load16(arow, k + 64 + (t & 3) * 16, a.K);
-        }
-        i32x4 fw[2], fa[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            fw[i] = *reinterpret_cast<const i32x4*>(&lds[0][(wn + i * 16 + c16) * 80 + g * 16]);
-            fa[i] = *reinterpret_cast<const i32x4*>(&lds[1][(wm + i * 16 + c16) * 80 + g * 16]);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[i], fa[j], acc[i][j], 0, 0, 0);
+// Rows of fewer than 16 bytes: a thread per value of C.
+__global__ __launch_bounds__(256) void gemm_int8_short_kernel(GemmInt8Args a) {
+    const size_t values = (size_t)a.M * a.N;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < values; i += (size_t)gridDim.x * 256) {
+        const int m = (int)(i / a.N), n = (int)(i % a.N);
+        int acc = 0;
+        for (int k = 0; k < a.K; ++k) acc += (int)a.A[m * a.lda + k] * (int)a.W[n * a.ldw + k];
+        float v = (float)acc * a.sa[m] * a.sw[n];
+        if (a.bias) v += a.bias[n];
+        const size_t at = (size_t)m * a.ldc + n;
+        if (a.type == BB_F32) ((float*)a.C)[at] = v;
+        else if (a.type == BB_F16) ((half_t*)a.C)[at] = (half_t)v;
+        else ((__bf16*)a.C)[at] = (__bf16)v;
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) store_c4(a, m0 + wm + j * 16 + c16, n0 + wn + i * 16 + 4 * g, acc[i][j]);
 }
 
 // Rows of any alignment -> rows of whole 16-byte pieces with zeros past K, for the tiled kernel.
@@ -249,9 +217,7 @@ __global__ __launch_bounds__(256, PER_CU) void gemm_int8_tiled_kernel(TiledArgs 
                 for (int j = 0; j < AT_ONCE; ++j) {
                     const int i = i0 + j, row = (wave + 4 * (i < LA ? i : i - LA)) * 8 + lr;
                     const int8_t* p = i < LA ? a.A + min(f_m0 + row, a.M - 1) * a.lda : a.W + min(f_n0 + row, a.N - 1) * a.ldw;
-                    v[j] = u32x4{0u, 0u, 0u, 0u};
-                    if (k + 16 <= a.K) v[j] = *reinterpret_cast<const u32x4*>(p + k);
-                    else if (k < a.K) v[j] = load16(p, k, a.K);
+                    v[j] = load16(p, k, a.K);
                 }
 #pragma unroll
                 for (int j = 0; j < AT_ONCE; ++j) *reinterpret_cast<u32x4*>(lds + wr + (wave + 4 * (i0 + j)) * 1024 + lane * 16) = v[j];
@@ -440,16 +406,13 @@ void launch_gemm_int8(const int8_t* A, long lda, const float* sa, const int8_t* 
 }
 size_t gemm_int8_partial_bytes(int M, int N, int K) { return int8_plan(M, N, K).partial_bytes; }
 
-// Rows that are not 16-byte aligned: up to I8_ANY_ROWS rows of A the kernel for any alignment (M = 64, 24576 x 4096 matrix: X us against
-// Y with aligned copies), above aligned copies of both operands in the workspace and the tiled kernel.
-#define I8_ANY_ROWS 64
-static bool copies(int M, int K, int aligned) { return !aligned && M > I8_ANY_ROWS && K >= 16; }
+// Rows that are not 16-byte aligned go through copies that are, in the workspace.  (A kernel that took any alignment through registers was slower
+// at every size: us, 64 x 24576 x 4097 79 against 65 with the copies, 64 x 4096 x 4097 64 against 26.)
 static size_t copy_bytes(int rows, int K) { return align_up((size_t)rows * align_up(K, 16), 256); }
 static bool sizes_ok(int M, int N, int K) { return M >= 0 && N >= 0 && M <= BB_GEMM_INT8_MAX_ROWS && N <= BB_GEMM_INT8_MAX_ROWS && K >= 1 && K <= BB_GEMM_INT8_MAX_K; }
 
 extern "C" size_t bb_gemm_int8_workspace_bytes(int M, int N, int K, int aligned) {
-    if (!sizes_ok(M, N, K) || M == 0 || N == 0 || (!aligned && !copies(M, K, aligned))) return 0;
-    if (aligned && K < 16) return 0;
+    if (!sizes_ok(M, N, K) || M == 0 || N == 0 || K < 16) return 0;
     return align_up(int8_plan(M, N, K).partial_bytes, 256) + (aligned ? 0 : copy_bytes(M, K) + copy_bytes(N, K));
 }
 
@@ -470,9 +433,8 @@ extern "C" int bb_gemm_int8(const int8_t* A_dev, long lda, const float* a_scale_
     if (need > 0 && (!workspace_dev || (uintptr_t)workspace_dev % 16)) return workspace_bytes < need ? BB_ENOMEM : BB_EINVAL;
     if (workspace_bytes < need) return BB_ENOMEM;
     GemmInt8Args a{A_dev, W_dev, a_scale_dev, w_scale_dev, bias_dev, C_dev, lda, ldw, ldc, M, N, K, c_type, nullptr};
-    if (K < 16 || (!aligned && !copies(M, K, aligned))) {
-        const int tiles_n = (N + 63) / 64;
-        gemm_int8_any_kernel<<<(unsigned)((size_t)tiles_n * ((M + 63) / 64)), 256, 0, s>>>(a, tiles_n);
+    if (K < 16) {
+        gemm_int8_short_kernel<<<(unsigned)std::min<size_t>(((size_t)M * N + 255) / 256, 8192), 256, 0, s>>>(a);
         return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
     }
     const Int8Plan p = int8_plan(M, N, K);
