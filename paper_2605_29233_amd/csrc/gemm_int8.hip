@@ -254,9 +254,11 @@ __global__ __launch_bounds__(256, PER_CU) void gemm_int8_tiled_kernel(TiledArgs 
         asm volatile("" ::: "memory");
     };
     landed(IC((NS - 1) * L));
-    // Half a chunk: R slots of T MFMAs; the next half's fragments are asked for in the first of them, in the second half also the
-    // chunk NS ahead, into the place of this one, whose last fragments all waves have by then.
-    constexpr int READ_SLOTS = R > 2 ? R - R / 4 : R, FETCH_SLOTS = R;
+    // Half a chunk: R slots of T MFMAs; the next half's fragments are asked for in the first of them.  Once all waves have those of a chunk's second half
+    // (a barrier half way through its first half) its place is free and the chunk NS ahead is asked for, spread over the slots that are left until the
+    // chunk's end: as soon and as evenly as can be, since what the L2s deliver sets the time (us, 128 x 128 and 256 x 192 tiles, 8192 x 4096 x 12288: 401 and
+    // 365 when it was asked for in the second half only, 361 and 337 so).
+    constexpr int READ_SLOTS = R > 2 ? R / 2 : R, FREE = R - READ_SLOTS, FETCH_SLOTS = FREE + R, EARLY = L * FREE / FETCH_SLOTS;
     auto half = [&](auto H, auto First) {
         constexpr int h = decltype(H)::value;
         unroll<R>([&](auto Rr) {
@@ -265,8 +267,15 @@ __global__ __launch_bounds__(256, PER_CU) void gemm_int8_tiled_kernel(TiledArgs 
             for (int t = 0; t < T; ++t) acc[r][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[h][t], b[h][r], decltype(First)::value ? i32x4{0, 0, 0, 0} : acc[r][t], 0, 0, 0);
             if constexpr (r < READ_SLOTS)
                 unroll<(R + T) * (r + 1) / READ_SLOTS - (R + T) * r / READ_SLOTS>([&](auto J) { read(IC(1 - h), (R + T) * r / READ_SLOTS + decltype(J)::value); });
-            if constexpr (h == 1 && r < FETCH_SLOTS)
-                unroll<L * (r + 1) / FETCH_SLOTS - L * r / FETCH_SLOTS>([&](auto I) { fetch(L * r / FETCH_SLOTS + decltype(I)::value); });
+            if constexpr (h == 0 && FREE > 0 && r == READ_SLOTS) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+            }
+            if constexpr (h == 1 || r >= READ_SLOTS) {
+                constexpr int f = h == 0 ? r - READ_SLOTS : FREE + r;
+                unroll<L * (f + 1) / FETCH_SLOTS - L * f / FETCH_SLOTS>([&](auto I) { fetch(L * f / FETCH_SLOTS + decltype(I)::value); });
+            }
             __builtin_amdgcn_sched_barrier(0);
         });
     };
@@ -281,7 +290,7 @@ __global__ __launch_bounds__(256, PER_CU) void gemm_int8_tiled_kernel(TiledArgs 
         auto chunk = [&](auto First) {
             half(IC(0), First);
             bump(rd);
-            landed(IC((NS - 2) * L));
+            landed(IC((NS - 2) * L + EARLY));
             half(IC(1), std::false_type{});
             next_chunk();
         };

@@ -207,14 +207,19 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
     // Rows so large or small that fp32 products would not do (and those that hold an infinity or a NaN): everything in double.
     const bool hard = !(top_bits > 0x0D800000u && top_bits < 0x71800000u);     // 2^-100, 2^100
     bool bad = false;
-    if (hard && top_bits != 0u) {
+    // (a row of zeros needs no second look: what v holds exactly, and SiLU * up below fp32's range counts as zero)
+    if (hard && (top_bits != 0u || (OP == QOP_NORM && ss > 0.0))) {
         double d = 0.0;
         int b = 0;
-        for (int c = t; c < cols; c += THREADS) {
+        auto look = [&](int c) {                            // (columns of this thread's own: h is as it wrote it)
             const double y = fabs(exact_value<OP, T>(a, row, c));
             b |= !(y < INFINITY);
             d = fmax(d, y);
-        }
+        };
+        for (int g = t; g < groups; g += THREADS)
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j) look(g * 8 + j);
+        if (tail) look(c_tail);
         top = reduce_top(b ? INFINITY : d);
         bad = !(top < INFINITY);
     } else if (OP == QOP_SWIGLU && top_bits != 0u) {        // the largest of those that may be the maximum
@@ -322,11 +327,20 @@ template <int OP, class T> static void launch_quantize(const QuantArgs& a, hipSt
     else launch_body<OP, T, 1024, 0>(a, s);
 }
 
-template <int OP> static int quantize(int type, const QuantArgs& a, hipStream_t s) {
-    switch (type) {
-        case BB_F32: launch_quantize<OP, float>(a, s); break;
-        case BB_BF16: launch_quantize<OP, bf16_t>(a, s); break;
-        default: launch_quantize<OP, half_t>(a, s); break;
+// (a launch holds under 2^32 threads: rows by parts)
+template <int OP> static int quantize(int type, QuantArgs a, hipStream_t s) {
+    const long rows = a.rows, most = 1L << 21, size = type == BB_F32 ? 4 : 2;
+    auto skip = [&](const void*& p, long ld) { if (p) p = (const char*)p + most * ld * size; };
+    for (long r = 0; r < rows; r += most) {
+        a.rows = std::min(most, rows - r);
+        switch (type) {
+            case BB_F32: launch_quantize<OP, float>(a, s); break;
+            case BB_BF16: launch_quantize<OP, bf16_t>(a, s); break;
+            default: launch_quantize<OP, half_t>(a, s); break;
+        }
+        skip(a.x, a.ldx); skip(a.x2, a.ldx2);
+        if (a.h) a.h = (char*)a.h + most * a.ldh * size;
+        a.q += most * a.ldq; a.scale += most;
     }
     return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
 }

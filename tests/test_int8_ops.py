@@ -177,6 +177,45 @@ def test_extreme_rows(cols):
         assert torch.isnan(s[5]) and (q[5] == 0).all()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("cols", [6, 40, 700, 4096, 40000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm_of_rows_whose_products_leave_fp32(cols, dtype):
+    """Gains by which h * gain overflows or underflows fp32 while the norm itself does not; with the sum over x or the residual, and rows
+    of zeros between them."""
+    t = TYPES[dtype]
+    x, r = rnd(60 + cols, 5, cols, dtype), rnd(61 + cols, 5, cols, dtype)
+    if dtype == "fp16":
+        gain, by = rnd(62, 1, cols, dtype)[0] * 2.0 ** -12, 2.0 ** -10
+    else:
+        gain, by = (rnd(62, 1, cols, dtype)[0].float() * 1e-25).to(t), 1e-25
+    x[1], r[1] = x[1] * by, r[1] * by
+    x[2], r[2] = 0, 0
+    for g, eps in ((gain, 0.0), (gain, 1e-5)) + (() if dtype == "fp16" else ((1 / gain.clamp(min=1e-27), 1e-5),)):
+        if dtype != "fp16":
+            x[3] = x[3] * 1e13 if g is not gain else x[3]
+        h = (x.float() + r.float()).to(t)
+        if eps == 0.0:
+            keep = [0, 1, 3, 4]                 # (0 / 0 of the row of zeros is NaN in the formula too)
+        else:
+            keep = [0, 1, 2, 3, 4]
+        over, into = x.to(DEV), r.to(DEV)
+        q, s = bb.rmsnorm_quantize(over, g.to(DEV), eps, residual=into, residual_out=over)
+        q2, s2 = bb.rmsnorm_quantize(x.to(DEV), g.to(DEV), eps, residual=into)
+        assert torch.equal(over.cpu(), h) and torch.equal(into.cpu(), h) and torch.equal(q, q2) and torch.equal(s.view(torch.int32), s2.view(torch.int32))
+        check_norm(q[keep], s[keep], h[keep], g, eps)
+
+
+@pytest.mark.gpu
+def test_more_rows_than_one_launch_holds():
+    rows = (1 << 21) + 3
+    x = (torch.arange(rows * 8, device=DEV) % 509 - 254).view(rows, 8).float()
+    q, s = bb.quantize_rows(x)
+    top = x.abs().amax(1).double()
+    assert torch.equal(s, (top / 127).float())
+    assert torch.equal(q, torch.round(127 * x.double() / top[:, None]).to(torch.int8))
+
+
 def codes(seed, rows, cols):
     return torch.randint(-128, 128, (rows, cols), generator=gen(seed), dtype=torch.int16).to(torch.int8)
 
@@ -218,6 +257,36 @@ def test_gemm_int8_against_the_exact_product(M, N, K, dtype):
     pad = 16 - K % 16 if K % 16 else 16
     out = bb.gemm_int8(strided(a, pad), dsa, strided(w, pad), dsw, bias=db, dtype=t)
     check_gemm(out, a, sa, w, sw, bias)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,bias", [("bf16", True), ("fp32", False), ("fp16", True)])
+@pytest.mark.parametrize("M,N,K", [
+    (2047, 8190, 4100),                         # 256 x 256 tiles
+    (511, 24570, 1030), (767, 3582, 18950),     # 256 x 192, k whole and in four
+    (2999, 5001, 1200), (897, 4096, 12290),     # 128 x 128, and k in two; several tiles per workgroup
+    (2600, 7700, 260), (119, 4090, 12300),      # 128 x 64, and k in four
+    (255, 1023, 8193),                          # 64 x 64, k in four
+    (15, 1022, 8200), (1, 24576, 1040),         # 32 x 32, k in eight and whole
+])
+def test_gemm_int8_every_tile_and_split(M, N, K, dtype, bias):
+    """Large enough for each of the tiles, with ragged rows, columns and k; on the GPU in 64 bits (integers below 2^53: exact)."""
+    g = torch.Generator(device=DEV).manual_seed(M + N + K)
+    ld = (K + 15) // 16 * 16
+    a, w = (torch.randint(-128, 128, (rows, ld), generator=g, device=DEV, dtype=torch.int8)[:, :K] for rows in (M, N))
+    sa, sw = torch.rand(M, generator=g, device=DEV) * 0.02, torch.rand(N, generator=g, device=DEV) * (0.5 / K)
+    b = torch.randn(N, generator=g, device=DEV) if bias else None
+    base = torch.full((M + 1, N + 5), 7.0, dtype=TYPES[dtype], device=DEV)
+    out = base[:M, 3:N + 3]
+    bb.gemm_int8(a, sa, w, sw, bias=b, out=out)
+    scaled = torch.mm(a.double(), w.double().t().contiguous()) * sa.double()[:, None] * sw.double()
+    want, size = scaled, scaled.abs()
+    if bias:
+        want, size = want + b.double(), size + b.double().abs()
+    half = 0.0 if dtype == "fp32" else torch.finfo(out.dtype).eps / 2 * (1 + 2.0 ** -20)
+    assert ((out.double() - want).abs() <= 4 * 2.0 ** -24 * size + half * want.abs() + (2.0 ** -25 if dtype == "fp16" else 2.0 ** -149)).all()
+    base[:M, 3:N + 3] = 7
+    assert (base == 7).all()
 
 
 @pytest.mark.gpu
