@@ -6,6 +6,13 @@
 // The operands: the matrix cores take 16 rows x 64 k, lane l holding the 16 bytes k = 16 (l / 16) .. + 15 of row l % 16, so row-major
 // operands need no re-tiling: 16-byte pieces of their rows are what a lane wants.  W is the first operand: a lane then holds four
 // consecutive columns of one row of C.
+//
+// What bounds it.  Large products: what the L2s deliver, at the clock that power allows.  MFMAs alone on such operands run at 4.1 POP/s (1.95 GHz);
+// with the LDS reads 3.6-3.8; with the loads too 2.9 in the loop over k of a 256 x 256 tile (64 KB per CU and chunk of 128 k, 1.36 us, of 47 KB/us; the
+// matrix pipes are busy 0.67 of the time at 1.88 GHz), and 2.4 over 8192 x 8192 x 8192 (459 us) and 8192 x 24576 x 4096 (0.68 ms), with the
+// tiles' ends.  Loads by 64-byte runs reach half the rate of whole lines (66 against 130 KB/us and CU from an L2): hence chunks of 128 k, and
+// rows at multiples of 128 bytes are fastest (1402 x 4610 rows of 3592 k 41 us, of 3584 34).  Few rows: the stream of W, 5.4 TB/s of 100 MB
+// at one row; between them (120 rows, 50 MB) 14 us beside 5 us that join four splits of k.
 #include "bb_internal.h"
 #include "lds.h"
 #include "sched.h"
@@ -93,6 +100,7 @@ static __device__ __forceinline__ u32x4 load16(const int8_t* row, int k, int K) 
     hi >>= sh;
     return __builtin_bit_cast(u32x4, u64x2{none ? 0 : lo, none ? 0 : hi});
 }
+
 // Rows of fewer than 16 bytes: a thread per value of C.
 __global__ __launch_bounds__(256) void gemm_int8_short_kernel(GemmInt8Args a) {
     const size_t values = (size_t)a.M * a.N;
@@ -120,8 +128,8 @@ __global__ __launch_bounds__(256) void align_rows_kernel(const int8_t* __restric
 // The tiled kernel: operands whose rows are 16-byte aligned.  A workgroup of four waves (WM of them along m) owns 16 R WM rows x 16 T (4 / WM)
 // columns, a wave 16 R x 16 T of them.  Both operands pass through LDS in chunks of 128 k: a direct-to-LDS load brings a unit of eight rows x
 // 128 k (1 KiB), eight lanes a row, so that whole 128-byte lines are asked for at once, into a ring of NS chunks; fragments of the next
-// half chunk move into registers while the matrix cores work on the present one.  In a unit piece c (16 bytes) of row r lies at
-// 8 r + (c ^ r): eight lanes that read one piece of eight rows touch all banks once.
+// half chunk move into registers while the matrix cores work on the present one.  In unit u piece c (16 bytes) of row r lies at
+// 8 r + (c ^ r ^ 4 (u % 2)): eight lanes that read one piece of eight rows, of one unit or of half of two (see column_of), touch all banks once.
 // Workgroups are as many as run at once and take item after item (a tile, or a split's part of its k): the chunks of all their items pass
 // through the ring as one stream, so that the next item's are on their way while a tile is stored.
 // The chunk of a ragged end of k (K % 128) is brought through registers, with zeros past the end.

@@ -367,6 +367,27 @@ def test_capture_replay_and_another_stream():
     assert torch.equal(got, want)
 
 
+@pytest.mark.gpu
+def test_two_streams_at_once():
+    """Products whose k is split, on two streams together: each has its own partial sums."""
+    M, N, K = 120, 2048, 8192
+    g = torch.Generator(device=DEV).manual_seed(9)
+    sides = []
+    for _ in range(2):
+        a, w = (torch.randint(-128, 128, (n, K), generator=g, device=DEV, dtype=torch.int8) for n in (M, N))
+        sides.append((a, torch.rand(M, generator=g, device=DEV), w, torch.rand(N, generator=g, device=DEV)))
+    want = [bb.gemm_int8(*s, dtype=torch.float32) for s in sides]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for _ in range(20):
+        for i, st in enumerate(streams):
+            got[i].append(bb.gemm_int8(*sides[i], dtype=torch.float32, stream=st))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[i]) for i in range(2) for o in got[i])
+
+
 def fake(*shape, dtype=torch.float32):
     return torch.zeros(*shape, dtype=dtype)
 
