@@ -369,14 +369,18 @@ template <int R, int T, int WM, int NS, int PER_CU> static void launch_tiled(con
 }
 
 // The bodies of the tiled kernel and what they cost, in us: start + per round of items the most loaded CU takes (round), per chunk of
-// those (chunk), per chunk and workgroup that shares a CU (shared); per join (join) and MB of partial sums (per_mb).  Fitted to 8600 launches
-// (18 row counts from 1 to 8192 x 11 matrices from 256 x 688 to 37888 x 3584 x k splits); over those the choice is on average 2 % slower than
-// the best body and split of all that were tried, at worst 32 %.
+// those (chunk), per chunk and workgroup that shares a CU (shared); per join (join) and MB of partial sums (per_mb).  Fitted to launches of
+// 18 row counts from 1 to 8192 x 11 matrices from 256 x 688 to 37888 x 3584 x k splits; there the choice is on average 1 % slower than the best
+// of these bodies and splits, at worst 26 %, and where all weights come from memory (640 MB of them in turn, 13 row counts up to 1024) 1 and
+// 16 %.  The second 128 x 128, one workgroup a CU and a chunk more in flight than the first's two each, is for such weights when no CU has a
+// second tile: bf16 results of 192 rows by 12288 x 4096 23.4 us (30.9 with the first, 27.8 the best without it), 120 by 24576 x 4096 30.1
+// (34.6); with more tiles two workgroups that overlap win: 1024 by 37888 x 3584 166 (182).
 struct Int8Body { int bm, bn, per_cu; float start, round, chunk, shared, join, per_mb; };
 static const Int8Body i8_bodies[] = {
     {256, 256, 1, 0.64f, 11.92f, 1.328f, 0.043f, 0.0f, 0.239f},
     {256, 192, 1, 0.77f, 8.02f, 0.994f, 0.006f, 1.89f, 0.197f},
     {128, 128, 2, 2.03f, 2.69f, 0.369f, 0.485f, 2.62f, 0.238f},
+    {128, 128, 1, 4.20f, 1.25f, 0.484f, 0.0f, 3.19f, 0.262f},
     {128, 64, 2, 3.89f, 0.95f, 0.028f, 0.529f, 2.54f, 0.248f},
     {64, 64, 2, 3.95f, 0.49f, 0.073f, 0.305f, 2.25f, 0.328f},
     {32, 32, 3, 4.06f, 0.11f, 0.100f, 0.184f, 1.85f, 0.770f},
@@ -409,8 +413,9 @@ static void launch_plan(const GemmInt8Args& a, const Int8Plan& p, void* workspac
         case 0: launch_tiled<8, 8, 2, 2, 1>(a, p.split, workspace_dev, s); break;
         case 1: launch_tiled<8, 6, 2, 2, 1>(a, p.split, workspace_dev, s); break;
         case 2: launch_tiled<4, 4, 2, 2, 2>(a, p.split, workspace_dev, s); break;
-        case 3: launch_tiled<4, 2, 2, 3, 2>(a, p.split, workspace_dev, s); break;
-        case 4: launch_tiled<2, 2, 2, 4, 2>(a, p.split, workspace_dev, s); break;
+        case 3: launch_tiled<4, 4, 2, 3, 1>(a, p.split, workspace_dev, s); break;
+        case 4: launch_tiled<4, 2, 2, 3, 2>(a, p.split, workspace_dev, s); break;
+        case 5: launch_tiled<2, 2, 2, 4, 2>(a, p.split, workspace_dev, s); break;
         default: launch_tiled<1, 1, 2, 4, 3>(a, p.split, workspace_dev, s); break;
     }
 }

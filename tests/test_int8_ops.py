@@ -264,7 +264,9 @@ def test_gemm_int8_against_the_exact_product(M, N, K, dtype):
 @pytest.mark.parametrize("M,N,K", [
     (2047, 8190, 4100),                         # 256 x 256 tiles
     (511, 24570, 1030), (767, 3582, 18950),     # 256 x 192, k whole and in four
-    (2999, 5001, 1200), (897, 4096, 12290),     # 128 x 128, and k in two; several tiles per workgroup
+    (2999, 5001, 1200), (271, 8117, 19000),     # 128 x 128, and k in two; several tiles per workgroup
+    (897, 4096, 12290), (199, 4610, 8200),      # 128 x 128 with the deeper ring, k whole and in three
+    (549, 4094, 1100),
     (2600, 7700, 260), (119, 4090, 12300),      # 128 x 64, and k in four
     (255, 1023, 8193),                          # 64 x 64, k in four
     (15, 1022, 8200), (1, 24576, 1040),         # 32 x 32, k in eight and whole
