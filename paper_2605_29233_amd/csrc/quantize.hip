@@ -65,25 +65,40 @@ template <class T> struct Eight {
     __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, w, sizeof(w)); }
 };
 
-// x / (1 + exp(-x)).  exp(-x) = 2^(-x log2 e): the product in two parts, the second (its rounding, and what a float of log2 e leaves out)
-// as a factor 1 + part ln 2.  Halves of a last place: 1 for the product's parts, 2 each for the hardware's exp2 and reciprocal, 1 each for the
-// factor, the sum, the product with x: 8, and 1 for the product with `up`.
+// x / (1 + exp(-x)) for x >= SILU_FAR.  exp(-x) = 2^(-x log2 e): the product in two parts, the second (its rounding, and what a float of log2 e
+// leaves out) as a factor 1 + part ln 2.  Halves of a last place: 1 for the product's parts, 2 each for the hardware's exp2 and reciprocal, 1 each for
+// the factor, the sum, the product with x: 8, and 1 for the product with `up`.
+#define SILU_FAR (-87.0f)
+#define SILU_FAR_BITS 0xC2AE0000u
 static __device__ __forceinline__ float silu(float x) {
     constexpr float L = -1.44269504088896340736f, L_REST = (float)(-1.44269504088896340736 - (double)L);
     const float hi = x * L, lo = fmaf(x, L_REST, fmaf(x, L, -hi)), e0 = __builtin_amdgcn_exp2f(hi);
     const float e = fabsf(hi) < 126.0f ? fmaf(e0, lo * 0.693147180559945309417f, e0) : e0;     // (beyond, infinity times a small part)
     return x * __builtin_amdgcn_rcpf(1.0f + e);
 }
+// SiLU(x) * up for x < SILU_FAR, where 1 + exp(-x) nears or leaves fp32's range (and its reciprocal is subnormal) although the product with a large `up` is an
+// ordinary value: x exp(x) up (1 + exp(x) is 1 to 2^-125), exp(x) as the square of 2^(x log2 e / 2), `up` between its factors, so that nothing leaves the range
+// before the value itself does (below x = -174 the value is under 2^-110 whatever `up` is).  Halves of a last place: 2 for each of the two factors, 4 products, 1 for the second
+// part's factor: 9.
+static __device__ __forceinline__ float silu_far(float x, float up) {
+    constexpr float L = 1.44269504088896340736f, L_REST = (float)(1.44269504088896340736 - (double)L);
+    const float least = fmaxf(x, -512.0f), hi = least * L, lo = fmaf(least, L_REST, fmaf(least, L, -hi)), e = __builtin_amdgcn_exp2f(0.5f * hi);
+    return x * e * up * (e * fmaf(lo, 0.693147180559945309417f, 1.0f));        // (-infinity times 0 is NaN, as in the formula)
+}
 
-// What a row's values are, at column c, in 64 bits, from memory (h once it is written).
-template <int OP, class T> static __device__ __forceinline__ double exact_value(const QuantArgs& a, long row, int c) {
+// What a row's values are, at column c, in 64 bits, from memory (h once it is written).  ZEROS: products with a zero are likely.
+template <int OP, class T, bool ZEROS = false> static __device__ __forceinline__ double exact_value(const QuantArgs& a, long row, int c) {
     if constexpr (OP == QOP_PANEL) {
         auto term = [&](int t) { return (double)widen(((const T*)((const u32x4*)a.x + packA_u4((int)row, c >> 3, a.mt_total, t)))[c & 7]); };
         return term(0) + term(1);
     }
     const double x = widen((OP == QOP_NORM && a.x2 ? (const T*)a.h + row * a.ldh : (const T*)a.x + row * a.ldx)[c]);
     if constexpr (OP == QOP_NORM) return x * (double)widen(((const T*)a.gain)[c]);
-    if constexpr (OP == QOP_SWIGLU) return x / (1.0 + exp(-x)) * (double)widen(((const T*)a.x2 + row * a.ldx2)[c]);
+    if constexpr (OP == QOP_SWIGLU) {
+        const double up = widen(((const T*)a.x2 + row * a.ldx2)[c]);
+        if (ZEROS && (x == 0.0 || up == 0.0)) return x * up;
+        return x / (1.0 + exp(-x)) * up;
+    }
     return x;
 }
 
@@ -109,6 +124,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
     float v[KEEP][8], v_tail = 0.f;
     double ss = 0.0, top2 = 0.0;
     unsigned top_bits = 0u;                                 // as whole numbers |v| are in order, infinity and NaN at the end
+    unsigned low_bits = 0u;                                 // of the lowest gate: as whole numbers negative values come after all others, the lowest last
     Eight<T> kx[KEEP], ky[OP == QOP_ROWS ? 1 : KEEP], kr[OP == QOP_NORM ? KEEP : 1];
     auto fetch = [&](int i, int g, bool again) {            // (nothing that would make a load wait for the one before it)
         const int c = g * 8;
@@ -124,19 +140,19 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
             if (x2 && !again) kr[i].load(x2 + c);
         }
     };
-    auto value = [&](float f, float w) {
+    auto value = [&](float f, float w, bool far) {          // far: a gate below SILU_FAR
         float y = f;
         if constexpr (OP == QOP_NORM) {
             y = f * w;
             ss = fma((double)f, (double)f, ss);
             if constexpr (TOP_IN_DOUBLE) top2 = fmax(top2, fabs((double)f * (double)w));
         }
-        if constexpr (OP == QOP_SWIGLU) y = silu(f) * w;
+        if constexpr (OP == QOP_SWIGLU) y = far ? silu_far(f, w) : silu(f) * w;
         if constexpr (OP == QOP_PANEL) y = f + w;           // (exact: 16 bits and the sign)
         top_bits = max(top_bits, __float_as_uint(y) & 0x7FFFFFFFu);
         return y;
     };
-    auto values = [&](int i, int g, bool again) {
+    auto values = [&](int i, int g, bool again, auto Far) {      // Far: gates below SILU_FAR taken as such; else only noticed
         if constexpr (OP == QOP_NORM)
             if (x2 && !again) {
 #pragma unroll
@@ -144,8 +160,14 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
                 kx[i].store(h + g * 8);
             }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = value(kx[i].get(j), OP == QOP_ROWS ? 0.f : ky[OP == QOP_ROWS ? 0 : i].get(j));
+        for (int j = 0; j < 8; ++j) {
+            const float f = kx[i].get(j);
+            if constexpr (OP == QOP_SWIGLU && !decltype(Far)::value) low_bits = max(low_bits, __float_as_uint(f));
+            v[i][j] = value(f, OP == QOP_ROWS ? 0.f : ky[OP == QOP_ROWS ? 0 : i].get(j), decltype(Far)::value && f < SILU_FAR);
+        }
     };
+    const std::false_type near{};
+    const std::true_type far{};
     if constexpr (G > 0) {
 #pragma unroll
         for (int i = 0; i < G; ++i) if (t + i * THREADS < groups) fetch(i, t + i * THREADS, false);
@@ -158,17 +180,34 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
                 h[c_tail] = n;
                 f = widen(n);
             }
-        v_tail = value(f, OP == QOP_NORM ? widen(gain[c_tail]) : OP == QOP_SWIGLU ? widen(x2[c_tail]) : 0.f);
+        v_tail = value(f, OP == QOP_NORM ? widen(gain[c_tail]) : OP == QOP_SWIGLU ? widen(x2[c_tail]) : 0.f, f < SILU_FAR);
     }
     if constexpr (G > 0) {
 #pragma unroll
         for (int i = 0; i < G; ++i) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-            if (t + i * THREADS < groups) values(i, t + i * THREADS, false);
+            if (t + i * THREADS < groups) values(i, t + i * THREADS, false, near);
         }
     } else
-        for (int g = t; g < groups; g += THREADS) { fetch(0, g, false); values(0, g, false); }
+        for (int g = t; g < groups; g += THREADS) { fetch(0, g, false); values(0, g, false, near); }
+    // Gates below SILU_FAR are rare: they are only noticed above, and a wave that met one reads its groups again.
+    bool careful = false;
+    if constexpr (OP == QOP_SWIGLU) {
+        careful = __any(low_bits > SILU_FAR_BITS);
+        if (__builtin_expect(careful, 0)) {
+            top_bits = __float_as_uint(v_tail) & 0x7FFFFFFFu;
+            if constexpr (G > 0) {
+#pragma unroll
+                for (int i = 0; i < G; ++i) if (t + i * THREADS < groups) { fetch(i, t + i * THREADS, true); values(i, t + i * THREADS, true, far); }
+            } else
+                for (int g = t; g < groups; g += THREADS) { fetch(0, g, true); values(0, g, true, far); }
+        }
+    }
+    auto values_again = [&](int g) {                        // (G = 0)
+        fetch(0, g, true);
+        if (careful) values(0, g, true, far); else values(0, g, true, near);
+    };
 
     // ---- the row's maximum (and sum of squares) ----------------------------------------------------------------------------------------
     __shared__ double sh_ss[16], sh_top[16];
@@ -209,12 +248,12 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
     // Rows so large or small that fp32 products would not do (and those that hold an infinity or a NaN): everything in double.
     const bool hard = !(top_bits > 0x0D800000u && top_bits < 0x71800000u);     // 2^-100, 2^100
     bool bad = false;
-    // (a row of zeros needs no second look: what v holds exactly, and SiLU * up below fp32's range counts as zero)
-    if (hard && (top_bits != 0u || (OP == QOP_NORM && ss > 0.0))) {
+    // (zeros that v holds exactly need no second look; a norm's or SwiGLU's products below fp32's range do)
+    if (hard && (top_bits != 0u || (OP == QOP_NORM && ss > 0.0) || OP == QOP_SWIGLU)) {
         double d = 0.0;
         int b = 0;
         auto look = [&](int c) {                            // (columns of this thread's own: h is as it wrote it)
-            const double y = fabs(exact_value<OP, T>(a, row, c));
+            const double y = fabs(exact_value<OP, T, true>(a, row, c));
             b |= !(y < INFINITY);
             d = fmax(d, y);
         };
@@ -238,7 +277,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
 #pragma unroll
             for (int i = 0; i < G; ++i) look(i, t + i * THREADS);       // (groups that do not exist hold zeros)
         } else
-            for (int g = t; g < groups; g += THREADS) { fetch(0, g, true); values(0, g, true); look(0, g); }
+            for (int g = t; g < groups; g += THREADS) { values_again(g); look(0, g); }
         if (fabsf(v_tail) >= least) d = fmax(d, fabs(exact_value<OP, T>(a, row, c_tail)));
         top = reduce_top(d);
     }
@@ -299,7 +338,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
 #pragma unroll
         for (int i = 0; i < G; ++i) if (t + i * THREADS < groups) codes(i, t + i * THREADS);
     } else
-        for (int g = t; g < groups; g += THREADS) { fetch(0, g, true); values(0, g, true); codes(0, g); }
+        for (int g = t; g < groups; g += THREADS) { values_again(g); codes(0, g); }
     if (tail) {
         float far;
         const unsigned b = code_bits(v_tail, far);
