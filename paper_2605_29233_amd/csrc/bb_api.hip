@@ -485,7 +485,13 @@ static void int8_layout(const bb_ctx* c, char* base, size_t* total, std::vector<
     *total = align_up(b.off, 256);
 }
 
+// (the exact sums' limit; d_model is at most 8192)
+static bool int8_shape_ok(const bb_model_cfg& m) {
+    return m.d_ffn <= BB_GEMM_INT8_MAX_K && (long)m.n_q_heads * m.head_dim <= BB_GEMM_INT8_MAX_K;
+}
+
 static size_t bb_int8_layers_bytes_impl(bb_ctx* c) {
+    if (!int8_shape_ok(c->m)) return 0;
     std::vector<Int8Layer> layers; int8_t* rows; float* scales; char* part; size_t part_bytes, total = 0;
     int8_layout(c, nullptr, &total, &layers, &rows, &scales, &part, &part_bytes);
     return total;
@@ -498,6 +504,7 @@ static int bb_int8_layers_impl(bb_ctx* c, void* mem, size_t bytes) {
         c->i8.clear();
         return BB_OK;
     }
+    if (!int8_shape_ok(c->m)) return fail(c, BB_EINVAL, "d_ffn and the heads' width must not exceed BB_GEMM_INT8_MAX_K");
     if (reinterpret_cast<uintptr_t>(mem) % 256) return fail(c, BB_EINVAL, "the int8 layers' memory must be 256-byte aligned");
     if (bytes < bb_int8_layers_bytes_impl(c)) return fail(c, BB_ENOMEM, "less memory than bb_int8_layers_bytes");
     if (!c->i8.empty()) HIPCHK(c, hipStreamSynchronize(c->stream));     // (the memory given before is the caller's again)
