@@ -269,7 +269,7 @@ int bb_gemm_static(const float* A_dev, const uint16_t* W_dev, float* C_dev, int 
  * channel; embeddings, norms, attention, K,V and the LM head stay as they are.  A block step then streams a byte per weight instead of two.
  * mem_dev: device memory of at least bb_int8_layers_bytes(ctx), 256-byte aligned, which the context uses until it is destroyed or the
  * call is made again (mem_dev == NULL: the format is switched off); a call that takes memory away waits for the stream first.  The codes are made from the loaded weights by
- * the next forward, and again after bb_load_weights.  The tuning knobs of the other formats (bb_debug_set_gemm_plan,
+ * the next forward, and again after bb_load_weights (one that is captured into a graph makes them at every replay).  The tuning knobs of the other formats (bb_debug_set_gemm_plan,
  * bb_debug_wide_format) have no effect meanwhile.  d_ffn and n_q_heads * head_dim must not exceed BB_GEMM_INT8_MAX_K (0 bytes, BB_EINVAL). */
 size_t bb_int8_layers_bytes(bb_ctx* ctx);
 int bb_int8_layers(bb_ctx* ctx, void* mem_dev, size_t bytes);

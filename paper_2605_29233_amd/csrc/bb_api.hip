@@ -536,7 +536,9 @@ static int int8_weights(bb_ctx* c, int li) {
     if (rc == BB_OK) rc = matrix(W.wgu, L.gu, 2 * m.d_ffn, m.d_model, m.d_ffn);
     if (rc == BB_OK) rc = matrix(W.wdown, L.down, m.d_model, m.d_ffn, 0);
     if (rc != BB_OK) return fail(c, rc, "quantising the weights failed");
-    L.stale = false;
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;        // (captured work has not run: the codes are still to be made)
+    if (c->stream) HIPCHK(c, hipStreamIsCapturing(c->stream, &capture));
+    L.stale = capture != hipStreamCaptureStatusNone;
     return BB_OK;
 }
 
