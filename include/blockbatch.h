@@ -279,7 +279,7 @@ int bb_int8_layers(bb_ctx* ctx, void* mem_dev, size_t bytes);
  * needed; all work is enqueued on hip_stream (a hipStream_t of the current device, NULL = its default stream); nothing is
  * allocated, memset or synchronised, so every call may be captured into a graph.  Pointers are device memory, aligned to their
  * element's size; ld* is the distance between rows in elements (ignored for a single row): rows of an output must not overlap
- * (ld >= columns), those of an input may, and nothing between the columns and ld is read or written.  Rows that are 16-byte aligned are
+ * (ld >= columns) nor overlap an input's, those of an input may overlap each other, and nothing between the columns and ld is read or written.  Rows that are 16-byte aligned are
  * fastest.  Malformed arguments: BB_EINVAL; a HIP error: BB_EHIP (no context, hence no bb_last_error text).  No rows: BB_OK,
  * nothing is launched. */
 #define BB_F32  0
@@ -293,7 +293,7 @@ int bb_int8_layers(bb_ctx* ctx, void* mem_dev, size_t bytes);
 int bb_quantize_rows(const void* x_dev, long ldx, int8_t* q_dev, long ldq, float* scale_dev, long rows, int cols, int type,
                      void* hip_stream);
 
-/* h = x + residual, rounded to `type` and stored in residual_out (may be residual or x themselves); then the rows of
+/* h = x + residual, rounded to `type` and stored in residual_out (may be residual or x themselves, with their ld; BB_EINVAL if it overlaps them otherwise); then the rows of
  * y = h / sqrt(mean_c h^2 + eps) * gain quantised as above, y unrounded.  Without a residual (both residual pointers NULL) h = x.
  * gain: [cols]; x, residual, residual_out, gain of the same type.  eps >= 0. */
 int bb_rmsnorm_quantize(const void* x_dev, long ldx, const void* residual_dev, long ldr, void* residual_out_dev, long ldo,

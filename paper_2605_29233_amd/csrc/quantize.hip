@@ -13,6 +13,7 @@
 // a large copy reaches 5.1.  One row of 4096: 3.1, 3.9 and 4.2 us, an empty launch 2.5.
 #include "bb_internal.h"
 #include <algorithm>
+#include <cstdlib>
 #include <type_traits>
 
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
@@ -396,6 +397,17 @@ static bool refuse_out(const void* q, long ldq, const void* scale, long rows, in
 static bool refuse_rows(const void* p, int type, long rows, long ld) {
     return !p || (uintptr_t)p % (type == BB_F32 ? 4 : 2) || (rows > 1 && ld < 0);
 }
+// Rows that are written (w, ldw >= cols) while others (r) are read: right where they are the same rows or have no element in common.  Two matrices of one row
+// distance may interleave (column ranges of one tensor); of different ones whose extents overlap, it counts as overlap.
+static bool refuse_overlap(const void* r, long ldr, const void* w, long ldw, long rows, int cols, int type) {
+    const long size = type == BB_F32 ? 4 : 2, r0 = (long)(uintptr_t)r, w0 = (long)(uintptr_t)w;
+    if (rows == 1) ldr = ldw = cols;
+    if (r0 == w0 && ldr == ldw) return false;
+    const long r1 = r0 + ((rows - 1) * ldr + cols) * size, w1 = w0 + ((rows - 1) * ldw + cols) * size;
+    if (r1 <= w0 || w1 <= r0) return false;
+    const long apart = labs(r0 - w0) % (ldw * size);
+    return ldr != ldw || apart < cols * size || ldw * size - apart < cols * size;
+}
 
 // The layers of a forward: fp32 rows, of which *live count.
 void launch_rmsnorm_quantize(const float* x, float* residual, const float* gain, float eps, int8_t* q, long ldq, float* scale, long rows, int cols,
@@ -431,7 +443,9 @@ extern "C" int bb_rmsnorm_quantize(const void* x_dev, long ldx, const void* resi
     if (rows == 0) return BB_OK;
     if (refuse_out(q_dev, ldq, scale_dev, rows, cols) || refuse_rows(x_dev, type, rows, ldx) || refuse_rows(gain_dev, type, rows, 0)) return BB_EINVAL;
     if (!(eps >= 0.f) || !(eps < INFINITY) || !residual_dev != !residual_out_dev) return BB_EINVAL;
-    if (residual_dev && (refuse_rows(residual_dev, type, rows, ldr) || refuse_rows(residual_out_dev, type, rows, ldo) || (rows > 1 && ldo < cols))) return BB_EINVAL;
+    if (residual_dev && (refuse_rows(residual_dev, type, rows, ldr) || refuse_rows(residual_out_dev, type, rows, ldo) || (rows > 1 && ldo < cols) ||
+                         refuse_overlap(x_dev, ldx, residual_out_dev, ldo, rows, cols, type) || refuse_overlap(residual_dev, ldr, residual_out_dev, ldo, rows, cols, type)))
+        return BB_EINVAL;
     QuantArgs a{};
     a.x = x_dev; a.ldx = ldx; a.x2 = residual_dev; a.ldx2 = ldr; a.h = residual_out_dev; a.ldh = ldo; a.gain = gain_dev; a.eps = eps;
     a.q = q_dev; a.ldq = ldq; a.scale = scale_dev; a.rows = rows; a.cols = cols;

@@ -1,11 +1,12 @@
-"""The 8-bit integer operators at the edges of their ranges: gates so negative that exp(-gate) leaves fp32.
+"""The 8-bit integer operators at the edges of their ranges: gates so negative that exp(-gate) leaves fp32, sums written
+over rows that are still to be read.
 
 The references and tolerances are those of tests/test_int8_ops.py: codes equal the formula's in 64 bits, a scale is one fp32 rounding of it."""
 import pytest
 import torch
 
 import paper_2605_29233_amd as bb
-from test_int8_ops import DEV, TYPES, check_swiglu, gen, rnd, strided
+from test_int8_ops import DEV, TYPES, check_norm, check_swiglu, gen, rnd, strided
 
 
 @pytest.mark.gpu
@@ -50,3 +51,42 @@ def test_swiglu_of_the_lowest_gates_and_of_infinities(dtype):
     gate[3, 7], up[3, 7] = -1e4, float("inf")
     gate[4], up[4] = -300.0, 1e38           # 1e-90: the scale rounds to 0
     check_swiglu(*bb.swiglu_quantize(gate.to(DEV), up.to(DEV)), gate, up)
+
+
+def test_a_sum_written_over_rows_still_to_be_read_is_refused_on_the_host():
+    """residual_out may be x or residual (same address and row distance) or lie apart or between them, column ranges of one tensor; rows of it that are other rows
+    of an input are a race.  Refused before anything is launched: the addresses are never dereferenced."""
+    from paper_2605_29233_amd.binding import load_library
+    lib = load_library()
+    p = 1 << 20
+
+    def norm(x, ldx, res, ldr, out, ldo, rows=4, cols=64):
+        return lib.bb_rmsnorm_quantize(x, ldx, res, ldr, out, ldo, p, 1e-5, p, 64, p, rows, cols, 1, None)
+
+    far = p + (1 << 16)
+    for x, ldx, res, ldr, out, ldo in (
+            (p, 64, far, 64, p, 128), (p, 0, far, 64, p, 64), (far, 64, p, 64, p, 128), (far, 64, p, 0, p, 64),         # the same rows at another distance
+            (p, 64, far, 64, p + 128, 64), (far, 64, p + 128, 64, p, 64), (p, 128, far, 64, p + 2 * 128 * 2, 128),      # other rows of the same tensor
+            (p, 128, far, 64, p + 2 * 63, 128), (p, 128, far, 64, p + 2 * 65, 128), (p + 2 * 127, 128, far, 64, p, 128),    # columns in common
+            (p + 2 * 100, 0, far, 64, p, 128)):                                                                         # one row read again and again
+        assert norm(x, ldx, res, ldr, out, ldo) == -1, (x - p, ldx, res - p, ldr, out - p, ldo)
+
+
+@pytest.mark.gpu
+def test_sums_beside_and_over_their_inputs():
+    """What stays allowed: over x or residual, or between their columns in one tensor; a single row at any distance."""
+    cols, rows = 72, 37
+    for x0, r0, o0, width in ((0, 72, 144, 216), (0, 72, 0, 144), (0, 72, 72, 200), (72, 0, 144, 216)):
+        base = torch.randn(rows, width, generator=gen(x0 + r0 + o0)).to(torch.bfloat16)
+        d, gain = base.to(DEV), rnd(5, 1, cols, "bf16")[0]
+        x, r = base[:, x0:x0 + cols], base[:, r0:r0 + cols]
+        h = (x.float() + r.float()).to(torch.bfloat16)
+        q, s = bb.rmsnorm_quantize(d[:, x0:x0 + cols], gain.to(DEV), 1e-5, residual=d[:, r0:r0 + cols], residual_out=d[:, o0:o0 + cols])
+        check_norm(q, s, h, gain, 1e-5)
+        base[:, o0:o0 + cols] = h
+        assert torch.equal(d.cpu(), base)
+    with pytest.raises(bb.BBError):
+        bb.rmsnorm_quantize(d[1:, :cols], gain.to(DEV), 1e-5, residual=d[:-1, cols:2 * cols], residual_out=d[:-1, :cols])
+    one = rnd(6, 1, cols, "bf16").to(DEV)
+    h = (one.float() * 2).to(torch.bfloat16).cpu()
+    check_norm(*bb.rmsnorm_quantize(one, gain.to(DEV), 1e-5, residual=one), h, gain, 1e-5)
