@@ -309,8 +309,8 @@ int bb_swiglu_quantize(const void* gate_dev, long ldg, const void* up_dev, long 
  * M and N at most BB_GEMM_INT8_MAX_ROWS.
  * workspace_dev: at least bb_gemm_int8_workspace_bytes(M, N, K, aligned) bytes, 16-byte aligned (may be NULL if that is 0), used
  * by this call alone until its work is done; BB_ENOMEM if it is smaller.  aligned: nonzero if A_dev, W_dev, lda and ldw are multiples of 16
- * (and lda, ldw at most 2^23; the ld of a single row counts as 0).  Operands that are not are copied first;
- * rows at multiples of 128 bytes are fastest. */
+ * (and lda, ldw at most 2^23; the ld of a single row counts as 0).  An operand that is not is copied first (the
+ * workspace has room for both); rows at multiples of 128 bytes are fastest. */
 #define BB_GEMM_INT8_MAX_K 131071
 #define BB_GEMM_INT8_MAX_ROWS (1 << 30)
 size_t bb_gemm_int8_workspace_bytes(int M, int N, int K, int aligned);

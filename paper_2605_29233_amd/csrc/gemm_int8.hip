@@ -450,8 +450,9 @@ extern "C" int bb_gemm_int8(const int8_t* A_dev, long lda, const float* a_scale_
     hipStream_t s = (hipStream_t)hip_stream;
     // the tiled kernel's offsets within a tile are of 32 bits
     const long far = 1 << 23;
-    const int aligned = (uintptr_t)A_dev % 16 == 0 && (uintptr_t)W_dev % 16 == 0 && lda % 16 == 0 && ldw % 16 == 0 && lda <= far && ldw <= far;
-    const size_t need = bb_gemm_int8_workspace_bytes(M, N, K, aligned);
+    auto aligned = [&](const int8_t* p, long ld) { return (uintptr_t)p % 16 == 0 && ld % 16 == 0 && ld <= far; };
+    const bool a_aligned = aligned(A_dev, lda), w_aligned = aligned(W_dev, ldw);
+    const size_t need = bb_gemm_int8_workspace_bytes(M, N, K, a_aligned && w_aligned);
     if (need > 0 && (!workspace_dev || (uintptr_t)workspace_dev % 16)) return workspace_bytes < need ? BB_ENOMEM : BB_EINVAL;
     if (workspace_bytes < need) return BB_ENOMEM;
     GemmInt8Args a{A_dev, W_dev, a_scale_dev, w_scale_dev, bias_dev, C_dev, lda, ldw, ldc, M, N, K, c_type, nullptr};
@@ -460,19 +461,17 @@ extern "C" int bb_gemm_int8(const int8_t* A_dev, long lda, const float* a_scale_
         return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
     }
     const Int8Plan p = int8_plan(M, N, K);
-    if (!aligned) {
-        const int per_row = (K + 15) / 16;
-        char* at = (char*)workspace_dev + align_up(p.partial_bytes, 256);
-        auto copy = [&](const int8_t* src, long ld, int rows) {
-            const size_t pieces = (size_t)rows * per_row;
-            align_rows_kernel<<<(unsigned)std::min<size_t>((pieces + 255) / 256, 8192), 256, 0, s>>>(src, ld, (u32x4*)at, pieces, per_row, K);
-            const int8_t* to = (const int8_t*)at;
-            at += copy_bytes(rows, K);
-            return to;
-        };
-        a.A = copy(A_dev, lda, M); a.lda = per_row * 16L;
-        a.W = copy(W_dev, ldw, N); a.ldw = per_row * 16L;
-    }
+    const int per_row = (K + 15) / 16;
+    char* at = (char*)workspace_dev + align_up(p.partial_bytes, 256);
+    auto copy = [&](const int8_t* src, long ld, int rows) {
+        const size_t pieces = (size_t)rows * per_row;
+        align_rows_kernel<<<(unsigned)std::min<size_t>((pieces + 255) / 256, 8192), 256, 0, s>>>(src, ld, (u32x4*)at, pieces, per_row, K);
+        const int8_t* to = (const int8_t*)at;
+        at += copy_bytes(rows, K);
+        return to;
+    };
+    if (!a_aligned) { a.A = copy(A_dev, lda, M); a.lda = per_row * 16L; }
+    if (!w_aligned) { a.W = copy(W_dev, ldw, N); a.ldw = per_row * 16L; }
     launch_plan(a, p, workspace_dev, s);
     return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
 }

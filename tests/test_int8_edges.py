@@ -1,12 +1,12 @@
 """The 8-bit integer operators at the edges of their ranges: gates so negative that exp(-gate) leaves fp32, sums written
-over rows that are still to be read.
+over rows that are still to be read, products of one operand that is aligned and one that is not.
 
 The references and tolerances are those of tests/test_int8_ops.py: codes equal the formula's in 64 bits, a scale is one fp32 rounding of it."""
 import pytest
 import torch
 
 import paper_2605_29233_amd as bb
-from test_int8_ops import DEV, TYPES, check_norm, check_swiglu, gen, rnd, strided
+from test_int8_ops import DEV, TYPES, check_gemm, check_norm, check_swiglu, codes, gen, rnd, strided
 
 
 @pytest.mark.gpu
@@ -90,3 +90,28 @@ def test_sums_beside_and_over_their_inputs():
     one = rnd(6, 1, cols, "bf16").to(DEV)
     h = (one.float() * 2).to(torch.bfloat16).cpu()
     check_norm(*bb.rmsnorm_quantize(one, gain.to(DEV), 1e-5, residual=one), h, gain, 1e-5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("odd", ["a", "w", "both"])
+@pytest.mark.parametrize("M,N,K", [(1, 4096, 1040), (5, 130, 257), (120, 512, 8192)])
+def test_only_the_operand_that_is_not_aligned_is_copied(M, N, K, odd):
+    """The workspace past the copy that is needed stays as it was (one row of activations at an odd address leaves the weights where they are)."""
+    from paper_2605_29233_amd.binding import load_library
+    lib = load_library()
+    a, w = codes(M + K, M, K), codes(N + K, N, K)
+    sa, sw = torch.rand(M, generator=gen(1)) * 0.02, torch.rand(N, generator=gen(2)) * 0.001
+    pad = -K % 16 + 16
+    da, dw = (strided(t, pad, int(odd in (name, "both"))) for t, name in ((a, "a"), (w, "w")))
+    dsa, dsw, out = sa.to(DEV), sw.to(DEV), torch.empty(M, N, device=DEV)
+    partial = (lib.bb_gemm_int8_workspace_bytes(M, N, K, 1) + 255) // 256 * 256
+    copy = {"a": M, "w": N}
+    copy = {k: (rows * ((K + 15) // 16 * 16) + 255) // 256 * 256 for k, rows in copy.items()}
+    need = lib.bb_gemm_int8_workspace_bytes(M, N, K, 0)
+    assert need == partial + copy["a"] + copy["w"]
+    ws = torch.full((need,), 0x5A, dtype=torch.uint8, device=DEV)
+    assert lib.bb_gemm_int8(da.data_ptr(), da.stride(0), dsa.data_ptr(), dw.data_ptr(), dw.stride(0), dsw.data_ptr(), None, out.data_ptr(), N, 0, M, N, K, ws.data_ptr(), need,
+                            torch.cuda.current_stream().cuda_stream) == 0
+    check_gemm(out, a, sa, w, sw, None)
+    used = partial + sum(copy.values() if odd == "both" else [copy[odd]])
+    assert (ws[used:] == 0x5A).all() and (ws[partial:used] != 0x5A).any()
