@@ -318,6 +318,15 @@ int bb_gemm_int8(const int8_t* A_dev, long lda, const float* a_scale_dev, const 
                  const float* bias_dev, void* C_dev, long ldc, int c_type, int M, int N, int K, void* workspace_dev,
                  size_t workspace_bytes, void* hip_stream);
 
+/* Tests: the launch that bb_gemm_int8 takes (host only, no device needed): out = {body, tile rows, tile columns, workgroups per CU, k split}.  The bodies are
+ * numbered from 0. */
+int bb_debug_gemm_int8_plan(int M, int N, int K, int out[5]);
+/* Tests: the product of fp32 results by a body and k split of the caller's choice, over the first *live_dev rows (NULL: all M) as inside a forward.  Rows of A and W
+ * 16-byte aligned, at distance ld; at least tiles * split * tile size * 4 bytes of workspace if split > 1 (BB_ENOMEM). */
+int bb_debug_gemm_int8(const int8_t* A_dev, const float* a_scale_dev, const int8_t* W_dev, const float* w_scale_dev, long ld, float* C_dev,
+                       int M, int N, int K, int body, int split, const int* live_dev, void* workspace_dev, size_t workspace_bytes,
+                       void* hip_stream);
+
 /* Tests: on != 0 makes every later forward also store the fp32 logits of the rows that receive them (view's
  * logits_dev); off (the default) the logits exist only in the registers of the LM-head GEMM. */
 int bb_debug_keep_logits(bb_ctx* ctx, int on);

@@ -475,3 +475,26 @@ extern "C" int bb_gemm_int8(const int8_t* A_dev, long lda, const float* a_scale_
     launch_plan(a, p, workspace_dev, s);
     return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
 }
+
+// ---- tests ------------------------------------------------------------------------------------------------------------------------------------
+extern "C" int bb_debug_gemm_int8_plan(int M, int N, int K, int out[5]) {
+    if (!out || !sizes_ok(M, N, K) || M == 0 || N == 0 || K < 16) return BB_EINVAL;
+    const Int8Plan p = int8_plan(M, N, K);
+    const Int8Body& b = i8_bodies[p.body];
+    out[0] = p.body; out[1] = b.bm; out[2] = b.bn; out[3] = b.per_cu; out[4] = p.split;
+    return BB_OK;
+}
+
+extern "C" int bb_debug_gemm_int8(const int8_t* A_dev, const float* a_scale_dev, const int8_t* W_dev, const float* w_scale_dev, long ld, float* C_dev, int M, int N, int K,
+                                  int body, int split, const int* live_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    const int n_bodies = (int)(sizeof(i8_bodies) / sizeof(i8_bodies[0]));
+    if (!A_dev || !a_scale_dev || !W_dev || !w_scale_dev || !C_dev || !sizes_ok(M, N, K) || M == 0 || N == 0 || K < 16 || (uintptr_t)A_dev % 16 || (uintptr_t)W_dev % 16 ||
+        ld % 16 || ld < K || ld > 1 << 23 || body < 0 || body >= n_bodies || split < 1 || split > 16 || split > (K + 127) / 128) return BB_EINVAL;
+    const Int8Body& b = i8_bodies[body];
+    const size_t tiles = ((size_t)M + b.bm - 1) / b.bm * (((size_t)N + b.bn - 1) / b.bn), partial = split > 1 ? tiles * split * b.bm * b.bn * 4 : 0;
+    if (partial > workspace_bytes || tiles * split > 1u << 30) return BB_ENOMEM;
+    if (partial > 0 && (!workspace_dev || (uintptr_t)workspace_dev % 16)) return BB_EINVAL;
+    GemmInt8Args a{A_dev, W_dev, a_scale_dev, w_scale_dev, nullptr, C_dev, ld, ld, N, M, N, K, BB_F32, live_dev};
+    launch_plan(a, Int8Plan{body, split, partial}, workspace_dev, (hipStream_t)hip_stream);
+    return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
+}
