@@ -327,6 +327,12 @@ int bb_debug_gemm_int8(const int8_t* A_dev, const float* a_scale_dev, const int8
                        int M, int N, int K, int body, int split, const int* live_dev, void* workspace_dev, size_t workspace_bytes,
                        void* hip_stream);
 
+/* Tests: rows of fp32 packed into a panel of two bf16 terms, as attention leaves them for the output projection, and the int8 codes and scales that the int8
+ * layers make of it, of the first *live_dev rows (NULL: all).  cols a multiple of 16; q_dev [rows][cols]; panel_dev: 16-byte aligned, 4 bytes for every element of
+ * the rows rounded up to 32 and the columns to 64 (BB_ENOMEM). */
+int bb_debug_panel_quantize(const float* x_dev, int rows, int cols, void* panel_dev, size_t panel_bytes, int8_t* q_dev, float* scale_dev,
+                            const int* live_dev, void* hip_stream);
+
 /* Tests: on != 0 makes every later forward also store the fp32 logits of the rows that receive them (view's
  * logits_dev); off (the default) the logits exist only in the registers of the LM-head GEMM. */
 int bb_debug_keep_logits(bb_ctx* ctx, int on);

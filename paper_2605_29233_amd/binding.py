@@ -66,7 +66,7 @@ EXPORTS = ("bb_workspace_bytes", "bb_create", "bb_destroy", "bb_last_error", "bb
            "bb_request_close", "bb_refresh", "bb_denoise_step", "bb_merge_commit", "bb_get_tokens", "bb_get_stats",
            "bb_get_view", "bb_set_state", "bb_get_kv", "bb_set_kv", "bb_read_device", "bb_synchronize", "bb_debug_gemm", "bb_debug_gemm_wide", "bb_debug_wide_format", "bb_profile_enable", "bb_profile_read", "bb_debug_set_gemm_plan", "bb_debug_gemm_plan", "bb_debug_attention_plan", "bb_debug_copy16", "bb_generate", "bb_kv_diag_scratch_bytes", "bb_kv_diagnostics", "bb_gemm_static", "bb_debug_mfma_rate", "bb_debug_keep_logits",
            "bb_quantize_rows", "bb_rmsnorm_quantize", "bb_swiglu_quantize", "bb_gemm_int8", "bb_gemm_int8_workspace_bytes", "bb_int8_layers", "bb_int8_layers_bytes",
-           "bb_debug_gemm_int8_plan", "bb_debug_gemm_int8")
+           "bb_debug_gemm_int8_plan", "bb_debug_gemm_int8", "bb_debug_panel_quantize")
 KERNEL_CLASSES = ("gemm_skinny", "gemm_wide", "attention", "glue", "policy")
 
 
@@ -128,6 +128,7 @@ def load_library():
         lib.bb_gemm_int8_workspace_bytes.restype = C.c_size_t
         lib.bb_debug_gemm_int8_plan.argtypes = [i32, i32, i32, C.POINTER(i32)]
         lib.bb_debug_gemm_int8.argtypes = [ptr, ptr, ptr, ptr, i64, ptr, i32, i32, i32, i32, i32, ptr, ptr, C.c_size_t, ptr]
+        lib.bb_debug_panel_quantize.argtypes = [ptr, i32, i32, ptr, C.c_size_t, ptr, ptr, ptr, ptr]
         lib.bb_int8_layers_bytes.argtypes = [ptr]
         lib.bb_int8_layers_bytes.restype = C.c_size_t
         lib.bb_int8_layers.argtypes = [ptr, ptr, C.c_size_t]

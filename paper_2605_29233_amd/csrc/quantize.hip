@@ -149,7 +149,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
             if constexpr (TOP_IN_DOUBLE) top2 = fmax(top2, fabs((double)f * (double)w));
         }
         if constexpr (OP == QOP_SWIGLU) y = far ? silu_far(f, w) : silu(f) * w;
-        if constexpr (OP == QOP_PANEL) y = f + w;           // (exact: 16 bits and the sign)
+        if constexpr (OP == QOP_PANEL) y = f + w;           // (exact: store_panel8 splits an fp32 value, both terms are multiples of its last place and no larger)
         top_bits = max(top_bits, __float_as_uint(y) & 0x7FFFFFFFu);
         return y;
     };
@@ -460,4 +460,15 @@ extern "C" int bb_swiglu_quantize(const void* gate_dev, long ldg, const void* up
     QuantArgs a{};
     a.x = gate_dev; a.ldx = ldg; a.x2 = up_dev; a.ldx2 = ldu; a.q = q_dev; a.ldq = ldq; a.scale = scale_dev; a.rows = rows; a.cols = cols;
     return quantize<QOP_SWIGLU>(type, a, (hipStream_t)hip_stream);
+}
+
+// ---- tests ------------------------------------------------------------------------------------------------------------------------------------
+extern "C" int bb_debug_panel_quantize(const float* x_dev, int rows, int cols, void* panel_dev, size_t panel_bytes, int8_t* q_dev, float* scale_dev, const int* live_dev,
+                                       void* hip_stream) {
+    if (!x_dev || !panel_dev || !q_dev || !scale_dev || rows < 1 || rows > 1 << 20 || cols < 16 || cols > 1 << 20 || cols % 16 || (uintptr_t)panel_dev % 16) return BB_EINVAL;
+    const int mt = (rows + 31) / 32;
+    if (panel_bytes < (size_t)mt * 32 * ((cols + 63) / 64 * 64) * 2 * BB_SPLIT) return BB_ENOMEM;
+    launch_pack_rows(x_dev, rows, cols, (u32x4*)panel_dev, mt, (hipStream_t)hip_stream);
+    launch_panel_quantize((const u32x4*)panel_dev, mt, q_dev, cols, scale_dev, rows, cols, live_dev, (hipStream_t)hip_stream);
+    return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
 }
