@@ -1,6 +1,7 @@
-"""The int8 layers at the edges: shapes whose sums would not be exact, codes that a captured forward has yet to make, and attention's output on its way
-into the output projection."""
+"""The int8 layers at the edges: shapes whose sums would not be exact, codes that a captured forward has yet to make, attention's output on its way into the output
+projection, and fewer live rows than a forward is sized for."""
 import ctypes as C
+import types
 
 import numpy as np
 import pytest
@@ -8,7 +9,7 @@ import torch
 
 import paper_2605_29233_amd as pkg
 from paper_2605_29233_amd import BB_INIT, BBError, BlockBatch, Limits
-from paper_2605_29233_amd.binding import load_library
+from paper_2605_29233_amd.binding import gemm_int8_plan, load_library
 from test_int8_ops import check_codes, gen
 from workload import gen_prompt, gen_weights
 from workload.configs import TINY, DecodeParams, ModelShape
@@ -181,4 +182,41 @@ def test_attention_output_through_its_codes_into_the_output_projection():
     for row, gbr in zip(got, branch):
         y, tol, _ = expected(ids[gbr // len(blocks)], int(gbr % len(blocks)))
         assert ((row[:d] - y).abs() <= tol).all(), ((row[:d] - y).abs() / tol).max()
+    bb.close()
+
+
+@pytest.mark.parametrize("d_ffn", [8192, 688])
+def test_fewer_live_rows_give_the_rows_that_are_left_their_results(d_ffn):
+    """A step sized for 288 rows of which some branches have finished: the rows of the others keep their logits bit for bit, although they lie elsewhere in the products, whose tiles
+    and k splits (twelve of the down projection with d_ffn 8192) are those of 288 rows."""
+    model = ModelShape("int8live", 2, 256, 4, 2, 64, d_ffn, 512)
+    blocks, gen_len, prompt_len = (32, 96, 160), 160, 24
+    if d_ffn == 8192:
+        assert gemm_int8_plan(288, 256, 8192)["split"] > 1 and gemm_int8_plan(288, 256, 8192)["bm"] < 288
+    bb = BlockBatch(model, DecodeParams(), Limits(1, 3, prompt_len + gen_len, gen_len, sum(blocks)), poison_workspace=True)
+    bb.load_weights(gen_weights(model, 31))
+    bb.keep_logits(True)
+    bb.int8_layers()
+    bb._i8.fill_(0x5A)
+    torch.cuda.synchronize()
+    rid = bb.request_open(gen_prompt(model, 31, 0, prompt_len), gen_len, blocks)
+    bb.refresh([rid], BB_INIT)
+    X = bb.get_tokens(rid)
+    X[:, prompt_len::3] = np.arange(len(X[0, prompt_len::3])) % 500             # some rows of every window are decoded already
+    every = None
+    for done in ((), (0,), (1,), (2,), (0, 1), (1, 2), (0, 2), (0, 1, 2), ()):
+        bb.set_state(rid, X, [types.SimpleNamespace(start=prompt_len, end=prompt_len + b, done=k in done, mean_conf=0.5) for k, b in enumerate(blocks)])
+        print("finished:", done, flush=True)
+        view = bb.denoise_step([rid])
+        assert view.m_q == sum(b for k, b in enumerate(blocks) if k not in done)
+        if view.m_lm == 0:
+            assert len(done) == 3
+            continue
+        gbr, pos = view.rows()
+        at = view.lm_rows()
+        rows = {(int(gbr[m]), int(pos[m])): logits for m, logits in zip(at, view.logits())}
+        every = every or rows
+        assert len(rows) == sum(g not in done for g, _ in every)
+        for key, logits in rows.items():
+            assert np.array_equal(logits, every[key]), (done, key)
     bb.close()
