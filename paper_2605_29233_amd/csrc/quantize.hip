@@ -192,7 +192,8 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
         }
     } else
         for (int g = t; g < groups; g += THREADS) { fetch(0, g, false); values(0, g, false, near); }
-    // Gates below SILU_FAR are rare: they are only noticed above, and a wave that met one reads its groups again.
+    // Gates below SILU_FAR are rare: they are only noticed above, and a wave that met one reads its groups again
+    // (6143 x 12288 bf16 75 us without any, 125 with some in every row).
     bool careful = false;
     if constexpr (OP == QOP_SWIGLU) {
         careful = __any(low_bits > SILU_FAR_BITS);
@@ -258,7 +259,9 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void quantize_kernel
             b |= !(y < INFINITY);
             d = fmax(d, y);
         };
-        for (int g = t; g < groups; g += THREADS)
+        // (a row of zeros as gates, which pads a batch, is nothing but zeros: 70 us for 6143 x 12288 of them, 177 with a look at each)
+        const bool zeros = OP == QOP_SWIGLU && top_bits == 0u && low_bits == 0u;
+        for (int g = zeros ? groups : t; g < groups; g += THREADS)
 #pragma unroll 1
             for (int j = 0; j < 8; ++j) look(g * 8 + j);
         if (tail) look(c_tail);
