@@ -266,7 +266,7 @@ int bb_gemm_static(const float* A_dev, const uint16_t* W_dev, float* C_dev, int 
 
 /* Layer GEMMs in 8-bit integers: from the next forward on every layer's projections run as int8 products (bb_gemm_int8
  * below) of rows quantised per token, where they are made (norm, attention, SwiGLU), with weights quantised per output
- * channel; embeddings, norms, attention, K,V and the LM head stay as they are.  A block step then streams a byte per weight instead of two.
+ * channel; embeddings, norms, attention, K,V and the LM head stay as they are.  A block step then streams a byte per weight instead of two.  (The other formats' copies stay in the workspace.)
  * mem_dev: device memory of at least bb_int8_layers_bytes(ctx), 256-byte aligned, which the context uses until it is destroyed or the
  * call is made again (mem_dev == NULL: the format is switched off); a call that takes memory away waits for the stream first.  The codes are made from the loaded weights by
  * the next forward, and again after bb_load_weights (one that is captured into a graph makes them at every replay).  The tuning knobs of the other formats (bb_debug_set_gemm_plan,
@@ -295,12 +295,12 @@ int bb_quantize_rows(const void* x_dev, long ldx, int8_t* q_dev, long ldq, float
 
 /* h = x + residual, rounded to `type` and stored in residual_out (may be residual or x themselves, with their ld; BB_EINVAL if it overlaps them otherwise); then the rows of
  * y = h / sqrt(mean_c h^2 + eps) * gain quantised as above, y unrounded.  Without a residual (both residual pointers NULL) h = x.
- * gain: [cols]; x, residual, residual_out, gain of the same type.  eps >= 0. */
+ * gain: [cols]; x, residual, residual_out, gain of the same type.  eps >= 0 (a row of zeros stays one at eps = 0). */
 int bb_rmsnorm_quantize(const void* x_dev, long ldx, const void* residual_dev, long ldr, void* residual_out_dev, long ldo,
                         const void* gain_dev, float eps, int8_t* q_dev, long ldq, float* scale_dev, long rows, int cols, int type,
                         void* hip_stream);
 
-/* The rows of y = gate / (1 + exp(-gate)) * up (fp32, unrounded) quantised as above; gate and up of the same type. */
+/* The rows of y = gate / (1 + exp(-gate)) * up (unrounded) quantised as above; gate and up of the same type. */
 int bb_swiglu_quantize(const void* gate_dev, long ldg, const void* up_dev, long ldu, int8_t* q_dev, long ldq, float* scale_dev,
                        long rows, int cols, int type, void* hip_stream);
 

@@ -11,8 +11,8 @@
 // with the LDS reads 3.6-3.8; with the loads too 2.9 in the loop over k of a 256 x 256 tile (64 KB per CU and chunk of 128 k, 1.36 us, of 47 KB/us; the
 // matrix pipes are busy 0.67 of the time at 1.88 GHz), and 2.4 over 8192 x 8192 x 8192 (459 us) and 8192 x 24576 x 4096 (0.68 ms), with the
 // tiles' ends.  Loads by 64-byte runs reach half the rate of whole lines (66 against 130 KB/us and CU from an L2): hence chunks of 128 k, and
-// rows at multiples of 128 bytes are fastest (1402 x 4610 rows of 3592 k 41 us, of 3584 34).  Few rows: the stream of W, 5.4 TB/s of 100 MB
-// at one row; between them (120 rows, 50 MB) 14 us beside 5 us that join four splits of k.
+// rows at multiples of 128 bytes are fastest (1402 x 4610 rows of 3592 k 41 us, of 3584 34).  Few rows: the stream of W, 19.3 us of 101 MB
+// at one row (5.2 TB/s, partly out of the cache behind the L2s); between them (120 rows, 50 MB) 14 us beside 4 us that join four splits of k.
 #include "bb_internal.h"
 #include "lds.h"
 #include "sched.h"
@@ -372,7 +372,8 @@ template <int R, int T, int WM, int NS, int PER_CU> static void launch_tiled(con
 // those (chunk), per chunk and workgroup that shares a CU (shared); per join (join) and MB of partial sums (per_mb).  Fitted to launches of
 // 18 row counts from 1 to 8192 x 11 matrices from 256 x 688 to 37888 x 3584 x k splits; there the choice is on average 1 % slower than the best
 // of these bodies and splits, at worst 26 %, and where all weights come from memory (640 MB of them in turn, 13 row counts up to 1024) 1 and
-// 16 %.  The second 128 x 128, one workgroup a CU and a chunk more in flight than the first's two each, is for such weights when no CU has a
+// 16 %.  (What it chooses by, not a forecast: inside a forward, where weights and rows are cold, QKV and gate/up of 120 rows take 22 and 36 us where
+// it says 14 and 22.)  The second 128 x 128, one workgroup a CU and a chunk more in flight than the first's two each, is for such weights when no CU has a
 // second tile: bf16 results of 192 rows by 12288 x 4096 23.4 us (30.9 with the first, 27.8 the best without it), 120 by 24576 x 4096 30.1
 // (34.6); with more tiles two workgroups that overlap win: 1024 by 37888 x 3584 166 (182).
 struct Int8Body { int bm, bn, per_cu; float start, round, chunk, shared, join, per_mb; };
@@ -391,7 +392,8 @@ static Int8Plan int8_plan(int M, int N, int K, size_t most = I8_MAX_PARTIAL) {
     Int8Plan best{0, 1, 0};
     float best_cost = INFINITY;
     const int chunks = (K + 127) / 128;
-    const float stream = ((float)N * K + (float)M * K + 2.0f * (float)M * N) / 7.1e6f;      // us that the memory takes
+    // us that the memory takes, at a fitted rate: of the fitted launches' weights a part lay in the cache behind the L2s, and a copy reaches 5.1
+    const float stream = ((float)N * K + (float)M * K + 2.0f * (float)M * N) / 7.1e6f;
     for (int i = 0; i < (int)(sizeof(i8_bodies) / sizeof(i8_bodies[0])); ++i) {
         const Int8Body& b = i8_bodies[i];
         const size_t tiles = ((size_t)M + b.bm - 1) / b.bm * (((size_t)N + b.bn - 1) / b.bn);

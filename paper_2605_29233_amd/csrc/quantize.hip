@@ -9,8 +9,8 @@
 // maximum is 63.5) is seen as one.  So is the maximum itself where fp32 does not hold it.  Sums of squares are in double.
 //
 // What bounds it: memory.  A row is read once and its values stay in registers between the maximum and the codes.  Read + written, bf16: rows of
-// 24576 x 4096 55 us (5.5 TB/s), norm with residual of 20480 x 4096 102 (5.7), SwiGLU of 6143 x 12288 83 (4.6: its exponentials beside the loads);
-// a large copy reaches 5.1.  One row of 4096: 3.1, 3.9 and 4.2 us, an empty launch 2.5.
+// 24576 x 4096 53 us (5.7 TB/s), norm with residual of 20480 x 4096 100 (5.9), SwiGLU of 6143 x 12288 76 (5.0: its exponentials beside the loads);
+// a large copy reaches 5.1.  One row of 4096: 2.3, 3.0 and 3.4 us; a fill of one value 1.2.
 #include "bb_internal.h"
 #include <algorithm>
 #include <cstdlib>
