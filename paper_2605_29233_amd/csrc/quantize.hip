@@ -400,16 +400,28 @@ static bool refuse_out(const void* q, long ldq, const void* scale, long rows, in
 static bool refuse_rows(const void* p, int type, long rows, long ld) {
     return !p || (uintptr_t)p % (type == BB_F32 ? 4 : 2) || (rows > 1 && ld < 0);
 }
-// Rows that are written (w, ldw >= cols) while others (r) are read: right where they are the same rows or have no element in common.  Two matrices of one row
-// distance may interleave (column ranges of one tensor); of different ones whose extents overlap, it counts as overlap.
+// Rows that are written (w, ldw >= cols) while others (r) are read: right where they are the same rows, or have no element in common (apart, or between each
+// other: column ranges or alternate rows of one tensor).
 static bool refuse_overlap(const void* r, long ldr, const void* w, long ldw, long rows, int cols, int type) {
-    const long size = type == BB_F32 ? 4 : 2, r0 = (long)(uintptr_t)r, w0 = (long)(uintptr_t)w;
+    const long size = type == BB_F32 ? 4 : 2, n = cols * size, r0 = (long)(uintptr_t)r, w0 = (long)(uintptr_t)w;
     if (rows == 1) ldr = ldw = cols;
     if (r0 == w0 && ldr == ldw) return false;
-    const long r1 = r0 + ((rows - 1) * ldr + cols) * size, w1 = w0 + ((rows - 1) * ldw + cols) * size;
+    ldr *= size; ldw *= size;
+    const long r1 = r0 + (rows - 1) * ldr + n, w1 = w0 + (rows - 1) * ldw + n;
     if (r1 <= w0 || w1 <= r0) return false;
-    const long apart = labs(r0 - w0) % (ldw * size);
-    return ldr != ldw || apart < cols * size || ldw * size - apart < cols * size;
+    if (ldr == ldw) {                                       // (how far a row is from the next one before it)
+        const long apart = labs(r0 - w0) % ldw;
+        return apart < n || ldw - apart < n;
+    }
+    if (ldr <= n) {                                         // rows without gaps: a single run
+        const long i = std::max(0L, (r0 - w0) / ldw);       // the last row of w that begins at or before it, or the first
+        return (w0 + i * ldw < r1 && w0 + i * ldw + n > r0) || (i + 1 < rows && w0 + (i + 1) * ldw < r1);
+    }
+    for (long i = 0; i < rows; ++i) {
+        const long at = w0 + i * ldw, j = at < r0 ? 0 : std::min(rows - 1, (at - r0) / ldr);
+        if ((r0 + j * ldr < at + n && at < r0 + j * ldr + n) || (j + 1 < rows && r0 + (j + 1) * ldr < at + n)) return true;
+    }
+    return false;
 }
 
 // The layers of a forward: fp32 rows, of which *live count.

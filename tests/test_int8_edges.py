@@ -115,3 +115,18 @@ def test_only_the_operand_that_is_not_aligned_is_copied(M, N, K, odd):
     check_gemm(out, a, sa, w, sw, None)
     used = partial + sum(copy.values() if odd == "both" else [copy[odd]])
     assert (ws[used:] == 0x5A).all() and (ws[partial:used] != 0x5A).any()
+
+
+@pytest.mark.gpu
+def test_sums_between_rows_of_another_distance():
+    """Every other row of a tensor written, every fourth one between them read."""
+    rows, cols = 9, 40
+    base, gain = torch.randn(4 * rows, cols, generator=gen(90)), rnd(91, 1, cols, "fp32")[0]
+    d = base.to(DEV)
+    x, r, out = base[1::4], rnd(92, rows, cols, "fp32"), d[:2 * rows:2]
+    q, s = bb.rmsnorm_quantize(d[1::4], gain.to(DEV), 1e-5, residual=r.to(DEV), residual_out=out)
+    check_norm(q, s, x + r, gain, 1e-5)
+    base[:2 * rows:2] = x + r
+    assert torch.equal(d.cpu(), base)
+    with pytest.raises(bb.BBError):
+        bb.rmsnorm_quantize(d[::4], gain.to(DEV), 1e-5, residual=r.to(DEV), residual_out=out)
