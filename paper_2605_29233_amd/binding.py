@@ -66,6 +66,7 @@ EXPORTS = ("bb_workspace_bytes", "bb_create", "bb_destroy", "bb_last_error", "bb
            "bb_request_close", "bb_refresh", "bb_denoise_step", "bb_merge_commit", "bb_get_tokens", "bb_get_stats",
            "bb_get_view", "bb_set_state", "bb_get_kv", "bb_set_kv", "bb_read_device", "bb_synchronize", "bb_debug_gemm", "bb_debug_gemm_wide", "bb_debug_wide_format", "bb_profile_enable", "bb_profile_read", "bb_debug_set_gemm_plan", "bb_debug_gemm_plan", "bb_debug_attention_plan", "bb_debug_copy16", "bb_generate", "bb_kv_diag_scratch_bytes", "bb_kv_diagnostics", "bb_gemm_static", "bb_debug_mfma_rate", "bb_debug_keep_logits",
            "bb_quantize_rows", "bb_rmsnorm_quantize", "bb_swiglu_quantize", "bb_gemm_int8", "bb_gemm_int8_workspace_bytes", "bb_int8_layers", "bb_int8_layers_bytes",
+           "bb_rope_frequencies", "bb_rope", "bb_rope_append", "bb_attention_workspace_bytes", "bb_attention", "bb_shared_attention_workspace_bytes", "bb_shared_attention",
            "bb_debug_gemm_int8_plan", "bb_debug_gemm_int8", "bb_debug_panel_quantize")
 KERNEL_CLASSES = ("gemm_skinny", "gemm_wide", "attention", "glue", "policy")
 
@@ -126,6 +127,19 @@ def load_library():
         lib.bb_gemm_int8.argtypes = [ptr, i64, ptr, ptr, i64, ptr, ptr, ptr, i64, i32, i32, i32, i32, ptr, C.c_size_t, ptr]
         lib.bb_gemm_int8_workspace_bytes.argtypes = [i32, i32, i32, i32]
         lib.bb_gemm_int8_workspace_bytes.restype = C.c_size_t
+        f64, f32, size = C.c_double, C.c_float, C.c_size_t
+        rows = [ptr, i64, i64]                                  # data, strides between tokens and heads
+        pages = [ptr, i64, i64, i64]                            # data, strides between pages, heads and tokens
+        lib.bb_rope_frequencies.argtypes = [ptr, i32, f64, f64, f64, f64, f64]
+        lib.bb_rope.argtypes = [*rows, *rows, i32, *rows, *rows, i32, ptr, ptr, i32, i32, f32, i64, i32, i32, ptr]
+        lib.bb_rope_append.argtypes = [*rows, *rows, i32, *rows, *rows, i32, ptr, ptr, i32, i32, f32, ptr, *pages, *pages, i32, i64, i32, i32, ptr]
+        lib.bb_attention_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32]
+        lib.bb_attention_workspace_bytes.restype = size
+        lib.bb_attention.argtypes = [*rows, *rows, *rows, ptr, ptr, i32, i64, i64, i32, i32, i32, i32, i32, f32, *rows, ptr, ptr, size, ptr]
+        lib.bb_shared_attention_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32, i32, i32]
+        lib.bb_shared_attention_workspace_bytes.restype = size
+        lib.bb_shared_attention.argtypes = [*rows, ptr, i32, i64, *pages, *pages, i32, ptr, i64, i32, ptr, ptr, i64, i32, ptr, ptr, i32, i32, i32, i32, i32, i32, f32,
+                                            *rows, ptr, ptr, size, ptr]
         lib.bb_debug_gemm_int8_plan.argtypes = [i32, i32, i32, C.POINTER(i32)]
         lib.bb_debug_gemm_int8.argtypes = [ptr, ptr, ptr, ptr, i64, ptr, i32, i32, i32, i32, i32, ptr, ptr, C.c_size_t, ptr]
         lib.bb_debug_panel_quantize.argtypes = [ptr, i32, i32, ptr, C.c_size_t, ptr, ptr, ptr, ptr]
@@ -172,16 +186,16 @@ def gemm_int8_plan(M, N, K):
 # ---- 8-bit integer operators --------------------------------------------------------------------
 # (what these calls do on the host counts where a kernel takes a few microseconds: no objects made, nothing looked up twice)
 _TYPES = {}             # torch dtype -> BB_F32, BB_BF16, BB_F16
-_torch = _here = _raw_stream = _I8 = _F32 = None
+_torch = _here = _raw_stream = _I8 = _I32 = _F32 = _F64 = None
 
 
 def _ready():
     """What the calls below use of torch (imported with the first of them)."""
-    global _torch, _here, _raw_stream, _I8, _F32
+    global _torch, _here, _raw_stream, _I8, _I32, _F32, _F64
     import torch
     load_library()
     _TYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
-    _I8, _F32, _here = torch.int8, torch.float32, torch.cuda.current_device
+    _I8, _I32, _F32, _F64, _here = torch.int8, torch.int32, torch.float32, torch.float64, torch.cuda.current_device
     _raw_stream = torch._C._cuda_getCurrentRawStream        # (torch.cuda.current_stream without its 2 us)
     _torch = torch
 
@@ -326,6 +340,200 @@ def gemm_int8(a, a_scale, w, w_scale, bias=None, out=None, dtype=None, stream=No
     if rc:
         _done(rc, "bb_gemm_int8")
     return out
+
+
+# ---- operators around K,V ------------------------------------------------------------------------
+PAGE_TOKENS = 64
+
+
+def rope_frequencies(rot, base=10000.0, factor=1.0, context=0, low=1.0, high=4.0, device="cuda:0"):
+    """bb_rope_frequencies as a tensor of `device`: fp64 [rot / 2], base^(-2 j / rot), scaled for contexts `factor` times as long: all divided by it, or, of a
+    model trained on `context` tokens, those that turn at most `low` times over it, those that turn `high` times or more not at all."""
+    import torch
+    if rot < 2 or rot % 2:
+        raise BBError(f"rot: expected an even number of elements, at least 2, got {rot}")
+    f = torch.empty(rot // 2, dtype=torch.float64)
+    rc = load_library().bb_rope_frequencies(f.data_ptr(), int(rot), float(base), float(factor), float(context), float(low), float(high))
+    if rc:
+        _done(rc, "bb_rope_frequencies")
+    return f.to(device)
+
+
+def _heads(t, what, dtype, tokens, heads, dim, device):
+    """Address and strides (between tokens, between heads) of rows of heads [tokens][heads][dim]."""
+    if t.dtype is not dtype or t.shape != (tokens, heads, dim) or t.device != device:
+        raise BBError(f"{what}: expected {dtype} {(tokens, heads, dim)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    ts, hs, step = t.stride()
+    if step != 1 and dim > 1:
+        raise BBError(f"{what}: the elements of a head must be contiguous")
+    return t.data_ptr(), ts, hs
+
+
+def _cache(t, what, dtype, pages, heads, dim, device):
+    """Address and strides (between pages, heads, tokens) of a cache [pages][heads][PAGE_TOKENS][dim]."""
+    if t.dtype is not dtype or t.shape != (pages, heads, PAGE_TOKENS, dim) or t.device != device:
+        raise BBError(f"{what}: expected {dtype} {(pages, heads, PAGE_TOKENS, dim)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    ps, hs, ts, step = t.stride()
+    if step != 1 and dim > 1:
+        raise BBError(f"{what}: the elements of a head must be contiguous")
+    return t.data_ptr(), ps, hs, ts
+
+
+def _table(t, what, rows, device):
+    """Address, row distance and columns of a table of pages [rows][columns]."""
+    if t.dtype is not _I32 or t.dim() != 2 or t.shape[0] != rows or t.device != device:
+        raise BBError(f"{what}: expected torch.int32 ({rows}, pages) on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    ld, step = t.stride()
+    if step != 1 and t.shape[1] > 1:
+        raise BBError(f"{what}: the pages of a row must be contiguous")
+    return t.data_ptr(), ld, t.shape[1]
+
+
+def _starts(t, what, device):
+    """Address and number of ranges of starts [ranges + 1]."""
+    if t.dtype is not _I32 or t.dim() != 1 or t.shape[0] < 1 or t.device != device or (t.shape[0] > 1 and t.stride(0) != 1):
+        raise BBError(f"{what}: expected contiguous torch.int32 (ranges + 1,) on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr(), t.shape[0] - 1
+
+
+def _three(t, what):
+    if t.dim() != 3:
+        raise BBError(f"{what}: expected [tokens][heads][head_dim], got {tuple(t.shape)}")
+    return t.shape
+
+
+def rope(q, k, positions, freqs, interleaved=False, magnitude=1.0, q_out=None, k_out=None, stream=None):
+    """bb_rope on torch CUDA tensors: q [tokens][heads][dim] and k [tokens][kv heads][dim] (None: no keys) fp32, bf16 or fp16 turned by positions (int32 [tokens]) *
+    freqs (fp64 [rot / 2], see rope_frequencies; the heads' first rot elements); written to q_out and k_out (default: in place).  Returns (q_out, k_out).
+    Stream as in quantize_rows."""
+    if _torch is None:
+        _ready()
+    dev, dtype = q.device, q.dtype
+    if stream is not None or dev.index is None or dev.index != _here():
+        return _elsewhere(dev, stream, lambda: rope(q, k, positions, freqs, interleaved, magnitude, q_out, k_out))
+    tokens, heads, dim = _three(q, "q")
+    t = _type(dtype, "q")
+    if q_out is None:
+        q_out = q
+    kv_heads, ks, kos = 0, (None, 0, 0), (None, 0, 0)
+    if k is not None:
+        kv_heads = _three(k, "k")[1]
+        if k_out is None:
+            k_out = k
+        ks, kos = _heads(k, "k", dtype, tokens, kv_heads, dim, dev), _heads(k_out, "k_out", dtype, tokens, kv_heads, dim, dev)
+    elif k_out is not None:
+        raise BBError("k_out without k")
+    rot = 2 * freqs.shape[0] if freqs.dim() else 0
+    rc = _LIB.bb_rope(*_heads(q, "q", dtype, tokens, heads, dim, dev), *_heads(q_out, "q_out", dtype, tokens, heads, dim, dev), heads, *ks, *kos, kv_heads,
+                      _vec(positions, "positions", _I32, tokens, dev), _vec(freqs, "freqs", _F64, rot // 2, dev), rot, interleaved, magnitude, tokens, dim, t,
+                      _raw_stream(dev.index))
+    if rc:
+        _done(rc, "bb_rope")
+    return q_out, k_out
+
+
+def rope_append(q, k, v, positions, freqs, k_cache, v_cache, slots, interleaved=False, magnitude=1.0, q_out=None, stream=None):
+    """bb_rope_append: q turned into q_out (default: in place) as by rope, the turned k and v written to k_cache and v_cache [pages][kv heads][PAGE_TOKENS][dim] at
+    slots (int32 [tokens], page * PAGE_TOKENS + token in the page; a negative one keeps its token out).  Returns q_out.  Stream as in quantize_rows."""
+    if _torch is None:
+        _ready()
+    dev, dtype = q.device, q.dtype
+    if stream is not None or dev.index is None or dev.index != _here():
+        return _elsewhere(dev, stream, lambda: rope_append(q, k, v, positions, freqs, k_cache, v_cache, slots, interleaved, magnitude, q_out))
+    tokens, heads, dim = _three(q, "q")
+    kv_heads, t = _three(k, "k")[1], _type(dtype, "q")
+    if q_out is None:
+        q_out = q
+    pages = k_cache.shape[0] if k_cache.dim() else 0
+    rot = 2 * freqs.shape[0] if freqs.dim() else 0
+    rc = _LIB.bb_rope_append(*_heads(q, "q", dtype, tokens, heads, dim, dev), *_heads(q_out, "q_out", dtype, tokens, heads, dim, dev), heads,
+                             *_heads(k, "k", dtype, tokens, kv_heads, dim, dev), *_heads(v, "v", dtype, tokens, kv_heads, dim, dev), kv_heads,
+                             _vec(positions, "positions", _I32, tokens, dev), _vec(freqs, "freqs", _F64, rot // 2, dev), rot, interleaved, magnitude,
+                             _vec(slots, "slots", _I32, tokens, dev), *_cache(k_cache, "k_cache", dtype, pages, kv_heads, dim, dev),
+                             *_cache(v_cache, "v_cache", dtype, pages, kv_heads, dim, dev), pages, tokens, dim, t, _raw_stream(dev.index))
+    if rc:
+        _done(rc, "bb_rope_append")
+    return q_out
+
+
+def _attention_outputs(q, out, lse, scale):
+    """Sizes of q, the outputs made where not given, and the scale."""
+    tokens, heads, dim = _three(q, "q")
+    if out is None:
+        out = _torch.empty(tokens, heads, dim, dtype=q.dtype, device=q.device)
+    pl = None
+    if lse is not None:
+        if lse.dtype is not _F32 or lse.shape != (tokens, heads) or lse.device != q.device or not lse.is_contiguous():
+            raise BBError(f"lse: expected contiguous torch.float32 {(tokens, heads)} on {q.device}, got {lse.dtype} {tuple(lse.shape)} on {lse.device}")
+        pl = lse.data_ptr()
+    return tokens, heads, dim, out, pl, dim ** -0.5 if scale is None else scale
+
+
+def attention(q, k, v, q_starts, k_starts=None, block=0, scale=None, out=None, lse=None, stream=None):
+    """bb_attention on torch CUDA tensors: packed sequences of queries [tokens][heads][dim] on keys and values [tokens][kv heads][dim], bf16 or fp16; sequence s is
+    rows q_starts[s] .. q_starts[s + 1] - 1 of q and k_starts[s] .. (default: the same) of k and v (int32 [sequences + 1]).  block 0: every query sees all its keys, 1: causal, b:
+    keys before the end of its own block of b.  scale: default dim^-0.5.  Written to out [tokens][heads][dim] (made here where not given) and lse (fp32 [tokens][heads], where
+    given); returns out.  Stream as in quantize_rows; a workspace, where the call needs one, is allocated on it for this call alone."""
+    if _torch is None:
+        _ready()
+    dev, dtype = q.device, q.dtype
+    if stream is not None or dev.index is None or dev.index != _here():
+        return _elsewhere(dev, stream, lambda: attention(q, k, v, q_starts, k_starts, block, scale, out, lse))
+    tokens, heads, dim, out, pl, scale = _attention_outputs(q, out, lse, scale)
+    k_tokens, kv_heads, _ = _three(k, "k")
+    qs, n = _starts(q_starts, "q_starts", dev)
+    ks, nk = (qs, n) if k_starts is None else _starts(k_starts, "k_starts", dev)
+    if nk != n:
+        raise BBError(f"q_starts gives {n} sequences, k_starts {nk}")
+    nbytes = _LIB.bb_attention_workspace_bytes(tokens, k_tokens, n, heads, kv_heads, dim)
+    ws = _torch.empty(nbytes, dtype=_torch.uint8, device=dev) if nbytes else None
+    rc = _LIB.bb_attention(*_heads(q, "q", dtype, tokens, heads, dim, dev), *_heads(k, "k", dtype, k_tokens, kv_heads, dim, dev),
+                           *_heads(v, "v", dtype, k_tokens, kv_heads, dim, dev), qs, ks, n, tokens, k_tokens, heads, kv_heads, dim, _type(dtype, "q"), block, scale,
+                           *_heads(out, "out", dtype, tokens, heads, dim, dev), pl, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(dev.index))
+    if rc:
+        _done(rc, "bb_attention")
+    return out
+
+
+def shared_attention(q, q_starts, k_cache, v_cache, own_pages, own_lens, prefix_pages=None, prefix_lens=None, group_starts=None, block=0, scale=None, out=None,
+                     lse=None, stream=None):
+    """bb_shared_attention: queries [tokens][heads][dim] of branches (branch b: rows q_starts[b] .. q_starts[b + 1] - 1) over caches [pages][kv heads][PAGE_TOKENS][dim]:
+    the prefix of the branch's group (branches group_starts[g] .. group_starts[g + 1] - 1; prefix_lens[g] keys in the pages prefix_pages[g]), read once for all of
+    them, and the branch's own_lens[b] keys in the pages own_pages[b].  Tables, lengths and starts are int32 tensors of the device; without a prefix it is plain attention over pages.
+    block, scale, out, lse, stream and workspace as in attention (block counts from the first own key)."""
+    if _torch is None:
+        _ready()
+    dev, dtype = q.device, q.dtype
+    if stream is not None or dev.index is None or dev.index != _here():
+        return _elsewhere(dev, stream, lambda: shared_attention(q, q_starts, k_cache, v_cache, own_pages, own_lens, prefix_pages, prefix_lens, group_starts, block,
+                                                                scale, out, lse))
+    tokens, heads, dim, out, pl, scale = _attention_outputs(q, out, lse, scale)
+    if k_cache.dim() != 4:
+        raise BBError(f"k_cache: expected [pages][kv heads][{PAGE_TOKENS}][head_dim], got {tuple(k_cache.shape)}")
+    pages, kv_heads = k_cache.shape[:2]
+    qs, n = _starts(q_starts, "q_starts", dev)
+    own, own_ld, own_width = _table(own_pages, "own_pages", n, dev)
+    pre, pre_ld, pre_width, pre_lens, gs, groups = None, 0, 0, None, None, 0
+    if group_starts is not None:
+        if prefix_pages is None or prefix_lens is None:
+            raise BBError("group_starts without prefix_pages and prefix_lens")
+        gs, groups = _starts(group_starts, "group_starts", dev)
+        pre, pre_ld, pre_width = _table(prefix_pages, "prefix_pages", groups, dev)
+        pre_lens = _vec(prefix_lens, "prefix_lens", _I32, groups, dev)
+    elif prefix_pages is not None or prefix_lens is not None:
+        raise BBError("prefix_pages or prefix_lens without group_starts")
+    nbytes = _LIB.bb_shared_attention_workspace_bytes(tokens, n, groups, own_width, pre_width, heads, kv_heads, dim)
+    ws = _torch.empty(nbytes, dtype=_torch.uint8, device=dev) if nbytes else None
+    rc = _LIB.bb_shared_attention(*_heads(q, "q", dtype, tokens, heads, dim, dev), qs, n, tokens, *_cache(k_cache, "k_cache", dtype, pages, kv_heads, dim, dev),
+                                  *_cache(v_cache, "v_cache", dtype, pages, kv_heads, dim, dev), pages, own, own_ld, own_width,
+                                  _vec(own_lens, "own_lens", _I32, n, dev), pre, pre_ld, pre_width, pre_lens, gs, groups, heads, kv_heads, dim, _type(dtype, "q"), block, scale,
+                                  *_heads(out, "out", dtype, tokens, heads, dim, dev), pl, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(dev.index))
+    if rc:
+        _done(rc, "bb_shared_attention")
+    return out
+
+
+# ---- the engine -----------------------------------------------------------------------------------
 
 
 class StepView:
