@@ -38,22 +38,30 @@ struct KvArgs {
     const int *own_pages, *own_lens, *prefix_pages, *prefix_lens, *group_starts;
     long own_ld, prefix_ld;
     int q_tokens, k_tokens, n_seq, n_groups, n_pages, own_width, prefix_width;
-    int heads, each, tiles, block;
+    int heads, kv_heads, each, block;
     float scale;                                                        // times log2(e)
+    int own_tiles, own_split, prefix_tiles, prefix_split;               // row tiles that the branches (groups) may have, parts that their keys are cut into
+    float* part_o; float2* part_ml;                                     // [part][token][head]: unscaled output; maximum (times log2(e)) and sum.  Null: a single part
 };
+#define KV_LEAST_TILES 2                // of 64 keys, a part of a row tile's keys
+#define KV_MOST_PARTS 32
+#define KV_ROWS 128                     // rows (tokens x heads of a group) of a workgroup
 
-// Of `bound` sequences' row tiles the t-th: which sequence, its first and last token, which of its tiles.  Starts are taken as they come but never outside 0 .. q_tokens.
+// Of the sequences' row tiles the t-th: which sequence (range i of starts[step[i]] .., step null: i), its first token, its tokens, which of its tiles.  Starts are
+// taken as they come but never outside 0 .. q_tokens.
 struct RowTile { int seq, q0, n, tile; };
-static __device__ __forceinline__ bool find_tile(const KvArgs& a, int t, int rows_per_tile, RowTile& r) {
+static __device__ __forceinline__ bool find_tile(const KvArgs& a, const int* __restrict__ step, int ranges, int t, int each, int rows_per_tile, RowTile& r) {
     const int lane = threadIdx.x & 63;
-    for (int b = 0; b < a.n_seq; b += 64) {
+    for (int b = 0; b < ranges; b += 64) {
         const int i = b + lane;
         int s0 = 0, n = 0;
-        if (i < a.n_seq) {
-            s0 = min(max(a.q_starts[i], 0), a.q_tokens);
-            n = min(max(a.q_starts[i + 1], s0), a.q_tokens) - s0;
+        if (i < ranges) {
+            int i0 = i, i1 = i + 1;
+            if (step) { i0 = min(max(step[i], 0), a.n_seq); i1 = min(max(step[i + 1], i0), a.n_seq); }
+            s0 = min(max(a.q_starts[i0], 0), a.q_tokens);
+            n = min(max(a.q_starts[i1], s0), a.q_tokens) - s0;
         }
-        const int mine = (int)(((long)n * a.each + rows_per_tile - 1) / rows_per_tile);
+        const int mine = (int)(((long)n * each + rows_per_tile - 1) / rows_per_tile);
         int upto = mine;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -74,80 +82,230 @@ static __device__ __forceinline__ bool find_tile(const KvArgs& a, int t, int row
     return false;
 }
 
-// Which group a branch belongs to, -1: none.
-static __device__ __forceinline__ int find_group(const KvArgs& a, int seq) {
+// Whether a branch belongs to any group.
+static __device__ __forceinline__ bool has_group(const KvArgs& a, int seq) {
     const int lane = threadIdx.x & 63;
     for (int b = 0; b < a.n_groups; b += 64) {
         const int i = b + lane;
-        const unsigned long long hit = __ballot(i < a.n_groups && a.group_starts[i] <= seq && seq < a.group_starts[i + 1]);
-        if (hit) return b + __builtin_ctzll(hit);
+        if (__ballot(i < a.n_groups && a.group_starts[i] <= seq && seq < a.group_starts[i + 1])) return true;
     }
-    return -1;
+    return false;
 }
 
-// The keys of a row tile, 64 at a time: pages of the prefix, then pages of its own, or packed keys.  Pages that are not in the cache count as not there.
-struct KeyTile { const char *k, *v; int key0, n; bool own; };
-struct Keys {
-    const int *prefix, *own;        // page tables (null: packed)
-    int n_prefix, n_own, i;         // keys; i: the next tile
-    const char *k, *v;              // of the kv head (packed: of the sequence's first key)
+// A run of keys in tiles of KEYS tokens: pages, or packed.  The ids of 64 pages at a time stand in a register's lanes: a load per tile would have to be waited for, and
+// with it every fetch on its way.  Pages that are not in the cache count as not there.
+struct KeyTile { const char *k, *v; int key0, n; };
+template <int KEYS> struct Keys {
+    const int* table;               // null: packed
+    const char *k, *v;              // of the kv head (packed: of the first key)
+    int i, step, end, m;            // the next tile, how far to the one after it, where the run ends; keys in all
+    int ids, ids_at;                // page ids from ids_at on (-1: none yet)
     __device__ __forceinline__ bool next(const KvArgs& a, KeyTile& t) {
-        const int tiles_p = (n_prefix + 63) >> 6, tiles = tiles_p + ((n_own + 63) >> 6);
-        while (i < tiles) {
-            const int at = i++;
-            t.own = at >= tiles_p;
-            t.key0 = (t.own ? at - tiles_p : at) << 6;
-            t.n = min((t.own ? n_own : n_prefix) - t.key0, 64);
-            if (!a.k_starts) {
-                const int page = __builtin_amdgcn_readfirstlane((t.own ? own : prefix)[t.key0 >> 6]);
-                if ((unsigned)page >= (unsigned)a.n_pages) continue;
-                t.k = k + (long)page * a.k_ps * 2;
-                t.v = v + (long)page * a.v_ps * 2;
-            } else {
+        while (i < end) {
+            const int at = i;
+            i += step;
+            t.key0 = at * KEYS;
+            t.n = min(m - t.key0, KEYS);
+            if (!table) {
                 t.k = k + (long)t.key0 * a.k_ts * 2;
                 t.v = v + (long)t.key0 * a.v_ts * 2;
+                return true;
             }
+            const int page = t.key0 / BB_PAGE_TOKENS, within = t.key0 % BB_PAGE_TOKENS;
+            if (ids_at < 0 || page >= ids_at + 64) {
+                ids_at = page;
+                const int p = page + (int)(threadIdx.x & 63);
+                ids = p * BB_PAGE_TOKENS < m ? table[p] : -1;
+            }
+            const int id = __builtin_amdgcn_readlane(ids, page - ids_at);
+            if ((unsigned)id >= (unsigned)a.n_pages) continue;
+            t.k = k + ((long)id * a.k_ps + (long)within * a.k_ts) * 2;
+            t.v = v + ((long)id * a.v_ps + (long)within * a.v_ts) * 2;
             return true;
         }
         return false;
     }
 };
 
+// Where the 16-byte pieces of a row lie in LDS: piece c of row r at c ^ swizzle(r), so that what a wave reads at once (K: a piece of each of 32 rows; V: 32 bytes of four
+// rows, twice) touches all banks evenly.
 template <int D> static __device__ __forceinline__ int k_swizzle(int row) { return row & (D / 8 - 1); }
 template <int D> static __device__ __forceinline__ int v_swizzle(int row) { return D == 128 ? 4 * (row & 3) : 4 * (row >> 1 & 1); }
 
-// One tile's K and V on their way into LDS, rows past its end as its last one.
-template <int D> static __device__ __forceinline__ void fetch_tile(const KvArgs& a, const KeyTile& t, unsigned lds, int wave, int lane) {
-    constexpr int PER = D / 8, ROWS = 64 / PER, UNITS = 64 / ROWS;      // pieces per row, rows per KiB, KiB per tile
+// N KiB of a tile's K or V on their way into LDS, every STEP-th from the first-th on; rows past the tile's end as its last one.
+template <int D, bool V, int N, int STEP> static __device__ __forceinline__ void fetch(const char* src, long ts, int n, unsigned lds, int first, int lane) {
+    constexpr int PER = D / 8, ROWS = 64 / PER;             // pieces per row, rows per KiB
 #pragma unroll
-    for (int u = 0; u < UNITS / 4; ++u) {
-        const int unit = u * 4 + wave, row = unit * ROWS + lane / PER, piece = lane % PER, from = min(row, t.n - 1);
-        load_to_lds<0>(t.k, (unsigned)(from * (unsigned)a.k_ts * 2 + (unsigned)((piece ^ k_swizzle<D>(row)) * 16)), lds + unit * 1024);
-        load_to_lds<0>(t.v, (unsigned)(from * (unsigned)a.v_ts * 2 + (unsigned)((piece ^ v_swizzle<D>(row)) * 16)), lds + 128 * D + unit * 1024);
+    for (int u = 0; u < N; ++u) {
+        const int unit = u * STEP + first, row = unit * ROWS + lane / PER, piece = lane % PER, from = min(row, n - 1);
+        load_to_lds<0>(src, (unsigned)from * (unsigned)(ts * 2) + (unsigned)((piece ^ (V ? v_swizzle<D>(row) : k_swizzle<D>(row))) * 16), lds + unit * 1024);
     }
 }
-
-static __device__ __forceinline__ float other_half(float x, float& both) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    both = __uint_as_float(r[1]);
-    return __uint_as_float(r[0]);
+template <int N> static __device__ __forceinline__ void wait_loads() {      // until N of the wave's fetches are left
+    static_assert(N == 0 || N == 4 || N == 8, "");
+    if constexpr (N == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    else if constexpr (N == 4) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
 }
-static __device__ __forceinline__ float max_halves(float x) { float y; const float z = other_half(x, y); return fmaxf(z, y); }
-static __device__ __forceinline__ float sum_halves(float x) { float y; const float z = other_half(x, y); return z + y; }
+static __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-template <class E, int D>
-__global__ __launch_bounds__(256) void kv_attention_kernel(KvArgs a) {
+static __device__ __forceinline__ float max_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+static __device__ __forceinline__ float sum_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Parts of a row: maximum and sum.  A part without a key: (-inf, 0).  One whose scores were all -inf has a finite maximum, so that 0 / 0 comes out as the definition's NaN.
+static __device__ __forceinline__ bool no_key(float top, float sum) { return top == -INFINITY && sum == 0.f; }
+static __device__ __forceinline__ float rescale(float top, float to) { return top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - to); }
+static __device__ __forceinline__ float log_sum(float top, float sum) { return no_key(top, sum) ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718056f; }
+
+// What a lane keeps of its row: the running maximum (times scale), its half of the sum, its half of the output, whether a key was seen.
+template <int D> struct RowState { f32x16 o[D / 32]; float top, sum; bool met; };
+template <int D> static __device__ __forceinline__ void finish(RowState<D>& r) {
+    if (r.met && r.top == -INFINITY && r.sum == 0.f) r.top = -3e38f;
+}
+
+// S^T of 32 NK keys and the wave's 32 rows.
+template <class E, int D, int NK> static __device__ __forceinline__ void scores(const char* kt, const typename Half<E>::x8 (&qf)[D / 16], f32x16 (&s)[NK]) {
     typedef typename Half<E>::x8 x8;
+    const int lane = threadIdx.x & 63, h2 = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[i][e] = 0.f;
+        const int kr = 32 * i + (lane & 31);
+#pragma unroll
+        for (int st = 0; st < D / 16; ++st)
+            s[i] = Half<E>::mfma(*reinterpret_cast<const x8*>(kt + kr * 2 * D + (((2 * st + h2) ^ k_swizzle<D>(kr)) * 16)), qf[st], s[i]);
+    }
+}
+// Scores -> weights p in the operands' type.  seen: how many of the tile's keys the lane's row sees (part: not all of them in every row).
+// The maximum follows only when it would grow by more than 2^8: a weight is then at most that, of no less precision, and the output is seldom scaled.
+template <class E, int D, int NK>
+static __device__ __forceinline__ void weights(RowState<D>& r, f32x16 (&s)[NK], float scale, int seen, bool part, typename Half<E>::x8 (&p)[2 * NK]) {
+    const int h2 = (threadIdx.x & 63) >> 5;
+    r.met |= seen > 0;
+    if (part) {
+#pragma unroll
+        for (int i = 0; i < NK; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (32 * i + (e >> 2) * 8 + 4 * h2 + (e & 3) >= seen) s[i][e] = -INFINITY;
+    }
+    float best = s[0][0];
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) best = fmaxf(best, s[i][e]);
+    best = max_halves(best) * scale;
+    if (__ballot(best > r.top + 8.f)) {
+        best = fmaxf(best, r.top);
+        const float keep = r.top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(r.top - best);
+        r.sum *= keep;
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) r.o[t][e] *= keep;
+        r.top = best;
+    }
+    const float from = r.top == -INFINITY ? 0.f : r.top;        // (no key seen yet: every weight 0)
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], scale, -from));
+            sum += w;
+            p[2 * i + (e >> 3)][e & 7] = (E)w;
+        }
+    r.sum += sum;
+}
+// O^T += V^T P^T
+template <class E, int D, int NK>
+static __device__ __forceinline__ void weigh(RowState<D>& r, const char* vt, const typename Half<E>::x8 (&p)[2 * NK], int seen, bool part) {
+    typedef typename Half<E>::x8 x8;
+    const int lane = threadIdx.x & 63, h2 = lane >> 5;
+#pragma unroll
+    for (int st = 0; st < 2 * NK; ++st)
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) {
+            s16x4 f[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int key = 16 * st + 8 * u + 4 * h2 + (lane >> 2 & 3), d = 32 * t + (lane >> 4 & 1) * 16 + (lane & 3) * 4;
+                f[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4*)(vt + key * 2 * D + (((d >> 3) ^ v_swizzle<D>(key)) * 16) + (d & 7) * 2));
+            }
+            u32x4 vf;
+            __builtin_memcpy(&vf, f, 16);
+            if (part) {
+                // Weight 0 does not hide an infinity or a NaN that a row must not see from the product.  Where V holds any they are taken out, and
+                // given to the rows that see them, by a product of where they are (a NaN: both infinities).
+                unsigned bad = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) bad |= (vf[i] & Half<E>::exponent) + Half<E>::one;
+                if (__ballot((bad & 0x80008000u) != 0)) {
+                    const x8 all = __builtin_bit_cast(x8, vf);
+                    x8 fin, plus, minus, see;
+                    f32x16 z;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float x = (float)all[e];
+                        const bool fine = fabsf(x) < INFINITY;
+                        fin[e] = fine ? all[e] : (E)0.f;
+                        plus[e] = (E)(fine || x < 0.f ? 0.f : 1.f);
+                        minus[e] = (E)(fine || x > 0.f ? 0.f : 1.f);
+                        see[e] = (E)(16 * st + (e >> 2) * 8 + 4 * h2 + (e & 3) < seen ? 1.f : 0.f);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) z[e] = 0.f;
+                    const f32x16 up = Half<E>::mfma(plus, see, z), down = Half<E>::mfma(minus, see, z);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        if (up[e] > 0.f) r.o[t][e] += INFINITY;
+                        if (down[e] > 0.f) r.o[t][e] -= INFINITY;
+                    }
+                    vf = __builtin_bit_cast(u32x4, fin);
+                }
+            }
+            r.o[t] = Half<E>::mfma(__builtin_bit_cast(x8, vf), p[st], r.o[t]);
+        }
+}
+
+// A workgroup's item: a row tile of a kv head on a part of the keys of its prefix or of its own.
+// A tile of more than 32 rows: the four waves take 32 each, tiles of 64 keys pass through two stages of LDS that they share, a barrier per tile.
+// Up to 32 rows: every wave has all of them and takes each fourth tile of 32 keys through a slice of LDS of its own (K of the next while it works on V of the last),
+// without barriers; the four are joined at the end, in order.
+template <class E, int D, bool PAGED>
+__global__ __launch_bounds__(256, 2) void kv_attention_kernel(KvArgs a) {
+    typedef typename Half<E>::x8 x8;
+    typedef E x4 __attribute__((ext_vector_type(4)));
     constexpr int STAGE = 2 * 64 * D * 2, ST = D / 16, OT = D / 32;
     __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
+    __shared__ float2 ends[4][32];                          // few rows: each wave's maximum and sum
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h2 = lane >> 5;
-    const int kvh = blockIdx.x / a.tiles;
-    RowTile r;
-    if (!find_tile(a, a.tiles - 1 - (int)(blockIdx.x - kvh * a.tiles), 128, r)) return;
 
-    // the wave's rows
-    const int rows = r.n * a.each, row = r.tile * 128 + wave * 32 + (lane & 31);
-    const int token = min(row, rows - 1) / a.each, head = kvh * a.each + min(row, rows - 1) - token * a.each;
+    // Which item: the keys' parts of all kv heads are dealt to the XCDs (workgroups go to them round robin), so that the row tiles of one share an L2; last row tiles, which see
+    // the most keys, first.
+    int lin = blockIdx.x;
+    const int prefix_items = a.prefix_tiles * a.prefix_split * a.kv_heads;
+    const bool prefix = PAGED && lin < prefix_items;
+    if (!prefix) lin -= prefix_items;
+    const int tiles = prefix ? a.prefix_tiles : a.own_tiles, split = prefix ? a.prefix_split : a.own_split, chunks = split * a.kv_heads;
+    const int g8 = min(chunks & -chunks, 8), per = chunks / g8, j = lin / g8;
+    const int chunk = lin % g8 + g8 * (j % per), kvh = chunk / split, piece = chunk - kvh * split;
+    RowTile r;
+    if (!find_tile(a, prefix ? a.group_starts : nullptr, prefix ? a.n_groups : a.n_seq, tiles - 1 - j / per, a.each, KV_ROWS, r)) return;
+
+    // the lane's row
+    const int rows = r.n * a.each, tile_rows = min(rows - r.tile * KV_ROWS, KV_ROWS);
+    const bool few = tile_rows <= 32;
+    const int row = r.tile * KV_ROWS + (few ? 0 : wave * 32) + (lane & 31), row_in = min(row, rows - 1);
+    const int token = row_in / a.each, head = kvh * a.each + row_in - token * a.each;
     x8 qf[ST];
     {
         const char* q = a.q + ((long)(r.q0 + token) * a.q_ts + (long)head * a.q_hs) * 2 + 16 * h2;
@@ -155,193 +313,270 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvArgs a) {
         for (int s = 0; s < ST; ++s) qf[s] = *reinterpret_cast<const x8*>(q + 32 * s);
     }
 
-    // its keys
-    Keys keys{};
-    if (a.k_starts) {
+    // its keys, and how many of them the row sees
+    const int* table = nullptr;
+    int m, limit, tile_limit;
+    long first = 0;
+    if (!PAGED) {
         const int s0 = min(max(a.k_starts[r.seq], 0), a.k_tokens);
-        keys.n_own = __builtin_amdgcn_readfirstlane(min(max(a.k_starts[r.seq + 1], s0), a.k_tokens) - s0);
-        const int k0 = __builtin_amdgcn_readfirstlane(s0);
-        keys.k = a.k + ((long)k0 * a.k_ts + (long)kvh * a.k_hs) * 2;
-        keys.v = a.v + ((long)k0 * a.v_ts + (long)kvh * a.v_hs) * 2;
+        m = __builtin_amdgcn_readfirstlane(min(max(a.k_starts[r.seq + 1], s0), a.k_tokens) - s0);
+        first = __builtin_amdgcn_readfirstlane(s0);
+    } else if (prefix) {
+        m = __builtin_amdgcn_readfirstlane(min(max(a.prefix_lens[r.seq], 0), (int)min((long)a.prefix_width * BB_PAGE_TOKENS, 0x7FFFFFC0L)));
+        table = a.prefix_pages + (long)r.seq * a.prefix_ld;
     } else {
-        keys.n_own = __builtin_amdgcn_readfirstlane(min(max(a.own_lens[r.seq], 0), a.own_width * 64));
-        keys.own = a.own_pages + (long)r.seq * a.own_ld;
-        const int g = a.n_groups ? find_group(a, r.seq) : -1;
-        if (g >= 0) {
-            keys.n_prefix = __builtin_amdgcn_readfirstlane(min(max(a.prefix_lens[g], 0), a.prefix_width * 64));
-            keys.prefix = a.prefix_pages + (long)g * a.prefix_ld;
-        }
-        keys.k = a.k + (long)kvh * a.k_hs * 2;
-        keys.v = a.v + (long)kvh * a.v_hs * 2;
+        m = __builtin_amdgcn_readfirstlane(min(max(a.own_lens[r.seq], 0), (int)min((long)a.own_width * BB_PAGE_TOKENS, 0x7FFFFFC0L)));
+        table = a.own_pages + (long)r.seq * a.own_ld;
     }
-    const int m_keys = keys.n_own;
-    auto limit_of = [&](int tok) {      // how many of its own keys a query sees
-        if (a.block == 0) return m_keys;
-        const int p = m_keys - r.n + tok;
-        return p < 0 ? 0 : (int)min((long)m_keys, ((long)(p / a.block) + 1) * a.block);
-    };
-    const int limit = limit_of(token);
-    const int first_limit = __builtin_amdgcn_readfirstlane(limit);                      // (tokens ascend with the lane)
-    const bool live = r.tile * 128 + wave * 32 < rows;
-    const int last_limit = __builtin_amdgcn_readlane(limit, 31);
-    keys.n_own = limit_of(min(r.tile * 128 + 127, rows - 1) / a.each);                  // beyond it no row of the tile sees any
+    limit = tile_limit = m;
+    if (!prefix && a.block) {
+        auto limit_of = [&](int tok) {
+            const int p = m - r.n + tok;
+            return p < 0 ? 0 : (int)min((long)m, ((long)(p / a.block) + 1) * a.block);
+        };
+        limit = limit_of(token);
+        tile_limit = limit_of(min(r.tile * KV_ROWS + KV_ROWS - 1, rows - 1) / a.each);     // (limits ascend with the token)
+    }
+    const int first_limit = __builtin_amdgcn_readfirstlane(limit), last_limit = __builtin_amdgcn_readlane(limit, 31);
 
-    f32x16 o[OT];
+    RowState<D> st;
 #pragma unroll
     for (int t = 0; t < OT; ++t)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-    float top = -INFINITY, sum = 0.f;
-    bool met = false;                                               // a key was seen
+        for (int e = 0; e < 16; ++e) st.o[t][e] = 0.f;
+    st.top = -INFINITY; st.sum = 0.f; st.met = false;
 
     const unsigned base = lds_offset(lds);
-    KeyTile cur, nxt;
-    bool more = keys.next(a, cur);
-    if (more) fetch_tile<D>(a, cur, base, wave, lane);
-    for (int stage = 0; more; stage ^= 1) {
-        const bool after = keys.next(a, nxt);
-        if (after) {
-            fetch_tile<D>(a, nxt, base + (stage ^ 1) * STAGE, wave, lane);
-            if (D == 128) asm volatile("s_waitcnt vmcnt(8)" ::: "memory"); else asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
-        } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (live && (!cur.own || cur.key0 < last_limit)) {
-            const char* kt = lds + stage * STAGE;
-            const char* vt = kt + 128 * D;
-            f32x16 s[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[i][e] = 0.f;
-                const int kr = 32 * i + (lane & 31);
-#pragma unroll
-                for (int st = 0; st < ST; ++st)
-                    s[i] = Half<E>::mfma(*reinterpret_cast<const x8*>(kt + kr * 2 * D + (((2 * st + h2) ^ k_swizzle<D>(kr)) * 16)), qf[st], s[i]);
-            }
-            const int seen = cur.own ? limit - cur.key0 : cur.n;
-            met |= seen > 0;
-            const bool part = cur.own ? first_limit < cur.key0 + 64 : cur.n < 64;
-            if (part) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (32 * i + (e >> 2) * 8 + 4 * h2 + (e & 3) >= seen) s[i][e] = -INFINITY;
-            }
-            float best = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) best = fmaxf(best, s[i][e]);
-            best = fmaxf(top, max_halves(best) * a.scale);
-            if (__ballot(best > top)) {
-                const float keep = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - best);
-                sum *= keep;
-#pragma unroll
-                for (int t = 0; t < OT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[t][e] *= keep;
-                top = best;
-            }
-            const float from = top == -INFINITY ? 0.f : top;        // (no key seen yet: every weight 0)
-            x8 p[4];
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], a.scale, -from));
-                    sum += w;
-                    p[2 * i + (e >> 3)][e & 7] = (E)w;
-                }
-#pragma unroll
-            for (int st = 0; st < 4; ++st)
-#pragma unroll
-                for (int t = 0; t < OT; ++t) {
-                    s16x4 f[2];
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const int key = 16 * st + 8 * u + 4 * h2 + (lane >> 2 & 3), d = 32 * t + (lane >> 4 & 1) * 16 + (lane & 3) * 4;
-                        f[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            (__attribute__((address_space(3))) s16x4*)(vt + key * 2 * D + (((d >> 3) ^ v_swizzle<D>(key)) * 16) + (d & 7) * 2));
-                    }
-                    u32x4 vf;
-                    __builtin_memcpy(&vf, f, 16);
-                    if (part) {
-                        // Weight 0 does not hide an infinity or a NaN that a row must not see from the product.  Where V holds any they are taken out, and
-                        // given to the rows that see them, by a product of where they are (a NaN: both infinities).
-                        unsigned bad = 0;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) bad |= (vf[i] & Half<E>::exponent) + Half<E>::one;
-                        if (__ballot((bad & 0x80008000u) != 0)) {
-                            const x8 all = __builtin_bit_cast(x8, vf);
-                            x8 fin, plus, minus, see;
-                            f32x16 z;
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const float x = (float)all[e];
-                                const bool fine = fabsf(x) < INFINITY;
-                                fin[e] = fine ? all[e] : (E)0.f;
-                                plus[e] = (E)(fine || x < 0.f ? 0.f : 1.f);
-                                minus[e] = (E)(fine || x > 0.f ? 0.f : 1.f);
-                                see[e] = (E)(16 * st + (e >> 2) * 8 + 4 * h2 + (e & 3) < seen ? 1.f : 0.f);
-                            }
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) z[e] = 0.f;
-                            const f32x16 up = Half<E>::mfma(plus, see, z), down = Half<E>::mfma(minus, see, z);
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                if (up[e] > 0.f) o[t][e] += INFINITY;
-                                if (down[e] > 0.f) o[t][e] -= INFINITY;
-                            }
-                            vf = __builtin_bit_cast(u32x4, fin);
-                        }
-                    }
-                    o[t] = Half<E>::mfma(__builtin_bit_cast(x8, vf), p[st], o[t]);
-                }
+    const char *kb = a.k + ((long)kvh * a.k_hs + first * a.k_ts) * 2, *vb = a.v + ((long)kvh * a.v_hs + first * a.v_ts) * 2;
+    const int n_tiles = (tile_limit + 63) / 64, t0 = (int)((long)n_tiles * piece / split), t1 = (int)((long)n_tiles * (piece + 1) / split);
+    if (!few) {
+        constexpr int N = D / 32;                               // KiB of K (and of V) per wave and tile
+        Keys<64> keys{table, kb, vb, t0, 1, t1, tile_limit, 0, -1};
+        KeyTile cur, nxt;
+        const bool live = wave * 32 < tile_rows;
+        bool more = keys.next(a, cur);
+        if (more) {
+            fetch<D, false, N, 4>(cur.k, a.k_ts, cur.n, base, wave, lane);
+            fetch<D, true, N, 4>(cur.v, a.v_ts, cur.n, base + STAGE / 2, wave, lane);
         }
+        for (int stage = 0; more; stage ^= 1) {
+            wait_loads<0>();
+            __syncthreads();                                    // the tile is there, and all have left the one before it
+            more = keys.next(a, nxt);
+            if (more) {
+                const unsigned to = base + (stage ^ 1) * STAGE;
+                fetch<D, false, N, 4>(nxt.k, a.k_ts, nxt.n, to, wave, lane);
+                fetch<D, true, N, 4>(nxt.v, a.v_ts, nxt.n, to + STAGE / 2, wave, lane);
+            }
+            if (live && cur.key0 < last_limit) {
+                const char* at = lds + stage * STAGE;
+                const int seen = limit - cur.key0;
+                const bool part = first_limit < cur.key0 + 64;
+                f32x16 s[2];
+                x8 p[4];
+                scores<E, D, 2>(at, qf, s);
+                weights<E, D, 2>(st, s, a.scale, seen, part, p);
+                weigh<E, D, 2>(st, at + STAGE / 2, p, seen, part);
+            }
+            cur = nxt;
+        }
+    } else {
+        constexpr int N = D / 16;                               // KiB of K (and of V) per tile
+        const char* at = lds + wave * (STAGE / 2);
+        const unsigned to = base + wave * (STAGE / 2);
+        Keys<32> keys{table, kb, vb, 2 * t0 + wave, 4, min(2 * t1, (tile_limit + 31) / 32), tile_limit, 0, -1};
+        KeyTile cur, nxt;
+        bool more = keys.next(a, cur);
+        if (more) {
+            fetch<D, false, N, 1>(cur.k, a.k_ts, cur.n, to, 0, lane);
+            fetch<D, true, N, 1>(cur.v, a.v_ts, cur.n, to + STAGE / 4, 0, lane);
+        }
+        while (more) {
+            const int seen = limit - cur.key0;
+            const bool part = first_limit < cur.key0 + 32;
+            more = keys.next(a, nxt);
+            f32x16 s[1];
+            x8 p[2];
+            wait_loads<N>();
+            scores<E, D, 1>(at, qf, s);
+            wait_lds();
+            if (more) fetch<D, false, N, 1>(nxt.k, a.k_ts, nxt.n, to, 0, lane);
+            weights<E, D, 1>(st, s, a.scale, seen, part, p);
+            if (more) wait_loads<N>(); else wait_loads<0>();
+            weigh<E, D, 1>(st, at + STAGE / 4, p, seen, part);
+            wait_lds();
+            if (more) fetch<D, true, N, 1>(nxt.v, a.v_ts, nxt.n, to + STAGE / 4, 0, lane);
+            cur = nxt;
+        }
+        // the four waves' parts of the same rows: each brings its own to the largest maximum, then each sums a quarter of the output
+        st.sum = sum_halves(st.sum);
+        finish(st);
+        if (h2 == 0) ends[wave][lane] = make_float2(st.top, st.sum);
         __syncthreads();
-        cur = nxt;
-        more = after;
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, ends[w][lane & 31].x);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) sum += ends[w][lane & 31].y * rescale(ends[w][lane & 31].x, top);
+        const float keep = rescale(st.top, top);
+        float* all = (float*)lds;
+#pragma unroll
+        for (int t = 0; t < OT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) all[((wave * OT + t) * 16 + e) * 64 + lane] = st.o[t][e] * keep;
+        __syncthreads();
+        st.top = top; st.sum = sum;
+#pragma unroll
+        for (int e = 0; e < 4 * OT; ++e) {
+            float x = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) x += all[(w * OT * 16 + wave * 4 * OT + e) * 64 + lane];
+            st.o[e >> 4][e & 15] = x;
+        }
     }
 
-    sum = sum_halves(sum);
+    // out, or the part's share of it: a lane has runs of four elements of its row
+    if (!few) { st.sum = sum_halves(st.sum); finish(st); }
+    const bool alone = PAGED && !prefix && piece == 0 && a.prefix_split && !has_group(a, r.seq);      // (all lanes look)
     if (row >= rows) return;
-    const float inv = met ? 1.f / sum : 0.f;
-    char* out = a.out + ((long)(r.q0 + token) * a.o_ts + (long)head * a.o_hs) * 2;
-    typedef E x4 __attribute__((ext_vector_type(4)));
+    const long at_row = (long)(r.q0 + token) * a.heads + head;
+    const int groups = few ? OT : 4 * OT, g0 = few ? wave * OT : 0;
+    auto store = [&](auto&& put) {
 #pragma unroll
-    for (int t = 0; t < OT; ++t)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            x4 y;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = (E)(o[t][4 * j + i] * inv);
-            *reinterpret_cast<x4*>(out + (32 * t + 8 * j + 4 * h2) * 2) = y;
+        for (int i = 0; i < 4 * OT; ++i)
+            if (i < groups) {
+                const int g = g0 + i;                           // (run g: d = 32 (g / 4) + 8 (g % 4) + 4 h2)
+                put(32 * (g >> 2) + 8 * (g & 3) + 4 * h2, st.o[i >> 2][4 * (i & 3)], st.o[i >> 2][4 * (i & 3) + 1], st.o[i >> 2][4 * (i & 3) + 2], st.o[i >> 2][4 * (i & 3) + 3]);
+            }
+    };
+    if (!a.part_o) {
+        const float inv = no_key(st.top, st.sum) ? 0.f : 1.f / st.sum;
+        char* out = a.out + ((long)(r.q0 + token) * a.o_ts + (long)head * a.o_hs) * 2;
+        store([&](int d, float x, float y, float z, float w) { *reinterpret_cast<x4*>(out + 2 * d) = x4{(E)(x * inv), (E)(y * inv), (E)(z * inv), (E)(w * inv)}; });
+        if (a.lse && h2 == 0 && (!few || wave == 0)) a.lse[at_row] = log_sum(st.top, st.sum);
+    } else {
+        const long parts = (long)a.q_tokens * a.heads, slot = prefix ? piece : a.prefix_split + piece;
+        if (!no_key(st.top, st.sum)) {
+            float* out = a.part_o + (slot * parts + at_row) * D;
+            store([&](int d, float x, float y, float z, float w) { *reinterpret_cast<float4*>(out + d) = make_float4(x, y, z, w); });
         }
-    if (a.lse && h2 == 0) a.lse[(long)(r.q0 + token) * a.heads + head] = met ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718056f : -INFINITY;
+        if (h2 == 0 && (!few || wave == 0)) a.part_ml[slot * parts + at_row] = make_float2(st.top, st.sum);
+        // a branch outside every group: nobody else writes what its prefix would give
+        if (alone && h2 == 0 && (!few || wave == 0))
+            for (int p = 0; p < a.prefix_split; ++p) a.part_ml[p * parts + at_row] = make_float2(-INFINITY, 0.f);
+    }
 }
 
-template <class E> static void launch_kv(const KvArgs& a, int kv_heads, int head_dim, hipStream_t s) {
-    const unsigned grid = (unsigned)a.tiles * kv_heads;
-    if (head_dim == 128) kv_attention_kernel<E, 128><<<grid, 256, 0, s>>>(a);
-    else kv_attention_kernel<E, 64><<<grid, 256, 0, s>>>(a);
+// The parts of every row, joined: a group of D / 4 lanes takes each JOIN_WAYS-th of them, and the groups are joined in order.
+#define JOIN_WAYS 4
+template <class E, int D> __global__ __launch_bounds__(256) void kv_join_kernel(KvArgs a) {
+    typedef E x4 __attribute__((ext_vector_type(4)));
+    constexpr int LANES = D / 4, ROWS = 256 / LANES / JOIN_WAYS;
+    __shared__ float4 outs[JOIN_WAYS][ROWS][LANES];
+    __shared__ float sums[JOIN_WAYS][ROWS];
+    RowTile r;
+    if (!find_tile(a, nullptr, a.n_seq, blockIdx.x, a.heads, ROWS, r)) return;
+    const int rows = r.n * a.heads, n_parts = a.prefix_split + a.own_split;
+    const int l = threadIdx.x % LANES, i = threadIdx.x / LANES % ROWS, way = threadIdx.x / LANES / ROWS, row = r.tile * ROWS + i;
+    const long parts = (long)a.q_tokens * a.heads, at = (long)r.q0 * a.heads + min(row, rows - 1);
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < n_parts; ++p) top = fmaxf(top, a.part_ml[p * parts + at].x);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int p = way; p < n_parts; p += JOIN_WAYS) {
+        const float2 ml = a.part_ml[p * parts + at];
+        if (no_key(ml.x, ml.y)) continue;                       // (its output was not written)
+        const float keep = rescale(ml.x, top);
+        const float4 x = *reinterpret_cast<const float4*>(a.part_o + (p * parts + at) * D + 4 * l);
+        sum += ml.y * keep;
+        o.x += x.x * keep; o.y += x.y * keep; o.z += x.z * keep; o.w += x.w * keep;
+    }
+    outs[way][i][l] = o;
+    if (l == 0) sums[way][i] = sum;
+    __syncthreads();
+    if (way || row >= rows) return;
+#pragma unroll
+    for (int w = 1; w < JOIN_WAYS; ++w) {
+        const float4 x = outs[w][i][l];
+        o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+        sum += sums[w][i];
+    }
+    const float inv = no_key(top, sum) ? 0.f : 1.f / sum;
+    const int token = row / a.heads, head = row - token * a.heads;
+    *reinterpret_cast<x4*>(a.out + ((long)(r.q0 + token) * a.o_ts + (long)head * a.o_hs + 4 * l) * 2) = x4{(E)(o.x * inv), (E)(o.y * inv), (E)(o.z * inv), (E)(o.w * inv)};
+    if (a.lse && l == 0) a.lse[at] = log_sum(top, sum);
+}
+
+template <class E, bool PAGED> static void launch_kv(const KvArgs& a, int head_dim, hipStream_t s) {
+    const unsigned grid = (unsigned)((a.prefix_tiles * (long)a.prefix_split + a.own_tiles * (long)a.own_split) * a.kv_heads);
+    const int join_rows = 256 / (head_dim / 4) / JOIN_WAYS;
+    const unsigned join = (unsigned)(((long)a.q_tokens * a.heads + (join_rows - 1) * (long)a.n_seq) / join_rows);
+    if (head_dim == 128) {
+        kv_attention_kernel<E, 128, PAGED><<<grid, 256, 0, s>>>(a);
+        if (a.part_o) kv_join_kernel<E, 128><<<join, 256, 0, s>>>(a);
+    } else {
+        kv_attention_kernel<E, 64, PAGED><<<grid, 256, 0, s>>>(a);
+        if (a.part_o) kv_join_kernel<E, 64><<<join, 256, 0, s>>>(a);
+    }
 }
 
 static bool refuse_attention(long q_tokens, int n_seq, int heads, int kv_heads, int head_dim, int type, int block, float scale) {
     return (type != BB_BF16 && type != BB_F16) || (head_dim != 64 && head_dim != 128) || q_tokens < 0 || q_tokens > BB_MAX_TOKENS || n_seq < 0 || n_seq > BB_MAX_TOKENS || heads < 1 ||
            heads > BB_MAX_HEADS || kv_heads < 1 || heads % kv_heads || block < 0 || !(scale > 0) || !(scale < INFINITY);
 }
-// Tiles of 128 rows: as many as the sequences may need, whatever their lengths.
-static bool plan_tiles(KvArgs& a, int kv_heads) {
-    const long tiles = ((long)a.q_tokens * a.each + 127) / 128 + a.n_seq, n = tiles * kv_heads;
-    if (n > 0x7FFFFFFF) return false;
-    a.tiles = (int)tiles;
+// How many row tiles there can be, whatever the lengths, and into how many parts the keys are cut: few enough that joining them costs little, so many that the chip has
+// work.  Lengths stand on the device: tables count with their width, packed keys with their mean.
+static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim) {
+    const long rows = (long)a.q_tokens * a.each;
+    const long own = (rows + (KV_ROWS - 1) * (long)a.n_seq) / KV_ROWS, pre = prefix_keys > 0 ? (rows + (KV_ROWS - 1) * (long)a.n_groups) / KV_ROWS : 0;
+    // (tiles that sequences of equal lengths would have)
+    const long own_like = std::max(1L, a.n_seq * ((rows / a.n_seq + KV_ROWS - 1) / KV_ROWS)), pre_like = pre ? std::max(1L, a.n_groups * ((rows / a.n_groups + KV_ROWS - 1) / KV_ROWS)) : 0;
+    const long own_cols = std::max(1L, (own_keys + 63) / 64), pre_cols = std::max(1L, (prefix_keys + 63) / 64);
+    // us: a row tile on 64 keys where two workgroups share a CU / where one has it, what an item takes besides, the join's launch and its bytes per us
+    const double both = 2.2, alone = 1.4, item = 2.0, join = 4.0, join_bytes = 3e6;
+    const long most = std::max(own_cols, pre_cols);
+    long own_parts = 1, pre_parts = pre ? 1 : 0;
+    double best = 0;
+    for (long c = most, last = 0; c >= 1 && (c >= KV_LEAST_TILES || c == most); c = c * 7 / 8) {
+        const long op = std::min<long>((own_cols + c - 1) / c, KV_MOST_PARTS), pp = pre ? std::min<long>((pre_cols + c - 1) / c, KV_MOST_PARTS) : 0;
+        if (op + pp == last) continue;
+        last = op + pp;
+        const double oc = (double)((own_cols + op - 1) / op), pc = pp ? (double)((pre_cols + pp - 1) / pp) : 0, oi = (double)own_like * op * a.kv_heads, pi = (double)pre_like * pp * a.kv_heads;
+        const double u = oi + pi > 256 ? both : alone, all = (oi * (item + oc * u) + pi * (item + pc * u)) / (oi + pi > 256 ? 512 : 256);
+        const double cost = std::max(all, item + u * std::max(oc, pc)) + (op + pp > 1 ? join + (double)rows * a.kv_heads * (op + pp) * head_dim * 8 / join_bytes : 0);
+        if (best == 0 || cost < best) { best = cost; own_parts = op; pre_parts = pp; }
+    }
+    if ((own * own_parts + pre * pre_parts) * a.kv_heads > 0x7FFFFFFF || ((long)a.q_tokens * a.heads + 3L * a.n_seq) / 2 > 0x7FFFFFFF) return false;
+    a.own_tiles = (int)own; a.own_split = (int)own_parts; a.prefix_tiles = (int)pre; a.prefix_split = (int)pre_parts;
     return true;
+}
+static size_t parts_bytes(const KvArgs& a, int head_dim) {
+    const size_t parts = a.own_split + a.prefix_split;
+    return parts > 1 ? align_up((size_t)a.q_tokens * a.heads * parts * head_dim * 4, 256) + align_up((size_t)a.q_tokens * a.heads * parts * 8, 256) : 0;
+}
+static int place_parts(KvArgs& a, int head_dim, void* workspace_dev, size_t workspace_bytes) {
+    const size_t need = parts_bytes(a, head_dim);
+    if (need == 0) return BB_OK;
+    if (workspace_bytes < need) return BB_ENOMEM;
+    if (!workspace_dev || (uintptr_t)workspace_dev % 256) return BB_EINVAL;
+    a.part_o = (float*)workspace_dev;
+    a.part_ml = (float2*)((char*)workspace_dev + align_up((size_t)a.q_tokens * a.heads * (a.own_split + a.prefix_split) * head_dim * 4, 256));
+    return BB_OK;
 }
 // Within a tile offsets are of 32 bits.
 static bool far_rows(long ts) { return ts > 1 << 23; }
 
-extern "C" size_t bb_attention_workspace_bytes(long q_tokens, long k_tokens, int n_seq, int heads, int kv_heads, int head_dim) { return 0; }
+static bool refuse_tables(int n_groups, int own_width, int prefix_width) {
+    return n_groups < 0 || n_groups > BB_MAX_TOKENS || own_width < 0 || own_width > BB_MAX_PAGES || prefix_width < 0 || prefix_width > BB_MAX_PAGES;
+}
+
+extern "C" size_t bb_attention_workspace_bytes(long q_tokens, long k_tokens, int n_seq, int heads, int kv_heads, int head_dim) {
+    if (refuse_attention(q_tokens, n_seq, heads, kv_heads, head_dim, BB_BF16, 0, 1.f) || k_tokens < 0 || k_tokens > BB_MAX_TOKENS || q_tokens == 0 || n_seq == 0) return 0;
+    KvArgs a{};
+    a.q_tokens = (int)q_tokens; a.n_seq = n_seq; a.heads = heads; a.kv_heads = kv_heads; a.each = heads / kv_heads;
+    return plan_parts(a, k_tokens / n_seq, 0, head_dim) ? parts_bytes(a, head_dim) : 0;
+}
 
 extern "C" int bb_attention(const void* q_dev, long q_token, long q_head, const void* k_dev, long k_token, long k_head, const void* v_dev, long v_token, long v_head,
                             const int32_t* q_starts_dev, const int32_t* k_starts_dev, int n_seq, long q_tokens, long k_tokens, int heads, int kv_heads, int head_dim,
@@ -361,20 +596,26 @@ extern "C" int bb_attention(const void* q_dev, long q_token, long q_head, const 
     a.v = (const char*)v_dev; a.v_ts = k_tokens > 1 ? v_token : 0; a.v_hs = v_head; a.out = (char*)out_dev; a.o_ts = o_token; a.o_hs = o_head; a.lse = lse_dev;
     a.q_starts = q_starts_dev; a.k_starts = k_starts_dev; a.n_seq = n_seq; a.q_tokens = (int)q_tokens; a.k_tokens = (int)k_tokens;
     a.heads = heads; a.each = heads / kv_heads; a.block = block; a.scale = scale * 1.44269504089f;
-    if (!plan_tiles(a, kv_heads)) return BB_EINVAL;
-    if (type == BB_BF16) launch_kv<__bf16>(a, kv_heads, head_dim, (hipStream_t)hip_stream); else launch_kv<half_t>(a, kv_heads, head_dim, (hipStream_t)hip_stream);
+    a.kv_heads = kv_heads;
+    if (!plan_parts(a, k_tokens / n_seq, 0, head_dim)) return BB_EINVAL;
+    if (const int rc = place_parts(a, head_dim, workspace_dev, workspace_bytes)) return rc;
+    if (type == BB_BF16) launch_kv<__bf16, false>(a, head_dim, (hipStream_t)hip_stream); else launch_kv<half_t, false>(a, head_dim, (hipStream_t)hip_stream);
     return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
 }
 
-extern "C" size_t bb_shared_attention_workspace_bytes(long q_tokens, int n_branches, int n_groups, int own_width, int prefix_width, int heads, int kv_heads, int head_dim) { return 0; }
+extern "C" size_t bb_shared_attention_workspace_bytes(long q_tokens, int n_branches, int n_groups, int own_width, int prefix_width, int heads, int kv_heads, int head_dim) {
+    if (refuse_attention(q_tokens, n_branches, heads, kv_heads, head_dim, BB_BF16, 0, 1.f) || refuse_tables(n_groups, own_width, prefix_width) || q_tokens == 0 || n_branches == 0) return 0;
+    KvArgs a{};
+    a.q_tokens = (int)q_tokens; a.n_seq = n_branches; a.n_groups = n_groups; a.heads = heads; a.kv_heads = kv_heads; a.each = heads / kv_heads;
+    return plan_parts(a, 64L * own_width, n_groups ? 64L * prefix_width : 0, head_dim) ? parts_bytes(a, head_dim) : 0;
+}
 
 extern "C" int bb_shared_attention(const void* q_dev, long q_token, long q_head, const int32_t* q_starts_dev, int n_branches, long q_tokens, const void* k_cache_dev, long kc_page,
                                    long kc_head, long kc_token, const void* v_cache_dev, long vc_page, long vc_head, long vc_token, int n_pages, const int32_t* own_pages_dev,
                                    long own_ld, int own_width, const int32_t* own_lens_dev, const int32_t* prefix_pages_dev, long prefix_ld, int prefix_width,
                                    const int32_t* prefix_lens_dev, const int32_t* group_starts_dev, int n_groups, int heads, int kv_heads, int head_dim, int type, int block,
                                    float scale, void* out_dev, long o_token, long o_head, float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
-    if (refuse_attention(q_tokens, n_branches, heads, kv_heads, head_dim, type, block, scale) || n_groups < 0 || n_groups > BB_MAX_TOKENS || n_pages < 1 || n_pages > BB_MAX_PAGES ||
-        own_width < 0 || own_width > BB_MAX_PAGES || prefix_width < 0 || prefix_width > BB_MAX_PAGES || (n_branches > 1 && own_ld < 0) || (n_groups > 1 && prefix_ld < 0))
+    if (refuse_attention(q_tokens, n_branches, heads, kv_heads, head_dim, type, block, scale) || refuse_tables(n_groups, own_width, prefix_width) || n_pages < 1 || n_pages > BB_MAX_PAGES || (n_branches > 1 && own_ld < 0) || (n_groups > 1 && prefix_ld < 0))
         return BB_EINVAL;
     if (q_tokens == 0 || n_branches == 0) return BB_OK;
     if (!q_starts_dev || !own_lens_dev || (own_width > 0 && !own_pages_dev) || (uintptr_t)q_starts_dev % 4 || (uintptr_t)own_pages_dev % 4 || (uintptr_t)own_lens_dev % 4 ||
@@ -392,7 +633,9 @@ extern "C" int bb_shared_attention(const void* q_dev, long q_token, long q_head,
     a.q_starts = q_starts_dev; a.n_seq = n_branches; a.q_tokens = (int)q_tokens; a.own_pages = own_pages_dev; a.own_ld = own_ld; a.own_lens = own_lens_dev; a.own_width = own_width;
     a.prefix_pages = prefix_pages_dev; a.prefix_ld = prefix_ld; a.prefix_lens = prefix_lens_dev; a.prefix_width = prefix_width; a.group_starts = group_starts_dev; a.n_groups = n_groups;
     a.n_pages = n_pages; a.heads = heads; a.each = heads / kv_heads; a.block = block; a.scale = scale * 1.44269504089f;
-    if (!plan_tiles(a, kv_heads)) return BB_EINVAL;
-    if (type == BB_BF16) launch_kv<__bf16>(a, kv_heads, head_dim, (hipStream_t)hip_stream); else launch_kv<half_t>(a, kv_heads, head_dim, (hipStream_t)hip_stream);
+    a.kv_heads = kv_heads;
+    if (!plan_parts(a, 64L * own_width, n_groups ? 64L * prefix_width : 0, head_dim)) return BB_EINVAL;
+    if (const int rc = place_parts(a, head_dim, workspace_dev, workspace_bytes)) return rc;
+    if (type == BB_BF16) launch_kv<__bf16, true>(a, head_dim, (hipStream_t)hip_stream); else launch_kv<half_t, true>(a, head_dim, (hipStream_t)hip_stream);
     return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
 }
