@@ -13,9 +13,99 @@ struct RopeArgs {
     long tokens, n_slots;
     int q_heads, k_heads, dim, rot, interleaved;
     float magnitude;
+    // pieces: units of a token and of a head, with 2^32 / them rounded up; tokens of a workgroup, units that it takes of them
+    int units, head_units, per_group, per_slice; unsigned by_units, by_head;
 };
+#define ROPE_TURNS 1024
 
-// A workgroup per token: its angles once, for all heads; then a thread per pair, or per element of what is not turned.
+static __device__ __forceinline__ float2 turn_of(double position, double freq, float magnitude) {
+    double turns = position * freq * 0.15915494309189533577;           // 1 / (2 pi)
+    turns -= rint(turns);
+    float s, c;
+    sincospif(2.f * (float)turns, &s, &c);
+    return make_float2(c * magnitude, s * magnitude);
+}
+// The tokens of a slot: where its key and value go.
+struct RopePlace { long k_at, v_at; bool kept; };
+static __device__ __forceinline__ RopePlace place_of(const RopeArgs& a, long t) {
+    if (!a.slots) return {t * a.ko_ts, 0, true};
+    const long slot = a.slots[t];
+    if (slot < 0 || slot >= a.n_slots) return {0, 0, false};           // kept out of the cache
+    return {(slot >> 6) * a.ko_ps + (slot & 63) * a.ko_ts, (slot >> 6) * a.vo_ps + (slot & 63) * a.vo_ts, true};
+}
+
+// Rows of 16-byte pieces.  A unit is a piece and the one it is turned with (half: half the turned range further on; interleaved: a piece holds its pairs), or a piece of what is
+// not turned; values move in the same units.  A thread takes units of all its workgroup's tokens' heads, its loads on their way while the angles are made.
+template <class E, bool INTER> __global__ __launch_bounds__(256) void rope_pieces_kernel(RopeArgs a) {
+    constexpr int VEC = 16 / sizeof(E), AT_ONCE = 4;
+    typedef E vec __attribute__((ext_vector_type(VEC)));
+    __shared__ __attribute__((aligned(16))) float2 turn[ROPE_TURNS];
+    const int half = a.rot >> 1, turned = INTER ? a.rot / VEC : half / VEC;
+    const long t0 = (long)blockIdx.x * a.per_group;
+    const int tokens = (int)min((long)a.per_group, a.tokens - t0), units = a.units, all = tokens * units;
+    const int from = blockIdx.y * a.per_slice, to = min(from + a.per_slice, all);
+    bool first = true;
+    for (int i0 = from; i0 < to; i0 += 256 * AT_ONCE) {
+        vec x[AT_ONCE][2];
+        E *y[AT_ONCE];
+        int pair[AT_ONCE];                                          // which turns; -1: a copy of both, -2: of the first piece, -3: nothing
+#pragma unroll
+        for (int n = 0; n < AT_ONCE; ++n) {
+            const int i = i0 + n * 256 + (int)threadIdx.x;
+            pair[n] = -3;
+            if (i >= to) continue;
+            const int tk = (int)__umulhi(i, a.by_units), in = i - tk * units, h = (int)__umulhi(in, a.by_head), j = in - h * a.head_units;
+            const long t = t0 + tk;
+            const int kind = h < a.q_heads ? 0 : h < a.q_heads + a.k_heads ? 1 : 2;
+            const RopePlace at = kind ? place_of(a, t) : RopePlace{};
+            if (kind && !at.kept) continue;
+            const int hk = h - a.q_heads - (kind == 2 ? a.k_heads : 0);
+            const E* src = kind == 0 ? (const E*)a.q + t * a.q_ts + h * a.q_hs : kind == 1 ? (const E*)a.k + t * a.k_ts + hk * a.k_hs : (const E*)a.v + t * a.v_ts + hk * a.v_hs;
+            E* dst = kind == 0 ? (E*)a.qo + t * a.qo_ts + h * a.qo_hs : kind == 1 ? (E*)a.ko + at.k_at + hk * a.ko_hs : (E*)a.vo + at.v_at + hk * a.vo_hs;
+            const bool turn_it = j < turned;
+            const int e = turn_it ? j * VEC : a.rot + (j - turned) * VEC;
+            y[n] = dst + e;
+            x[n][0] = *reinterpret_cast<const vec*>(src + e);
+            if (!INTER && turn_it) x[n][1] = *reinterpret_cast<const vec*>(src + e + half);
+            pair[n] = !turn_it ? -2 : kind == 2 ? (INTER ? -2 : -1) : tk * half + (INTER ? e >> 1 : e);
+        }
+        if (first) {
+            for (int i = threadIdx.x; i < tokens * half; i += 256) {
+                const int tk = i / half;
+                turn[i] = turn_of((double)a.positions[t0 + tk], a.freqs[i - tk * half], a.magnitude);
+            }
+            __syncthreads();
+            first = false;
+        }
+#pragma unroll
+        for (int n = 0; n < AT_ONCE; ++n) {
+            if (pair[n] == -3) continue;
+            vec u = x[n][0], w = x[n][1];
+            if (pair[n] >= 0) {
+                const float2* cs = turn + pair[n];
+                if constexpr (INTER) {
+#pragma unroll
+                    for (int k = 0; k < VEC / 2; ++k) {
+                        const float p = (float)u[2 * k], q = (float)u[2 * k + 1];
+                        u[2 * k] = (E)(p * cs[k].x - q * cs[k].y);
+                        u[2 * k + 1] = (E)(p * cs[k].y + q * cs[k].x);
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) {
+                        const float p = (float)u[k], q = (float)w[k];
+                        u[k] = (E)(p * cs[k].x - q * cs[k].y);
+                        w[k] = (E)(p * cs[k].y + q * cs[k].x);
+                    }
+                }
+            }
+            *reinterpret_cast<vec*>(y[n]) = u;
+            if (!INTER && pair[n] >= -1) *reinterpret_cast<vec*>(y[n] + half) = w;
+        }
+    }
+}
+
+// Rows of any alignment, any number of elements: a workgroup per token, a thread per pair, or per element of what is not turned.
 template <class E>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     __shared__ float2 turn[BB_ROPE_MAX_DIM / 2];
@@ -23,28 +113,16 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     for (long t = blockIdx.x; t < a.tokens; t += gridDim.x) {
         const double p = (double)a.positions[t];
         __syncthreads();
-        for (int j = threadIdx.x; j < half; j += 256) {
-            double turns = p * a.freqs[j] * 0.15915494309189533577;    // 1 / (2 pi)
-            turns -= rint(turns);
-            float s, c;
-            sincospif(2.f * (float)turns, &s, &c);
-            turn[j] = make_float2(c * a.magnitude, s * a.magnitude);
-        }
+        for (int j = threadIdx.x; j < half; j += 256) turn[j] = turn_of(p, a.freqs[j], a.magnitude);
         __syncthreads();
-        long k_at = 0, v_at = 0, slot = t;
-        if (a.slots) {
-            slot = a.slots[t];
-            if (slot < 0 || slot >= a.n_slots) slot = -1;           // kept out of the cache
-            k_at = (slot >> 6) * a.ko_ps + (slot & 63) * a.ko_ts;
-            v_at = (slot >> 6) * a.vo_ps + (slot & 63) * a.vo_ts;
-        } else k_at = t * a.ko_ts;
+        const RopePlace at = place_of(a, t);
         const int pairs = half + (a.dim - a.rot);
-        const int heads = a.q_heads + (slot < 0 ? 0 : a.k_heads);
+        const int heads = a.q_heads + (at.kept ? a.k_heads : 0);
         for (int i = threadIdx.x; i < heads * pairs; i += 256) {
             const int h = i / pairs, j = i - h * pairs;
             const bool is_q = h < a.q_heads;
             const E* x = is_q ? (const E*)a.q + t * a.q_ts + h * a.q_hs : (const E*)a.k + t * a.k_ts + (h - a.q_heads) * a.k_hs;
-            E* y = is_q ? (E*)a.qo + t * a.qo_ts + h * a.qo_hs : (E*)a.ko + k_at + (h - a.q_heads) * a.ko_hs;
+            E* y = is_q ? (E*)a.qo + t * a.qo_ts + h * a.qo_hs : (E*)a.ko + at.k_at + (h - a.q_heads) * a.ko_hs;
             if (j < half) {
                 const int e0 = a.interleaved ? 2 * j : j, e1 = a.interleaved ? 2 * j + 1 : j + half;
                 const float u = (float)x[e0], w = (float)x[e1];
@@ -53,19 +131,49 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
                 y[e1] = (E)(u * cs.y + w * cs.x);
             } else y[a.rot + j - half] = x[a.rot + j - half];
         }
-        if (a.vo && slot >= 0)
+        if (a.vo && at.kept)
             for (int i = threadIdx.x; i < a.k_heads * a.dim; i += 256) {
                 const int h = i / a.dim, d = i - h * a.dim;
-                ((E*)a.vo)[v_at + h * a.vo_hs + d] = ((const E*)a.v)[t * a.v_ts + h * a.v_hs + d];
+                ((E*)a.vo)[at.v_at + h * a.vo_hs + d] = ((const E*)a.v)[t * a.v_ts + h * a.v_hs + d];
             }
     }
 }
 
-static int launch_rope(const RopeArgs& a, int type, hipStream_t s) {
-    const unsigned grid = (unsigned)std::min<long>(a.tokens, 1 << 20);
-    if (type == BB_F32) rope_kernel<float><<<grid, 256, 0, s>>>(a);
-    else if (type == BB_BF16) rope_kernel<__bf16><<<grid, 256, 0, s>>>(a);
-    else rope_kernel<half_t><<<grid, 256, 0, s>>>(a);
+// Units are numbered below 2^16, so that a product with 2^32 / n rounded up divides them by n exactly (n up to 2^16).
+#define ROPE_MOST_UNITS 65536
+template <class E> static void launch_rope(RopeArgs& a, hipStream_t s) {
+    constexpr int VEC = 16 / sizeof(E);
+    const int turned = a.interleaved ? a.rot / VEC : a.rot / 2 / VEC, rest = (a.dim - a.rot) / VEC, heads = a.q_heads + a.k_heads * (a.vo ? 2 : 1);
+    const bool whole = a.dim % VEC == 0 && (a.rot / (a.interleaved ? 1 : 2)) % VEC == 0;
+    const long units = (long)heads * (turned + rest);
+    auto aligned = [&](const void* p, long s0, long s1, long s2) { return (uintptr_t)p % 16 == 0 && s0 % VEC == 0 && s1 % VEC == 0 && s2 % VEC == 0; };
+    if (whole && units <= ROPE_MOST_UNITS && (!a.q_heads || (aligned(a.q, a.q_ts, a.q_hs, 0) && aligned(a.qo, a.qo_ts, a.qo_hs, 0))) &&
+        (!a.k_heads || (aligned(a.k, a.k_ts, a.k_hs, 0) && aligned(a.ko, a.ko_ps, a.ko_ts, a.ko_hs))) &&
+        (!a.vo || (aligned(a.v, a.v_ts, a.v_hs, 0) && aligned(a.vo, a.vo_ps, a.vo_ts, a.vo_hs)))) {
+        // one thread a unit while there are few; four, or more, where the chip is full
+        a.head_units = turned + rest; a.units = (int)units;
+        a.per_group = (int)std::max(1L, std::min<long>(256 / units, a.rot ? ROPE_TURNS / (a.rot / 2) : 256));
+        const long groups = (a.tokens + a.per_group - 1) / a.per_group, in_group = a.per_group * units;
+        const long slices = std::max(1L, std::min((in_group + 255) / 256, 1024 / groups));
+        a.per_slice = (int)((in_group + slices - 1) / slices + 255) / 256 * 256;
+        a.by_units = units > 1 ? (unsigned)((0x100000000ull + units - 1) / units) : 0;
+        a.by_head = a.head_units > 1 ? (unsigned)((0x100000000ull + a.head_units - 1) / a.head_units) : 0;
+        if (units > 1 && a.head_units > 1 && groups <= 0x7FFFFFFF) {
+            const dim3 grid((unsigned)groups, (unsigned)((in_group + a.per_slice - 1) / a.per_slice));
+            if (a.interleaved) rope_pieces_kernel<E, true><<<grid, 256, 0, s>>>(a); else rope_pieces_kernel<E, false><<<grid, 256, 0, s>>>(a);
+            return;
+        }
+    }
+    rope_kernel<E><<<(unsigned)std::min<long>(a.tokens, 1 << 20), 256, 0, s>>>(a);
+}
+static int launch_rope(RopeArgs& a, int type, hipStream_t s) {
+    if (a.tokens == 1) a.q_ts = a.k_ts = a.v_ts = a.qo_ts = 0;             // (a single token, or head, has no next)
+    if (a.q_heads == 1) a.q_hs = a.qo_hs = 0;
+    if (a.k_heads == 1) a.k_hs = a.ko_hs = a.v_hs = a.vo_hs = 0;
+    if (!a.slots && a.tokens == 1) a.ko_ts = 0;
+    if (type == BB_F32) launch_rope<float>(a, s);
+    else if (type == BB_BF16) launch_rope<__bf16>(a, s);
+    else launch_rope<half_t>(a, s);
     return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
 }
 
