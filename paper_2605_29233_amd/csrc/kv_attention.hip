@@ -132,15 +132,35 @@ template <int KEYS> struct Keys {
 template <int D> static __device__ __forceinline__ int k_swizzle(int row) { return row & (D / 8 - 1); }
 template <int D> static __device__ __forceinline__ int v_swizzle(int row) { return D == 128 ? 4 * (row & 3) : 4 * (row >> 1 & 1); }
 
-// N KiB of a tile's K or V on their way into LDS, every STEP-th from the first-th on; rows past the tile's end as its last one.
-template <int D, bool V, int N, int STEP> static __device__ __forceinline__ void fetch(const char* src, long ts, int n, unsigned lds, int first, int lane) {
-    constexpr int PER = D / 8, ROWS = 64 / PER;             // pieces per row, rows per KiB
+// KiB of a tile's K or V on their way into LDS: N of them, every STEP-th from the first-th on.  A lane's offset is that of its row and piece in the first KiB; the rows of the
+// next lie `step` bytes further on, and their swizzle is the same, or (K, STEP 1, 16 pieces a row) one of four.
+template <int D, bool V, int N, int STEP> struct Fetch {
+    static constexpr int PER = D / 8, ROWS = 64 / PER, KINDS = !V && STEP == 1 && D == 128 ? 4 : 1;     // pieces per row, rows per KiB
+    unsigned off[KINDS]; long ts2;
+    __device__ __forceinline__ static unsigned piece_of(int row) { return (unsigned)(((threadIdx.x & 63) % PER ^ (V ? v_swizzle<D>(row) : k_swizzle<D>(row))) * 16); }
+    __device__ __forceinline__ Fetch(long ts, int first) : ts2(ts * 2) {
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
-        const int unit = u * STEP + first, row = unit * ROWS + lane / PER, piece = lane % PER, from = min(row, n - 1);
-        load_to_lds<0>(src, (unsigned)from * (unsigned)(ts * 2) + (unsigned)((piece ^ (V ? v_swizzle<D>(row) : k_swizzle<D>(row))) * 16), lds + unit * 1024);
+        for (int i = 0; i < KINDS; ++i) {
+            const int row = (first + i) * ROWS + (int)(threadIdx.x & 63) / PER;
+            off[i] = (unsigned)(row - i * ROWS) * (unsigned)ts2 + piece_of(row);
+        }
     }
-}
+    __device__ __forceinline__ void whole(const char* src, unsigned lds, int first) const {
+#pragma unroll
+        for (int u = 0; u < N; ++u) load_to_lds<0>(src + (long)(u * STEP * ROWS) * ts2, off[u % KINDS], lds + (u * STEP + first) * 1024);
+    }
+    // a tile that ends early: rows past its end as its last one
+    __device__ __forceinline__ void some(const char* src, int n, unsigned lds, int first) const {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int row = (u * STEP + first) * ROWS + (int)(threadIdx.x & 63) / PER;
+            load_to_lds<0>(src, (unsigned)min(row, n - 1) * (unsigned)ts2 + piece_of(row), lds + (u * STEP + first) * 1024);
+        }
+    }
+    __device__ __forceinline__ void operator()(const char* src, int n, int keys, unsigned lds, int first) const {
+        if (n == keys) whole(src, lds, first); else some(src, n, lds, first);
+    }
+};
 template <int N> static __device__ __forceinline__ void wait_loads() {      // until N of the wave's fetches are left
     static_assert(N == 0 || N == 4 || N == 8, "");
     if constexpr (N == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -169,27 +189,39 @@ template <int D> static __device__ __forceinline__ void finish(RowState<D>& r) {
     if (r.met && r.top == -INFINITY && r.sum == 0.f) r.top = -3e38f;
 }
 
+// Operands that are on their way from LDS while the matrix cores work; the order is fixed by hand, as the compiler would bring all of them first and spill.
+#define AHEAD 4
 // S^T of 32 NK keys and the wave's 32 rows.
 template <class E, int D, int NK> static __device__ __forceinline__ void scores(const char* kt, const typename Half<E>::x8 (&qf)[D / 16], f32x16 (&s)[NK]) {
     typedef typename Half<E>::x8 x8;
     const int lane = threadIdx.x & 63, h2 = lane >> 5;
+    constexpr int STEPS = NK * (D / 16);
+    x8 ring[AHEAD];
+    auto piece = [&](int n) {                               // step n: 16 d (16 (n / NK) on) of 32 keys (32 (n % NK) on)
+        const int kr = 32 * (n % NK) + (lane & 31);
+        return *reinterpret_cast<const x8*>(kt + kr * 2 * D + (((2 * (n / NK) + h2) ^ k_swizzle<D>(kr)) * 16));
+    };
 #pragma unroll
-    for (int i = 0; i < NK; ++i) {
+    for (int n = 0; n < AHEAD; ++n) ring[n] = piece(n);
+#pragma unroll
+    for (int i = 0; i < NK; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[i][e] = 0.f;
-        const int kr = 32 * i + (lane & 31);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int st = 0; st < D / 16; ++st)
-            s[i] = Half<E>::mfma(*reinterpret_cast<const x8*>(kt + kr * 2 * D + (((2 * st + h2) ^ k_swizzle<D>(kr)) * 16)), qf[st], s[i]);
+    for (int n = 0; n < STEPS; ++n) {
+        s[n % NK] = Half<E>::mfma(ring[n % AHEAD], qf[n / NK], s[n % NK]);
+        if (n + AHEAD < STEPS) ring[n % AHEAD] = piece(n + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
-// Scores -> weights p in the operands' type.  seen: how many of the tile's keys the lane's row sees (part: not all of them in every row).
+// Scores -> weights p in the operands' type.  PART: not every row sees all of the tile's keys; seen: how many of them the lane's row does.
 // The maximum follows only when it would grow by more than 2^8: a weight is then at most that, of no less precision, and the output is seldom scaled.
-template <class E, int D, int NK>
-static __device__ __forceinline__ void weights(RowState<D>& r, f32x16 (&s)[NK], float scale, int seen, bool part, typename Half<E>::x8 (&p)[2 * NK]) {
+template <class E, int D, int NK, bool PART>
+static __device__ __forceinline__ void weights(RowState<D>& r, f32x16 (&s)[NK], float scale, int seen, typename Half<E>::x8 (&p)[2 * NK]) {
     const int h2 = (threadIdx.x & 63) >> 5;
-    r.met |= seen > 0;
-    if (part) {
+    if (PART) {
+        r.met |= seen > 0;
 #pragma unroll
         for (int i = 0; i < NK; ++i)
 #pragma unroll
@@ -212,68 +244,91 @@ static __device__ __forceinline__ void weights(RowState<D>& r, f32x16 (&s)[NK], 
             for (int e = 0; e < 16; ++e) r.o[t][e] *= keep;
         r.top = best;
     }
-    const float from = r.top == -INFINITY ? 0.f : r.top;        // (no key seen yet: every weight 0)
-    float sum = 0.f;
+    const float from = r.top == -INFINITY ? 0.f : r.top;        // (no key seen yet, or only scores of -inf: every weight 0)
+    float sum = 0.f, sum2 = 0.f;
 #pragma unroll
     for (int i = 0; i < NK; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], scale, -from));
-            sum += w;
+            if (e & 1) sum2 += w; else sum += w;
             p[2 * i + (e >> 3)][e & 7] = (E)w;
         }
-    r.sum += sum;
+    r.sum += sum + sum2;
+}
+// V^T of 16 keys (from 16 st on) and 32 d (from 32 t on), in the order of the weights.
+template <class E, int D> static __device__ __forceinline__ typename Half<E>::x8 values(const char* vt, int st, int t) {
+    const int lane = threadIdx.x & 63, d = 32 * t + (lane >> 4 & 1) * 16 + (lane & 3) * 4;
+    s16x4 f[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int key = 16 * st + 8 * u + 4 * (lane >> 5) + (lane >> 2 & 3);
+        f[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + key * 2 * D + (((d >> 3) ^ v_swizzle<D>(key)) * 16) + (d & 7) * 2));
+    }
+    typename Half<E>::x8 v;
+    __builtin_memcpy(&v, f, 16);
+    return v;
+}
+// Whether a tile of V holds an infinity or a NaN.
+template <class E, int D, int NK> static __device__ __forceinline__ bool any_infinite(const char* vt) {
+    unsigned bad = 0;
+#pragma unroll
+    for (int i = 0; i < NK * D / 16; ++i) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(vt + i * 1024 + (threadIdx.x & 63) * 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) bad |= (x[j] & Half<E>::exponent) + Half<E>::one;
+        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);          // (no more registers than that)
+    }
+    return __ballot((bad & 0x80008000u) != 0) != 0;
 }
 // O^T += V^T P^T
-template <class E, int D, int NK>
-static __device__ __forceinline__ void weigh(RowState<D>& r, const char* vt, const typename Half<E>::x8 (&p)[2 * NK], int seen, bool part) {
+template <class E, int D, int NK, bool PART>
+static __device__ __forceinline__ void weigh(RowState<D>& r, const char* vt, const typename Half<E>::x8 (&p)[2 * NK], int seen) {
     typedef typename Half<E>::x8 x8;
-    const int lane = threadIdx.x & 63, h2 = lane >> 5;
+    if (!PART || !any_infinite<E, D, NK>(vt)) {
+        constexpr int OT = D / 32, STEPS = 2 * NK * OT;
+        x8 ring[AHEAD];
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) ring[n] = values<E, D>(vt, n / OT, n % OT);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < STEPS; ++n) {
+            r.o[n % OT] = Half<E>::mfma(ring[n % AHEAD], p[n / OT], r.o[n % OT]);
+            if (n + AHEAD < STEPS) ring[n % AHEAD] = values<E, D>(vt, (n + AHEAD) / OT, (n + AHEAD) % OT);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        return;
+    }
+    // Weight 0 does not hide an infinity or a NaN that a row must not see from the product: it is made without them, and rows that see them get them added, key by key.
 #pragma unroll
     for (int st = 0; st < 2 * NK; ++st)
 #pragma unroll
         for (int t = 0; t < D / 32; ++t) {
-            s16x4 f[2];
+            u32x4 v = __builtin_bit_cast(u32x4, values<E, D>(vt, st, t));
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int key = 16 * st + 8 * u + 4 * h2 + (lane >> 2 & 3), d = 32 * t + (lane >> 4 & 1) * 16 + (lane & 3) * 4;
-                f[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4*)(vt + key * 2 * D + (((d >> 3) ^ v_swizzle<D>(key)) * 16) + (d & 7) * 2));
+            for (int i = 0; i < 4; ++i) {
+                const unsigned bad = (v[i] & Half<E>::exponent) + Half<E>::one;
+                v[i] &= (bad & 0x8000u ? 0u : 0xFFFFu) | (bad & 0x80000000u ? 0u : 0xFFFF0000u);
             }
-            u32x4 vf;
-            __builtin_memcpy(&vf, f, 16);
-            if (part) {
-                // Weight 0 does not hide an infinity or a NaN that a row must not see from the product.  Where V holds any they are taken out, and
-                // given to the rows that see them, by a product of where they are (a NaN: both infinities).
-                unsigned bad = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) bad |= (vf[i] & Half<E>::exponent) + Half<E>::one;
-                if (__ballot((bad & 0x80008000u) != 0)) {
-                    const x8 all = __builtin_bit_cast(x8, vf);
-                    x8 fin, plus, minus, see;
-                    f32x16 z;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float x = (float)all[e];
-                        const bool fine = fabsf(x) < INFINITY;
-                        fin[e] = fine ? all[e] : (E)0.f;
-                        plus[e] = (E)(fine || x < 0.f ? 0.f : 1.f);
-                        minus[e] = (E)(fine || x > 0.f ? 0.f : 1.f);
-                        see[e] = (E)(16 * st + (e >> 2) * 8 + 4 * h2 + (e & 3) < seen ? 1.f : 0.f);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) z[e] = 0.f;
-                    const f32x16 up = Half<E>::mfma(plus, see, z), down = Half<E>::mfma(minus, see, z);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        if (up[e] > 0.f) r.o[t][e] += INFINITY;
-                        if (down[e] > 0.f) r.o[t][e] -= INFINITY;
-                    }
-                    vf = __builtin_bit_cast(u32x4, fin);
-                }
-            }
-            r.o[t] = Half<E>::mfma(__builtin_bit_cast(x8, vf), p[st], r.o[t]);
+            r.o[t] = Half<E>::mfma(__builtin_bit_cast(x8, v), p[st], r.o[t]);
+            __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll 1
+    for (int key = 0; key < 32 * NK; ++key)
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int d = 32 * t + 8 * j + 4 * ((threadIdx.x & 63) >> 5);
+                typedef E x4 __attribute__((ext_vector_type(4)));
+                const x4 v = *reinterpret_cast<const x4*>(vt + key * 2 * D + (((d >> 3) ^ v_swizzle<D>(key)) * 16) + (d & 7) * 2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = (float)v[i];
+                    r.o[t][4 * j + i] += key < seen && !(fabsf(x) < INFINITY) ? x : 0.f;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
 }
 
 // A workgroup's item: a row tile of a kv head on a part of the keys of its prefix or of its own.
@@ -329,6 +384,7 @@ __global__ __launch_bounds__(256, 2) void kv_attention_kernel(KvArgs a) {
         table = a.own_pages + (long)r.seq * a.own_ld;
     }
     limit = tile_limit = m;
+    int all_limit = m;                                          // keys that every row of the tile sees
     if (!prefix && a.block) {
         auto limit_of = [&](int tok) {
             const int p = m - r.n + tok;
@@ -336,8 +392,9 @@ __global__ __launch_bounds__(256, 2) void kv_attention_kernel(KvArgs a) {
         };
         limit = limit_of(token);
         tile_limit = limit_of(min(r.tile * KV_ROWS + KV_ROWS - 1, rows - 1) / a.each);     // (limits ascend with the token)
+        all_limit = limit_of(r.tile * KV_ROWS / a.each);
     }
-    const int first_limit = __builtin_amdgcn_readfirstlane(limit), last_limit = __builtin_amdgcn_readlane(limit, 31);
+    const int last_limit = __builtin_amdgcn_readlane(limit, 31);
 
     RowState<D> st;
 #pragma unroll
@@ -349,65 +406,89 @@ __global__ __launch_bounds__(256, 2) void kv_attention_kernel(KvArgs a) {
     const unsigned base = lds_offset(lds);
     const char *kb = a.k + ((long)kvh * a.k_hs + first * a.k_ts) * 2, *vb = a.v + ((long)kvh * a.v_hs + first * a.v_ts) * 2;
     const int n_tiles = (tile_limit + 63) / 64, t0 = (int)((long)n_tiles * piece / split), t1 = (int)((long)n_tiles * (piece + 1) / split);
+    // (the queries are there from here on: left to the loop, their wait would be one for the fetches that are on their way there, too)
+#pragma unroll
+    for (int i = 0; i < ST; ++i) asm volatile("" : "+v"(qf[i]));
     if (!few) {
         constexpr int N = D / 32;                               // KiB of K (and of V) per wave and tile
+        const Fetch<D, false, N, 4> fetch_k(a.k_ts, wave);
+        const Fetch<D, true, N, 4> fetch_v(a.v_ts, wave);
         Keys<64> keys{table, kb, vb, t0, 1, t1, tile_limit, 0, -1};
         KeyTile cur, nxt;
-        const bool live = wave * 32 < tile_rows;
         bool more = keys.next(a, cur);
         if (more) {
-            fetch<D, false, N, 4>(cur.k, a.k_ts, cur.n, base, wave, lane);
-            fetch<D, true, N, 4>(cur.v, a.v_ts, cur.n, base + STAGE / 2, wave, lane);
+            fetch_k(cur.k, cur.n, 64, base, wave);
+            fetch_v(cur.v, cur.n, 64, base + STAGE / 2, wave);
         }
-        for (int stage = 0; more; stage ^= 1) {
+        int stage = 0;
+        auto begin = [&]() {                                    // the present tile is there, and all have left the one before it: the next on its way into that one's place
             wait_loads<0>();
-            __syncthreads();                                    // the tile is there, and all have left the one before it
+            __syncthreads();
             more = keys.next(a, nxt);
             if (more) {
                 const unsigned to = base + (stage ^ 1) * STAGE;
-                fetch<D, false, N, 4>(nxt.k, a.k_ts, nxt.n, to, wave, lane);
-                fetch<D, true, N, 4>(nxt.v, a.v_ts, nxt.n, to + STAGE / 2, wave, lane);
+                fetch_k(nxt.k, nxt.n, 64, to, wave);
+                fetch_v(nxt.v, nxt.n, 64, to + STAGE / 2, wave);
             }
-            if (live && cur.key0 < last_limit) {
-                const char* at = lds + stage * STAGE;
-                const int seen = limit - cur.key0;
-                const bool part = first_limit < cur.key0 + 64;
-                f32x16 s[2];
-                x8 p[4];
-                scores<E, D, 2>(at, qf, s);
-                weights<E, D, 2>(st, s, a.scale, seen, part, p);
-                weigh<E, D, 2>(st, at + STAGE / 2, p, seen, part);
-            }
+        };
+        auto step = [&](auto part) {
+            constexpr bool PART = decltype(part)::value;
+            const char* at = lds + stage * STAGE;
+            const int seen = limit - cur.key0;
+            f32x16 s[2];
+            x8 p[4];
+            scores<E, D, 2>(at, qf, s);
+            weights<E, D, 2, PART>(st, s, a.scale, seen, p);
+            weigh<E, D, 2, PART>(st, at + STAGE / 2, p, seen);
+        };
+        if (wave * 32 >= tile_rows)                             // no rows: only its share of the fetches
+            while (more) { begin(); cur = nxt; stage ^= 1; }
+        // tiles that every row of the workgroup sees whole, then the others
+        if (more && cur.key0 + 64 <= all_limit) {
+            st.met = true;
+            do { begin(); step(std::false_type{}); cur = nxt; stage ^= 1; } while (more && cur.key0 + 64 <= all_limit);
+        }
+        while (more) {
+            begin();
+            if (cur.key0 < last_limit) step(std::true_type{});
             cur = nxt;
+            stage ^= 1;
         }
     } else {
         constexpr int N = D / 16;                               // KiB of K (and of V) per tile
+        const Fetch<D, false, N, 1> fetch_k(a.k_ts, 0);
+        const Fetch<D, true, N, 1> fetch_v(a.v_ts, 0);
         const char* at = lds + wave * (STAGE / 2);
         const unsigned to = base + wave * (STAGE / 2);
         Keys<32> keys{table, kb, vb, 2 * t0 + wave, 4, min(2 * t1, (tile_limit + 31) / 32), tile_limit, 0, -1};
         KeyTile cur, nxt;
         bool more = keys.next(a, cur);
         if (more) {
-            fetch<D, false, N, 1>(cur.k, a.k_ts, cur.n, to, 0, lane);
-            fetch<D, true, N, 1>(cur.v, a.v_ts, cur.n, to + STAGE / 4, 0, lane);
+            fetch_k(cur.k, cur.n, 32, to, 0);
+            fetch_v(cur.v, cur.n, 32, to + STAGE / 4, 0);
         }
-        while (more) {
+        auto step = [&](auto part) {
+            constexpr bool PART = decltype(part)::value;
             const int seen = limit - cur.key0;
-            const bool part = first_limit < cur.key0 + 32;
             more = keys.next(a, nxt);
             f32x16 s[1];
             x8 p[2];
             wait_loads<N>();
             scores<E, D, 1>(at, qf, s);
             wait_lds();
-            if (more) fetch<D, false, N, 1>(nxt.k, a.k_ts, nxt.n, to, 0, lane);
-            weights<E, D, 1>(st, s, a.scale, seen, part, p);
+            if (more) fetch_k(nxt.k, nxt.n, 32, to, 0);
+            weights<E, D, 1, PART>(st, s, a.scale, seen, p);
             if (more) wait_loads<N>(); else wait_loads<0>();
-            weigh<E, D, 1>(st, at + STAGE / 4, p, seen, part);
+            weigh<E, D, 1, PART>(st, at + STAGE / 4, p, seen);
             wait_lds();
-            if (more) fetch<D, true, N, 1>(nxt.v, a.v_ts, nxt.n, to + STAGE / 4, 0, lane);
+            if (more) fetch_v(nxt.v, nxt.n, 32, to + STAGE / 4, 0);
             cur = nxt;
+        };
+        if (more && cur.key0 + 32 <= all_limit) {
+            st.met = true;
+            do step(std::false_type{}); while (more && cur.key0 + 32 <= all_limit);
         }
+        while (more) step(std::true_type{});
         // the four waves' parts of the same rows: each brings its own to the largest maximum, then each sums a quarter of the output
         st.sum = sum_halves(st.sum);
         finish(st);
