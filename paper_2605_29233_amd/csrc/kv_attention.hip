@@ -40,40 +40,49 @@ struct KvArgs {
     int q_tokens, k_tokens, n_seq, n_groups, n_pages, own_width, prefix_width;
     int heads, kv_heads, each, block;
     float scale;                                                        // times log2(e)
-    int own_tiles, own_split, prefix_tiles, prefix_split;               // row tiles that the branches (groups) may have, parts that their keys are cut into
+    int own_tiles, own_split, prefix_tiles, prefix_split, halves;               // row tiles that the branches (groups) may have, parts that their keys are cut into
     float* part_o; float2* part_ml;                                     // [part][token][head]: unscaled output; maximum (times log2(e)) and sum.  Null: a single part
 };
 #define KV_LEAST_TILES 2                // of 64 keys, a part of a row tile's keys
 #define KV_MOST_PARTS 32
 #define KV_ROWS 128                     // rows (tokens x heads of a group) of a workgroup
 
+// Sums over the lanes up to each (in the row's order: within rows of 16, then across them).
+static __device__ __forceinline__ int lane_sums(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);     // row_shr:1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);     // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);     // row_bcast:31 into rows 2 and 3
+    return x;
+}
 // Of the sequences' row tiles the t-th: which sequence (range i of starts[step[i]] .., step null: i), its first token, its tokens, which of its tiles.  Starts are
-// taken as they come but never outside 0 .. q_tokens.
-struct RowTile { int seq, q0, n, tile; };
-static __device__ __forceinline__ bool find_tile(const KvArgs& a, const int* __restrict__ step, int ranges, int t, int each, int rows_per_tile, RowTile& r) {
+// taken as they come but never outside 0 .. q_tokens.  extra(i, x, y): two more values of the sequence, loaded with the starts.
+struct RowTile { int seq, q0, n, tile, x, y; };
+template <class F>
+static __device__ __forceinline__ bool find_tile(const KvArgs& a, const int* __restrict__ step, int ranges, int t, int each, int rows_per_tile, RowTile& r, F&& extra) {
     const int lane = threadIdx.x & 63;
     for (int b = 0; b < ranges; b += 64) {
         const int i = b + lane;
-        int s0 = 0, n = 0;
+        int s0 = 0, n = 0, x = 0, y = 0;
         if (i < ranges) {
             int i0 = i, i1 = i + 1;
             if (step) { i0 = min(max(step[i], 0), a.n_seq); i1 = min(max(step[i + 1], i0), a.n_seq); }
+            extra(i, x, y);
             s0 = min(max(a.q_starts[i0], 0), a.q_tokens);
             n = min(max(a.q_starts[i1], s0), a.q_tokens) - s0;
         }
         const int mine = (int)(((long)n * each + rows_per_tile - 1) / rows_per_tile);
-        int upto = mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int below = __shfl_up(upto, o, 64);
-            if (lane >= o) upto += below;
-        }
+        const int upto = lane_sums(mine);
         const unsigned long long hit = __ballot(upto > t);
         if (hit) {
             const int l = __builtin_ctzll(hit);
             r.seq = b + l;
             r.q0 = __builtin_amdgcn_readlane(s0, l);
             r.n = __builtin_amdgcn_readlane(n, l);
+            r.x = __builtin_amdgcn_readlane(x, l);
+            r.y = __builtin_amdgcn_readlane(y, l);
             r.tile = t - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));
             return true;
         }
@@ -92,25 +101,20 @@ static __device__ __forceinline__ bool has_group(const KvArgs& a, int seq) {
     return false;
 }
 
-// A run of keys in tiles of KEYS tokens: pages, or packed.  The ids of 64 pages at a time stand in a register's lanes: a load per tile would have to be waited for, and
-// with it every fetch on its way.  Pages that are not in the cache count as not there.
+// Keys in tiles of KEYS tokens: pages, or packed.  The ids of 64 pages at a time stand in a register's lanes: a load per tile would have to be waited for, and
+// with it every fetch on its way.  A tile past the end, or of a page that is not in the cache, has no keys (n = 0).
 struct KeyTile { const char *k, *v; int key0, n; };
 template <int KEYS> struct Keys {
     const int* table;               // null: packed
     const char *k, *v;              // of the kv head (packed: of the first key)
-    int i, step, end, m;            // the next tile, how far to the one after it, where the run ends; keys in all
+    int m;                          // keys
     int ids, ids_at;                // page ids from ids_at on (-1: none yet)
-    __device__ __forceinline__ bool next(const KvArgs& a, KeyTile& t) {
-        while (i < end) {
-            const int at = i;
-            i += step;
-            t.key0 = at * KEYS;
-            t.n = min(m - t.key0, KEYS);
-            if (!table) {
-                t.k = k + (long)t.key0 * a.k_ts * 2;
-                t.v = v + (long)t.key0 * a.v_ts * 2;
-                return true;
-            }
+    __device__ __forceinline__ KeyTile tile(const KvArgs& a, int i, int end) {
+        KeyTile t{};
+        if (i >= end) return t;
+        t.key0 = i * KEYS;
+        long k_at = (long)t.key0 * a.k_ts, v_at = (long)t.key0 * a.v_ts;
+        if (table) {
             const int page = t.key0 / BB_PAGE_TOKENS, within = t.key0 % BB_PAGE_TOKENS;
             if (ids_at < 0 || page >= ids_at + 64) {
                 ids_at = page;
@@ -118,12 +122,14 @@ template <int KEYS> struct Keys {
                 ids = p * BB_PAGE_TOKENS < m ? table[p] : -1;
             }
             const int id = __builtin_amdgcn_readlane(ids, page - ids_at);
-            if ((unsigned)id >= (unsigned)a.n_pages) continue;
-            t.k = k + ((long)id * a.k_ps + (long)within * a.k_ts) * 2;
-            t.v = v + ((long)id * a.v_ps + (long)within * a.v_ts) * 2;
-            return true;
+            if ((unsigned)id >= (unsigned)a.n_pages) return t;
+            k_at = (long)id * a.k_ps + (long)within * a.k_ts;
+            v_at = (long)id * a.v_ps + (long)within * a.v_ts;
         }
-        return false;
+        t.k = k + k_at * 2;
+        t.v = v + v_at * 2;
+        t.n = min(m - t.key0, KEYS);
+        return t;
     }
 };
 
@@ -236,7 +242,8 @@ static __device__ __forceinline__ void weights(RowState<D>& r, f32x16 (&s)[NK], 
     best = max_halves(best) * scale;
     if (__ballot(best > r.top + 8.f)) {
         best = fmaxf(best, r.top);
-        const float keep = r.top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(r.top - best);
+        // (not quite 0: an infinity in the output stays one)
+        const float keep = fmaxf(__builtin_amdgcn_exp2f(r.top - best), 1.2e-38f);
         r.sum *= keep;
 #pragma unroll
         for (int t = 0; t < D / 32; ++t)
@@ -281,68 +288,68 @@ template <class E, int D, int NK> static __device__ __forceinline__ bool any_inf
     }
     return __ballot((bad & 0x80008000u) != 0) != 0;
 }
-// O^T += V^T P^T
+// O^T += V^T P^T.  Weight 0 does not hide an infinity or a NaN that a row must not see from the product: in a tile that not every row sees whole (PART) and that holds any,
+// the product is made without them, and the rows that see them get them added, key by key.
 template <class E, int D, int NK, bool PART>
 static __device__ __forceinline__ void weigh(RowState<D>& r, const char* vt, const typename Half<E>::x8 (&p)[2 * NK], int seen) {
     typedef typename Half<E>::x8 x8;
-    if (!PART || !any_infinite<E, D, NK>(vt)) {
-        constexpr int OT = D / 32, STEPS = 2 * NK * OT;
-        x8 ring[AHEAD];
+    constexpr int OT = D / 32, STEPS = 2 * NK * OT;
+    bool bad = false;
+    if constexpr (PART) bad = any_infinite<E, D, NK>(vt);
+    x8 ring[AHEAD];
 #pragma unroll
-        for (int n = 0; n < AHEAD; ++n) ring[n] = values<E, D>(vt, n / OT, n % OT);
-        __builtin_amdgcn_sched_barrier(0);
+    for (int n = 0; n < AHEAD; ++n) ring[n] = values<E, D>(vt, n / OT, n % OT);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int n = 0; n < STEPS; ++n) {
-            r.o[n % OT] = Half<E>::mfma(ring[n % AHEAD], p[n / OT], r.o[n % OT]);
-            if (n + AHEAD < STEPS) ring[n % AHEAD] = values<E, D>(vt, (n + AHEAD) / OT, (n + AHEAD) % OT);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        return;
-    }
-    // Weight 0 does not hide an infinity or a NaN that a row must not see from the product: it is made without them, and rows that see them get them added, key by key.
-#pragma unroll
-    for (int st = 0; st < 2 * NK; ++st)
-#pragma unroll
-        for (int t = 0; t < D / 32; ++t) {
-            u32x4 v = __builtin_bit_cast(u32x4, values<E, D>(vt, st, t));
+    for (int n = 0; n < STEPS; ++n) {
+        x8 v = ring[n % AHEAD];
+        if (PART && bad) {
+            u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const unsigned bad = (v[i] & Half<E>::exponent) + Half<E>::one;
-                v[i] &= (bad & 0x8000u ? 0u : 0xFFFFu) | (bad & 0x80000000u ? 0u : 0xFFFF0000u);
+                const unsigned b = (w[i] & Half<E>::exponent) + Half<E>::one;
+                w[i] &= (b & 0x8000u ? 0u : 0xFFFFu) | (b & 0x80000000u ? 0u : 0xFFFF0000u);
             }
-            r.o[t] = Half<E>::mfma(__builtin_bit_cast(x8, v), p[st], r.o[t]);
-            __builtin_amdgcn_sched_barrier(0);
+            v = __builtin_bit_cast(x8, w);
         }
+        r.o[n % OT] = Half<E>::mfma(v, p[n / OT], r.o[n % OT]);
+        if (n + AHEAD < STEPS) ring[n % AHEAD] = values<E, D>(vt, (n + AHEAD) / OT, (n + AHEAD) % OT);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (PART && bad) {
 #pragma unroll 1
-    for (int key = 0; key < 32 * NK; ++key)
+        for (int key = 0; key < 32 * NK; ++key)
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t)
+            for (int t = 0; t < OT; ++t)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int d = 32 * t + 8 * j + 4 * ((threadIdx.x & 63) >> 5);
-                typedef E x4 __attribute__((ext_vector_type(4)));
-                const x4 v = *reinterpret_cast<const x4*>(vt + key * 2 * D + (((d >> 3) ^ v_swizzle<D>(key)) * 16) + (d & 7) * 2);
+                for (int j = 0; j < 4; ++j) {
+                    const int d = 32 * t + 8 * j + 4 * ((threadIdx.x & 63) >> 5);
+                    typedef E x4 __attribute__((ext_vector_type(4)));
+                    const x4 v = *reinterpret_cast<const x4*>(vt + key * 2 * D + (((d >> 3) ^ v_swizzle<D>(key)) * 16) + (d & 7) * 2);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float x = (float)v[i];
-                    r.o[t][4 * j + i] += key < seen && !(fabsf(x) < INFINITY) ? x : 0.f;
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = (float)v[i];
+                        r.o[t][4 * j + i] += key < seen && !(fabsf(x) < INFINITY) ? x : 0.f;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_sched_barrier(0);
-            }
+    }
 }
 
-// A workgroup's item: a row tile of a kv head on a part of the keys of its prefix or of its own.
-// A tile of more than 32 rows: the four waves take 32 each, tiles of 64 keys pass through two stages of LDS that they share, a barrier per tile.
-// Up to 32 rows: every wave has all of them and takes each fourth tile of 32 keys through a slice of LDS of its own (K of the next while it works on V of the last),
-// without barriers; the four are joined at the end, in order.
-template <class E, int D, bool PAGED>
-__global__ __launch_bounds__(256, 2) void kv_attention_kernel(KvArgs a) {
+// A workgroup's item: a row tile of a kv head on a part of the keys of its prefix or of its own.  It has HALVES times four waves.
+// A tile of more than 32 rows: a half's four waves take 32 rows each, its tiles of 64 keys (each HALVES-th) pass through two stages of LDS that they share, a barrier per tile.
+// Up to 32 rows: every wave has all of them and takes each 4 HALVES-th tile of 32 keys through a slice of LDS of its own (K of the next while it works on V of the last),
+// without barriers.  The waves of the same rows are joined at the end, in order.
+// One half, two workgroups a CU: where there are items enough (each runs on while the other waits at its barrier).  Two halves, one workgroup a CU: where there are few, so that
+// fewer parts of the keys have to be joined through memory.
+template <class E, int D, bool PAGED, int HALVES>
+__global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a) {
     typedef typename Half<E>::x8 x8;
     typedef E x4 __attribute__((ext_vector_type(4)));
-    constexpr int STAGE = 2 * 64 * D * 2, ST = D / 16, OT = D / 32;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
-    __shared__ float2 ends[4][32];                          // few rows: each wave's maximum and sum
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h2 = lane >> 5;
+    constexpr int STAGE = 2 * 64 * D * 2, ST = D / 16, OT = D / 32, WAVES = 4 * HALVES;
+    __shared__ __attribute__((aligned(1024))) char lds[HALVES * 2 * STAGE];
+    __shared__ float2 ends[WAVES][32];                      // the waves' maxima and sums
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h2 = lane >> 5, half = wave >> 2, w4 = wave & 3;
 
     // Which item: the keys' parts of all kv heads are dealt to the XCDs (workgroups go to them round robin), so that the row tiles of one share an L2; last row tiles, which see
     // the most keys, first.
@@ -354,12 +361,14 @@ __global__ __launch_bounds__(256, 2) void kv_attention_kernel(KvArgs a) {
     const int g8 = min(chunks & -chunks, 8), per = chunks / g8, j = lin / g8;
     const int chunk = lin % g8 + g8 * (j % per), kvh = chunk / split, piece = chunk - kvh * split;
     RowTile r;
-    if (!find_tile(a, prefix ? a.group_starts : nullptr, prefix ? a.n_groups : a.n_seq, tiles - 1 - j / per, a.each, KV_ROWS, r)) return;
+    const int* lens = PAGED ? prefix ? a.prefix_lens : a.own_lens : a.k_starts;
+    if (!find_tile(a, prefix ? a.group_starts : nullptr, prefix ? a.n_groups : a.n_seq, tiles - 1 - j / per, a.each, KV_ROWS, r, [&](int i, int& x, int& y) { x = lens[i]; if (!PAGED) y = lens[i + 1]; }))
+        return;
 
     // the lane's row
     const int rows = r.n * a.each, tile_rows = min(rows - r.tile * KV_ROWS, KV_ROWS);
     const bool few = tile_rows <= 32;
-    const int row = r.tile * KV_ROWS + (few ? 0 : wave * 32) + (lane & 31), row_in = min(row, rows - 1);
+    const int row = r.tile * KV_ROWS + (few ? 0 : w4 * 32) + (lane & 31), row_in = min(row, rows - 1);
     const int token = row_in / a.each, head = kvh * a.each + row_in - token * a.each;
     x8 qf[ST];
     {
@@ -373,15 +382,11 @@ __global__ __launch_bounds__(256, 2) void kv_attention_kernel(KvArgs a) {
     int m, limit, tile_limit;
     long first = 0;
     if (!PAGED) {
-        const int s0 = min(max(a.k_starts[r.seq], 0), a.k_tokens);
-        m = __builtin_amdgcn_readfirstlane(min(max(a.k_starts[r.seq + 1], s0), a.k_tokens) - s0);
-        first = __builtin_amdgcn_readfirstlane(s0);
-    } else if (prefix) {
-        m = __builtin_amdgcn_readfirstlane(min(max(a.prefix_lens[r.seq], 0), (int)min((long)a.prefix_width * BB_PAGE_TOKENS, 0x7FFFFFC0L)));
-        table = a.prefix_pages + (long)r.seq * a.prefix_ld;
+        first = min(max(r.x, 0), a.k_tokens);
+        m = min(max(r.y, (int)first), a.k_tokens) - (int)first;
     } else {
-        m = __builtin_amdgcn_readfirstlane(min(max(a.own_lens[r.seq], 0), (int)min((long)a.own_width * BB_PAGE_TOKENS, 0x7FFFFFC0L)));
-        table = a.own_pages + (long)r.seq * a.own_ld;
+        m = min(max(r.x, 0), (int)min((long)(prefix ? a.prefix_width : a.own_width) * BB_PAGE_TOKENS, 0x7FFFFFC0L));
+        table = prefix ? a.prefix_pages + (long)r.seq * a.prefix_ld : a.own_pages + (long)r.seq * a.own_ld;
     }
     limit = tile_limit = m;
     int all_limit = m;                                          // keys that every row of the tile sees
@@ -406,53 +411,67 @@ __global__ __launch_bounds__(256, 2) void kv_attention_kernel(KvArgs a) {
     const unsigned base = lds_offset(lds);
     const char *kb = a.k + ((long)kvh * a.k_hs + first * a.k_ts) * 2, *vb = a.v + ((long)kvh * a.v_hs + first * a.v_ts) * 2;
     const int n_tiles = (tile_limit + 63) / 64, t0 = (int)((long)n_tiles * piece / split), t1 = (int)((long)n_tiles * (piece + 1) / split);
-    // (the queries are there from here on: left to the loop, their wait would be one for the fetches that are on their way there, too)
+    // The queries have to be there before the loop: left to it, their wait would be one for the fetches that are on their way there, too.
+    auto have_queries = [&]() {
 #pragma unroll
-    for (int i = 0; i < ST; ++i) asm volatile("" : "+v"(qf[i]));
+        for (int i = 0; i < ST; ++i) asm volatile("" : "+v"(qf[i]));
+    };
     if (!few) {
         constexpr int N = D / 32;                               // KiB of K (and of V) per wave and tile
-        const Fetch<D, false, N, 4> fetch_k(a.k_ts, wave);
-        const Fetch<D, true, N, 4> fetch_v(a.v_ts, wave);
-        Keys<64> keys{table, kb, vb, t0, 1, t1, tile_limit, 0, -1};
-        KeyTile cur, nxt;
-        bool more = keys.next(a, cur);
-        if (more) {
-            fetch_k(cur.k, cur.n, 64, base, wave);
-            fetch_v(cur.v, cur.n, 64, base + STAGE / 2, wave);
-        }
-        int stage = 0;
-        auto begin = [&]() {                                    // the present tile is there, and all have left the one before it: the next on its way into that one's place
-            wait_loads<0>();
-            __syncthreads();
-            more = keys.next(a, nxt);
-            if (more) {
-                const unsigned to = base + (stage ^ 1) * STAGE;
-                fetch_k(nxt.k, nxt.n, 64, to, wave);
-                fetch_v(nxt.v, nxt.n, 64, to + STAGE / 2, wave);
-            }
+        const Fetch<D, false, N, 4> fetch_k(a.k_ts, w4);
+        const Fetch<D, true, N, 4> fetch_v(a.v_ts, w4);
+        Keys<64> keys{table, kb, vb, tile_limit, 0, -1};
+        const char* mine = lds + half * 2 * STAGE;
+        const unsigned to = base + half * 2 * STAGE;
+        auto fetch = [&](const KeyTile& t, int stage) {
+            if (t.n == 0) return;
+            fetch_k(t.k, t.n, 64, to + stage * STAGE, w4);
+            fetch_v(t.v, t.n, 64, to + stage * STAGE + STAGE / 2, w4);
         };
-        auto step = [&](auto part) {
+        KeyTile cur = keys.tile(a, t0 + half, t1), nxt;
+        fetch(cur, 0);
+        have_queries();
+        const bool live = w4 * 32 < tile_rows;
+        const int n_whole = min(max(all_limit / 64 - t0, 0), t1 - t0) / HALVES, n_all = (t1 - t0 + HALVES - 1) / HALVES;    // rounds: of tiles that every row sees whole, all
+        int i = 0;
+        auto round = [&](auto part) {
             constexpr bool PART = decltype(part)::value;
-            const char* at = lds + stage * STAGE;
-            const int seen = limit - cur.key0;
-            f32x16 s[2];
-            x8 p[4];
-            scores<E, D, 2>(at, qf, s);
-            weights<E, D, 2, PART>(st, s, a.scale, seen, p);
-            weigh<E, D, 2, PART>(st, at + STAGE / 2, p, seen);
-        };
-        if (wave * 32 >= tile_rows)                             // no rows: only its share of the fetches
-            while (more) { begin(); cur = nxt; stage ^= 1; }
-        // tiles that every row of the workgroup sees whole, then the others
-        if (more && cur.key0 + 64 <= all_limit) {
-            st.met = true;
-            do { begin(); step(std::false_type{}); cur = nxt; stage ^= 1; } while (more && cur.key0 + 64 <= all_limit);
-        }
-        while (more) {
-            begin();
-            if (cur.key0 < last_limit) step(std::true_type{});
+            wait_loads<0>();
+            __syncthreads();                                    // the round's tiles are there, and all have left those before them: the next on their way into their place
+            nxt = keys.tile(a, t0 + half + (i + 1) * HALVES, t1);
+            fetch(nxt, i + 1 & 1);
+            if (live && cur.n && (!PART || cur.key0 < last_limit)) {
+                const char* at = mine + (i & 1) * STAGE;
+                const int seen = limit - cur.key0;
+                f32x16 s[2];
+                x8 p[4];
+                if (!PART) st.met = true;
+                scores<E, D, 2>(at, qf, s);
+                weights<E, D, 2, PART>(st, s, a.scale, seen, p);
+                weigh<E, D, 2, PART>(st, at + STAGE / 2, p, seen);
+            }
             cur = nxt;
-            stage ^= 1;
+        };
+        for (; i < n_whole; ++i) round(std::false_type{});
+        for (; i < n_all; ++i) round(std::true_type{});
+        st.sum = sum_halves(st.sum);
+        finish(st);
+        if constexpr (HALVES == 2) {
+            __syncthreads();
+            float* other = (float*)(lds + 2 * STAGE) + w4 * 16 * OT * 64;
+            if (half) {
+                if (h2 == 0) ends[wave][lane] = make_float2(st.top, st.sum);
+#pragma unroll
+                for (int e = 0; e < 16 * OT; ++e) other[e * 64 + lane] = st.o[e >> 4][e & 15];
+            }
+            __syncthreads();
+            if (half) return;
+            const float2 theirs = ends[wave + 4][lane & 31];
+            const float top = fmaxf(st.top, theirs.x), keep = rescale(st.top, top), take = rescale(theirs.x, top);
+#pragma unroll
+            for (int e = 0; e < 16 * OT; ++e) st.o[e >> 4][e & 15] = st.o[e >> 4][e & 15] * keep + other[e * 64 + lane] * take;
+            st.sum = st.sum * keep + theirs.y * take;
+            st.top = top;
         }
     } else {
         constexpr int N = D / 16;                               // KiB of K (and of V) per tile
@@ -460,68 +479,70 @@ __global__ __launch_bounds__(256, 2) void kv_attention_kernel(KvArgs a) {
         const Fetch<D, true, N, 1> fetch_v(a.v_ts, 0);
         const char* at = lds + wave * (STAGE / 2);
         const unsigned to = base + wave * (STAGE / 2);
-        Keys<32> keys{table, kb, vb, 2 * t0 + wave, 4, min(2 * t1, (tile_limit + 31) / 32), tile_limit, 0, -1};
-        KeyTile cur, nxt;
-        bool more = keys.next(a, cur);
-        if (more) {
+        Keys<32> keys{table, kb, vb, tile_limit, 0, -1};
+        const int end = min(2 * t1, (tile_limit + 31) / 32);
+        int i = 2 * t0 + wave;
+        auto next = [&]() {                                     // (tiles without keys are passed over)
+            KeyTile t{};
+            while (i < end && t.n == 0) { t = keys.tile(a, i, end); i += WAVES; }
+            return t;
+        };
+        KeyTile cur = next(), nxt;
+        if (cur.n) {
             fetch_k(cur.k, cur.n, 32, to, 0);
             fetch_v(cur.v, cur.n, 32, to + STAGE / 4, 0);
         }
+        have_queries();
         auto step = [&](auto part) {
             constexpr bool PART = decltype(part)::value;
             const int seen = limit - cur.key0;
-            more = keys.next(a, nxt);
+            nxt = next();
             f32x16 s[1];
             x8 p[2];
+            if (!PART) st.met = true;
             wait_loads<N>();
             scores<E, D, 1>(at, qf, s);
             wait_lds();
-            if (more) fetch_k(nxt.k, nxt.n, 32, to, 0);
+            if (nxt.n) fetch_k(nxt.k, nxt.n, 32, to, 0);
             weights<E, D, 1, PART>(st, s, a.scale, seen, p);
-            if (more) wait_loads<N>(); else wait_loads<0>();
+            if (nxt.n) wait_loads<N>(); else wait_loads<0>();
             weigh<E, D, 1, PART>(st, at + STAGE / 4, p, seen);
             wait_lds();
-            if (more) fetch_v(nxt.v, nxt.n, 32, to + STAGE / 4, 0);
+            if (nxt.n) fetch_v(nxt.v, nxt.n, 32, to + STAGE / 4, 0);
             cur = nxt;
         };
-        if (more && cur.key0 + 32 <= all_limit) {
-            st.met = true;
-            do step(std::false_type{}); while (more && cur.key0 + 32 <= all_limit);
-        }
-        while (more) step(std::true_type{});
-        // the four waves' parts of the same rows: each brings its own to the largest maximum, then each sums a quarter of the output
+        while (cur.n && cur.key0 + 32 <= all_limit) step(std::false_type{});
+        while (cur.n) step(std::true_type{});
+        // the waves' parts of the same rows: each brings its own to the largest maximum, then each sums its share of the output
         st.sum = sum_halves(st.sum);
         finish(st);
         if (h2 == 0) ends[wave][lane] = make_float2(st.top, st.sum);
         __syncthreads();
         float top = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, ends[w][lane & 31].x);
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ends[w][lane & 31].x);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) sum += ends[w][lane & 31].y * rescale(ends[w][lane & 31].x, top);
+        for (int w = 0; w < WAVES; ++w) sum += ends[w][lane & 31].y * rescale(ends[w][lane & 31].x, top);
         const float keep = rescale(st.top, top);
         float* all = (float*)lds;
 #pragma unroll
-        for (int t = 0; t < OT; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) all[((wave * OT + t) * 16 + e) * 64 + lane] = st.o[t][e] * keep;
+        for (int e = 0; e < 16 * OT; ++e) all[(wave * OT * 16 + e) * 64 + lane] = st.o[e >> 4][e & 15] * keep;
         __syncthreads();
         st.top = top; st.sum = sum;
 #pragma unroll
-        for (int e = 0; e < 4 * OT; ++e) {
+        for (int e = 0; e < 16 * OT / WAVES; ++e) {
             float x = 0.f;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) x += all[(w * OT * 16 + wave * 4 * OT + e) * 64 + lane];
+            for (int w = 0; w < WAVES; ++w) x += all[(w * OT * 16 + wave * (16 * OT / WAVES) + e) * 64 + lane];
             st.o[e >> 4][e & 15] = x;
         }
     }
 
     // out, or the part's share of it: a lane has runs of four elements of its row
-    if (!few) { st.sum = sum_halves(st.sum); finish(st); }
     const bool alone = PAGED && !prefix && piece == 0 && a.prefix_split && !has_group(a, r.seq);      // (all lanes look)
     if (row >= rows) return;
     const long at_row = (long)(r.q0 + token) * a.heads + head;
-    const int groups = few ? OT : 4 * OT, g0 = few ? wave * OT : 0;
+    const int groups = few ? 4 * OT / WAVES : 4 * OT, g0 = few ? wave * (4 * OT / WAVES) : 0;
     auto store = [&](auto&& put) {
 #pragma unroll
         for (int i = 0; i < 4 * OT; ++i)
@@ -556,7 +577,7 @@ template <class E, int D> __global__ __launch_bounds__(256) void kv_join_kernel(
     __shared__ float4 outs[JOIN_WAYS][ROWS][LANES];
     __shared__ float sums[JOIN_WAYS][ROWS];
     RowTile r;
-    if (!find_tile(a, nullptr, a.n_seq, blockIdx.x, a.heads, ROWS, r)) return;
+    if (!find_tile(a, nullptr, a.n_seq, blockIdx.x, a.heads, ROWS, r, [](int, int&, int&) {})) return;
     const int rows = r.n * a.heads, n_parts = a.prefix_split + a.own_split;
     const int l = threadIdx.x % LANES, i = threadIdx.x / LANES % ROWS, way = threadIdx.x / LANES / ROWS, row = r.tile * ROWS + i;
     const long parts = (long)a.q_tokens * a.heads, at = (long)r.q0 * a.heads + min(row, rows - 1);
@@ -589,17 +610,15 @@ template <class E, int D> __global__ __launch_bounds__(256) void kv_join_kernel(
     if (a.lse && l == 0) a.lse[at] = log_sum(top, sum);
 }
 
-template <class E, bool PAGED> static void launch_kv(const KvArgs& a, int head_dim, hipStream_t s) {
+template <class E, int D, bool PAGED> static void launch_kv(const KvArgs& a, hipStream_t s) {
     const unsigned grid = (unsigned)((a.prefix_tiles * (long)a.prefix_split + a.own_tiles * (long)a.own_split) * a.kv_heads);
-    const int join_rows = 256 / (head_dim / 4) / JOIN_WAYS;
-    const unsigned join = (unsigned)(((long)a.q_tokens * a.heads + (join_rows - 1) * (long)a.n_seq) / join_rows);
-    if (head_dim == 128) {
-        kv_attention_kernel<E, 128, PAGED><<<grid, 256, 0, s>>>(a);
-        if (a.part_o) kv_join_kernel<E, 128><<<join, 256, 0, s>>>(a);
-    } else {
-        kv_attention_kernel<E, 64, PAGED><<<grid, 256, 0, s>>>(a);
-        if (a.part_o) kv_join_kernel<E, 64><<<join, 256, 0, s>>>(a);
-    }
+    if (a.halves == 2) kv_attention_kernel<E, D, PAGED, 2><<<grid, 512, 0, s>>>(a); else kv_attention_kernel<E, D, PAGED, 1><<<grid, 256, 0, s>>>(a);
+    constexpr int ROWS = 256 / (D / 4) / JOIN_WAYS;
+    if (a.part_o) kv_join_kernel<E, D><<<(unsigned)(((long)a.q_tokens * a.heads + (ROWS - 1) * (long)a.n_seq) / ROWS), 256, 0, s>>>(a);
+}
+template <bool PAGED> static void launch_kv(const KvArgs& a, int type, int head_dim, hipStream_t s) {
+    if (type == BB_BF16) head_dim == 128 ? launch_kv<__bf16, 128, PAGED>(a, s) : launch_kv<__bf16, 64, PAGED>(a, s);
+    else head_dim == 128 ? launch_kv<half_t, 128, PAGED>(a, s) : launch_kv<half_t, 64, PAGED>(a, s);
 }
 
 static bool refuse_attention(long q_tokens, int n_seq, int heads, int kv_heads, int head_dim, int type, int block, float scale) {
@@ -615,19 +634,23 @@ static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim)
     const long own_like = std::max(1L, a.n_seq * ((rows / a.n_seq + KV_ROWS - 1) / KV_ROWS)), pre_like = pre ? std::max(1L, a.n_groups * ((rows / a.n_groups + KV_ROWS - 1) / KV_ROWS)) : 0;
     const long own_cols = std::max(1L, (own_keys + 63) / 64), pre_cols = std::max(1L, (prefix_keys + 63) / 64);
     // us: a row tile on 64 keys where two workgroups share a CU / where one has it, what an item takes besides, the join's launch and its bytes per us
-    const double both = 2.2, alone = 1.4, item = 2.0, join = 4.0, join_bytes = 3e6;
+    const double both = 2.0, alone = 1.3, item = 2.5, join = 3.0, join_bytes = 3e6;
     const long most = std::max(own_cols, pre_cols);
     long own_parts = 1, pre_parts = pre ? 1 : 0;
     double best = 0;
-    for (long c = most, last = 0; c >= 1 && (c >= KV_LEAST_TILES || c == most); c = c * 7 / 8) {
-        const long op = std::min<long>((own_cols + c - 1) / c, KV_MOST_PARTS), pp = pre ? std::min<long>((pre_cols + c - 1) / c, KV_MOST_PARTS) : 0;
-        if (op + pp == last) continue;
-        last = op + pp;
-        const double oc = (double)((own_cols + op - 1) / op), pc = pp ? (double)((pre_cols + pp - 1) / pp) : 0, oi = (double)own_like * op * a.kv_heads, pi = (double)pre_like * pp * a.kv_heads;
-        const double u = oi + pi > 256 ? both : alone, all = (oi * (item + oc * u) + pi * (item + pc * u)) / (oi + pi > 256 ? 512 : 256);
-        const double cost = std::max(all, item + u * std::max(oc, pc)) + (op + pp > 1 ? join + (double)rows * a.kv_heads * (op + pp) * head_dim * 8 / join_bytes : 0);
-        if (best == 0 || cost < best) { best = cost; own_parts = op; pre_parts = pp; }
-    }
+    a.halves = 1;
+    for (int halves = 1; halves <= 2; ++halves)
+        for (long c = most, last = 0; c >= 1 && (c >= KV_LEAST_TILES || c == most); c = c * 7 / 8) {
+            const long op = std::min<long>((own_cols + c - 1) / c, KV_MOST_PARTS), pp = pre ? std::min<long>((pre_cols + c - 1) / c, KV_MOST_PARTS) : 0;
+            if (op + pp == last) continue;
+            last = op + pp;
+            auto rounds = [&](long cols, long parts) { return (double)(((cols + parts - 1) / parts + halves - 1) / halves); };
+            const double oc = rounds(own_cols, op), pc = pp ? rounds(pre_cols, pp) : 0, oi = (double)own_like * op * a.kv_heads, pi = (double)pre_like * pp * a.kv_heads;
+            const bool full = halves == 2 || oi + pi > 256;
+            const double u = full ? both : alone, all = (oi * (item + oc * u) + pi * (item + pc * u)) / (halves == 1 && full ? 512 : 256);
+            const double cost = std::max(all, item + u * std::max(oc, pc)) + (op + pp > 1 ? join + (double)rows * a.kv_heads * (op + pp) * head_dim * 8 / join_bytes : 0);
+            if (best == 0 || cost < best) { best = cost; own_parts = op; pre_parts = pp; a.halves = halves; }
+        }
     if ((own * own_parts + pre * pre_parts) * a.kv_heads > 0x7FFFFFFF || ((long)a.q_tokens * a.heads + 3L * a.n_seq) / 2 > 0x7FFFFFFF) return false;
     a.own_tiles = (int)own; a.own_split = (int)own_parts; a.prefix_tiles = (int)pre; a.prefix_split = (int)pre_parts;
     return true;
@@ -680,7 +703,7 @@ extern "C" int bb_attention(const void* q_dev, long q_token, long q_head, const 
     a.kv_heads = kv_heads;
     if (!plan_parts(a, k_tokens / n_seq, 0, head_dim)) return BB_EINVAL;
     if (const int rc = place_parts(a, head_dim, workspace_dev, workspace_bytes)) return rc;
-    if (type == BB_BF16) launch_kv<__bf16, false>(a, head_dim, (hipStream_t)hip_stream); else launch_kv<half_t, false>(a, head_dim, (hipStream_t)hip_stream);
+    launch_kv<false>(a, type, head_dim, (hipStream_t)hip_stream);
     return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
 }
 
@@ -717,6 +740,6 @@ extern "C" int bb_shared_attention(const void* q_dev, long q_token, long q_head,
     a.kv_heads = kv_heads;
     if (!plan_parts(a, 64L * own_width, n_groups ? 64L * prefix_width : 0, head_dim)) return BB_EINVAL;
     if (const int rc = place_parts(a, head_dim, workspace_dev, workspace_bytes)) return rc;
-    if (type == BB_BF16) launch_kv<__bf16, true>(a, head_dim, (hipStream_t)hip_stream); else launch_kv<half_t, true>(a, head_dim, (hipStream_t)hip_stream);
+    launch_kv<true>(a, type, head_dim, (hipStream_t)hip_stream);
     return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
 }
