@@ -157,10 +157,12 @@ template <int D, bool V, int N, int STEP> struct Fetch {
     }
     // a tile that ends early: rows past its end as its last one
     __device__ __forceinline__ void some(const char* src, int n, unsigned lds, int first) const {
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));                          // (not worth registers through the loop)
 #pragma unroll
         for (int u = 0; u < N; ++u) {
-            const int row = (u * STEP + first) * ROWS + (int)(threadIdx.x & 63) / PER;
-            load_to_lds<0>(src, (unsigned)min(row, n - 1) * (unsigned)ts2 + piece_of(row), lds + (u * STEP + first) * 1024);
+            const int row = (u * STEP + first) * ROWS + lane / PER;
+            load_to_lds<0>(src, (unsigned)min(row, n - 1) * (unsigned)ts2 + (unsigned)((lane % PER ^ (V ? v_swizzle<D>(row) : k_swizzle<D>(row))) * 16), lds + (u * STEP + first) * 1024);
         }
     }
     __device__ __forceinline__ void operator()(const char* src, int n, int keys, unsigned lds, int first) const {
@@ -195,36 +197,40 @@ template <int D> static __device__ __forceinline__ void finish(RowState<D>& r) {
     if (r.met && r.top == -INFINITY && r.sum == 0.f) r.top = -3e38f;
 }
 
+// LDS by its byte offset.
+template <class T> static __device__ __forceinline__ T lds_at(unsigned offset) { return *(__attribute__((address_space(3))) const T*)(size_t)offset; }
+// Where a lane's pieces of a tile lie, from the tile's first byte on: of K (row lane % 32, d = 8 (lane / 32) on) and of V (four keys' d, see values()).  The pieces of the d further on are
+// an exclusive or with a constant away, those of the rows further on a sum.
+template <int D> static __device__ __forceinline__ unsigned k_piece() {
+    const int lane = threadIdx.x & 63, row = lane & 31;
+    return row * 2 * D + ((lane >> 5 ^ k_swizzle<D>(row)) * 16);
+}
+template <int D> static __device__ __forceinline__ unsigned v_piece() {
+    const int lane = threadIdx.x & 63, key = 4 * (lane >> 5) + (lane >> 2 & 3), d = (lane >> 4 & 1) * 16 + (lane & 3) * 4;
+    return key * 2 * D + (((d >> 3) ^ v_swizzle<D>(key)) * 16) + (d & 7) * 2;
+}
 // Operands that are on their way from LDS while the matrix cores work; the order is fixed by hand, as the compiler would bring all of them first and spill.
 #define AHEAD 4
-// S^T of 32 NK keys and the wave's 32 rows.
-template <class E, int D, int NK> static __device__ __forceinline__ void scores(const char* kt, const typename Half<E>::x8 (&qf)[D / 16], f32x16 (&s)[NK]) {
+// Step n of a tile's scores: 16 d (16 (n / NK) on) of 32 keys (32 (n % NK) on).
+template <class X8, int D, int NK> static __device__ __forceinline__ X8 key_piece(unsigned kp, unsigned at, int n) { return lds_at<X8>((kp ^ 32 * (n / NK)) + at + n % NK * 64 * D); }
+// S^T of 32 NK keys (at LDS offset `at`) and the wave's 32 rows.  kp: k_piece.
+template <class E, int D, int NK> static __device__ __forceinline__ void scores(unsigned kp, unsigned at, const typename Half<E>::x8 (&qf)[D / 16], f32x16 (&s)[NK]) {
     typedef typename Half<E>::x8 x8;
-    const int lane = threadIdx.x & 63, h2 = lane >> 5;
     constexpr int STEPS = NK * (D / 16);
     x8 ring[AHEAD];
-    auto piece = [&](int n) {                               // step n: 16 d (16 (n / NK) on) of 32 keys (32 (n % NK) on)
-        const int kr = 32 * (n % NK) + (lane & 31);
-        return *reinterpret_cast<const x8*>(kt + kr * 2 * D + (((2 * (n / NK) + h2) ^ k_swizzle<D>(kr)) * 16));
-    };
 #pragma unroll
-    for (int n = 0; n < AHEAD; ++n) ring[n] = piece(n);
-#pragma unroll
-    for (int i = 0; i < NK; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[i][e] = 0.f;
+    for (int n = 0; n < AHEAD; ++n) ring[n] = key_piece<x8, D, NK>(kp, at, n);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int n = 0; n < STEPS; ++n) {
-        s[n % NK] = Half<E>::mfma(ring[n % AHEAD], qf[n / NK], s[n % NK]);
-        if (n + AHEAD < STEPS) ring[n % AHEAD] = piece(n + AHEAD);
+        s[n % NK] = Half<E>::mfma(ring[n % AHEAD], qf[n / NK], n < NK ? f32x16{} : s[n % NK]);
+        if (n + AHEAD < STEPS) ring[n % AHEAD] = key_piece<x8, D, NK>(kp, at, n + AHEAD);
         __builtin_amdgcn_sched_barrier(0);
     }
 }
-// Scores -> weights p in the operands' type.  PART: not every row sees all of the tile's keys; seen: how many of them the lane's row does.
-// The maximum follows only when it would grow by more than 2^8: a weight is then at most that, of no less precision, and the output is seldom scaled.
-template <class E, int D, int NK, bool PART>
-static __device__ __forceinline__ void weights(RowState<D>& r, f32x16 (&s)[NK], float scale, int seen, typename Half<E>::x8 (&p)[2 * NK]) {
+// The rows' maxima follow a tile's scores.  PART: not every row sees all of the tile's keys; seen: how many of them the lane's row does.
+// They follow only by more than 8 (of 2^8): a weight is then at most that, of no less precision, and the output is seldom scaled.
+template <int D, int NK, bool PART> static __device__ __forceinline__ void follow(RowState<D>& r, f32x16 (&s)[NK], float scale, int seen) {
     const int h2 = (threadIdx.x & 63) >> 5;
     if (PART) {
         r.met |= seen > 0;
@@ -251,37 +257,42 @@ static __device__ __forceinline__ void weights(RowState<D>& r, f32x16 (&s)[NK], 
             for (int e = 0; e < 16; ++e) r.o[t][e] *= keep;
         r.top = best;
     }
-    const float from = r.top == -INFINITY ? 0.f : r.top;        // (no key seen yet, or only scores of -inf: every weight 0)
-    float sum = 0.f, sum2 = 0.f;
-#pragma unroll
-    for (int i = 0; i < NK; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], scale, -from));
-            if (e & 1) sum2 += w; else sum += w;
-            p[2 * i + (e >> 3)][e & 7] = (E)w;
-        }
-    r.sum += sum + sum2;
 }
-// V^T of 16 keys (from 16 st on) and 32 d (from 32 t on), in the order of the weights.
-template <class E, int D> static __device__ __forceinline__ typename Half<E>::x8 values(const char* vt, int st, int t) {
-    const int lane = threadIdx.x & 63, d = 32 * t + (lane >> 4 & 1) * 16 + (lane & 3) * 4;
+// What the exponents start from (-inf: no key seen yet, or only scores of -inf: every weight 0).
+template <int D> static __device__ __forceinline__ float from_of(const RowState<D>& r) { return r.top == -INFINITY ? 0.f : r.top; }
+// Scores -> weights p in the operands' type, elements FROM to TO of all 16 NK.
+template <class E, int NK, int FROM, int TO>
+static __device__ __forceinline__ void weights(const f32x16 (&s)[NK], float scale, float from, float (&sum)[2], typename Half<E>::x8 (&p)[2 * NK]) {
+#pragma unroll
+    for (int n = FROM; n < TO; ++n) {
+        const int i = n >> 4, e = n & 15;
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], scale, -from));
+        sum[n & 1] += w;
+        p[n >> 3][n & 7] = (E)w;
+    }
+}
+template <class E, int D, int NK, bool PART>
+static __device__ __forceinline__ void weights(RowState<D>& r, f32x16 (&s)[NK], float scale, int seen, typename Half<E>::x8 (&p)[2 * NK]) {
+    follow<D, NK, PART>(r, s, scale, seen);
+    float sum[2] = {0.f, 0.f};
+    weights<E, NK, 0, 16 * NK>(s, scale, from_of(r), sum, p);
+    r.sum += sum[0] + sum[1];
+}
+// V^T of 16 keys (from 16 st on) and 32 d (from 32 t on), in the order of the weights.  vp: v_piece.
+template <class E, int D> static __device__ __forceinline__ typename Half<E>::x8 values(unsigned vp, unsigned at, int st, int t) {
     s16x4 f[2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const int key = 16 * st + 8 * u + 4 * (lane >> 5) + (lane >> 2 & 3);
-        f[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + key * 2 * D + (((d >> 3) ^ v_swizzle<D>(key)) * 16) + (d & 7) * 2));
-    }
+    for (int u = 0; u < 2; ++u) f[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(size_t)((vp ^ 64 * t) + at + (16 * st + 8 * u) * 2 * D));
     typename Half<E>::x8 v;
     __builtin_memcpy(&v, f, 16);
     return v;
 }
 // Whether a tile of V holds an infinity or a NaN.
-template <class E, int D, int NK> static __device__ __forceinline__ bool any_infinite(const char* vt) {
+template <class E, int D, int NK> static __device__ __forceinline__ bool any_infinite(unsigned at) {
     unsigned bad = 0;
 #pragma unroll
     for (int i = 0; i < NK * D / 16; ++i) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(vt + i * 1024 + (threadIdx.x & 63) * 16);
+        const u32x4 x = lds_at<u32x4>(at + i * 1024 + (threadIdx.x & 63) * 16);
 #pragma unroll
         for (int j = 0; j < 4; ++j) bad |= (x[j] & Half<E>::exponent) + Half<E>::one;
         if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);          // (no more registers than that)
@@ -289,16 +300,17 @@ template <class E, int D, int NK> static __device__ __forceinline__ bool any_inf
     return __ballot((bad & 0x80008000u) != 0) != 0;
 }
 // O^T += V^T P^T.  Weight 0 does not hide an infinity or a NaN that a row must not see from the product: in a tile that not every row sees whole (PART) and that holds any,
-// the product is made without them, and the rows that see them get them added, key by key.
+// the product is made without them, and the rows that see them get them added, key by key (tile: the LDS offset of the tile as a whole).
 template <class E, int D, int NK, bool PART>
-static __device__ __forceinline__ void weigh(RowState<D>& r, const char* vt, const typename Half<E>::x8 (&p)[2 * NK], int seen) {
+static __device__ __forceinline__ void weigh(RowState<D>& r, unsigned vp, unsigned at, const typename Half<E>::x8 (&p)[2 * NK], int seen, unsigned tile) {
     typedef typename Half<E>::x8 x8;
     constexpr int OT = D / 32, STEPS = 2 * NK * OT;
+    asm volatile("" : "+v"(vp));
     bool bad = false;
-    if constexpr (PART) bad = any_infinite<E, D, NK>(vt);
+    if constexpr (PART) bad = any_infinite<E, D, NK>(tile);
     x8 ring[AHEAD];
 #pragma unroll
-    for (int n = 0; n < AHEAD; ++n) ring[n] = values<E, D>(vt, n / OT, n % OT);
+    for (int n = 0; n < AHEAD; ++n) ring[n] = values<E, D>(vp, at, n / OT, n % OT);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int n = 0; n < STEPS; ++n) {
@@ -313,7 +325,7 @@ static __device__ __forceinline__ void weigh(RowState<D>& r, const char* vt, con
             v = __builtin_bit_cast(x8, w);
         }
         r.o[n % OT] = Half<E>::mfma(v, p[n / OT], r.o[n % OT]);
-        if (n + AHEAD < STEPS) ring[n % AHEAD] = values<E, D>(vt, (n + AHEAD) / OT, (n + AHEAD) % OT);
+        if (n + AHEAD < STEPS) ring[n % AHEAD] = values<E, D>(vp, at, (n + AHEAD) / OT, (n + AHEAD) % OT);
         __builtin_amdgcn_sched_barrier(0);
     }
     if (PART && bad) {
@@ -325,7 +337,7 @@ static __device__ __forceinline__ void weigh(RowState<D>& r, const char* vt, con
                 for (int j = 0; j < 4; ++j) {
                     const int d = 32 * t + 8 * j + 4 * ((threadIdx.x & 63) >> 5);
                     typedef E x4 __attribute__((ext_vector_type(4)));
-                    const x4 v = *reinterpret_cast<const x4*>(vt + key * 2 * D + (((d >> 3) ^ v_swizzle<D>(key)) * 16) + (d & 7) * 2);
+                    const x4 v = lds_at<x4>(tile + key * 2 * D + (((d >> 3) ^ v_swizzle<D>(key)) * 16) + (d & 7) * 2);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float x = (float)v[i];
@@ -349,6 +361,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
     constexpr int STAGE = 2 * 64 * D * 2, ST = D / 16, OT = D / 32, WAVES = 4 * HALVES;
     __shared__ __attribute__((aligned(1024))) char lds[HALVES * 2 * STAGE];
     __shared__ float2 ends[WAVES][32];                      // the waves' maxima and sums
+    __shared__ long places[4][32];                          // where a wave's rows go (-1: nowhere)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h2 = lane >> 5, half = wave >> 2, w4 = wave & 3;
 
     // Which item: the keys' parts of all kv heads are dealt to the XCDs (workgroups go to them round robin), so that the row tiles of one share an L2; last row tiles, which see
@@ -421,8 +434,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
         const Fetch<D, false, N, 4> fetch_k(a.k_ts, w4);
         const Fetch<D, true, N, 4> fetch_v(a.v_ts, w4);
         Keys<64> keys{table, kb, vb, tile_limit, 0, -1};
-        const char* mine = lds + half * 2 * STAGE;
-        const unsigned to = base + half * 2 * STAGE;
+        const unsigned to = base + half * 2 * STAGE, kp = k_piece<D>(), vp = v_piece<D>();
         auto fetch = [&](const KeyTile& t, int stage) {
             if (t.n == 0) return;
             fetch_k(t.k, t.n, 64, to + stage * STAGE, w4);
@@ -441,14 +453,14 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
             nxt = keys.tile(a, t0 + half + (i + 1) * HALVES, t1);
             fetch(nxt, i + 1 & 1);
             if (live && cur.n && (!PART || cur.key0 < last_limit)) {
-                const char* at = mine + (i & 1) * STAGE;
+                const unsigned at = to + (i & 1) * STAGE;
                 const int seen = limit - cur.key0;
                 f32x16 s[2];
                 x8 p[4];
                 if (!PART) st.met = true;
-                scores<E, D, 2>(at, qf, s);
+                scores<E, D, 2>(kp, at, qf, s);
                 weights<E, D, 2, PART>(st, s, a.scale, seen, p);
-                weigh<E, D, 2, PART>(st, at + STAGE / 2, p, seen);
+                weigh<E, D, 2, PART>(st, vp, at + STAGE / 2, p, seen, at + STAGE / 2);
             }
             cur = nxt;
         };
@@ -458,18 +470,22 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
         finish(st);
         if constexpr (HALVES == 2) {
             __syncthreads();
-            float* other = (float*)(lds + 2 * STAGE) + w4 * 16 * OT * 64;
+            float4* other = (float4*)(lds + 2 * STAGE) + w4 * 4 * OT * 64;
             if (half) {
                 if (h2 == 0) ends[wave][lane] = make_float2(st.top, st.sum);
 #pragma unroll
-                for (int e = 0; e < 16 * OT; ++e) other[e * 64 + lane] = st.o[e >> 4][e & 15];
+                for (int e = 0; e < 4 * OT; ++e) other[e * 64 + lane] = make_float4(st.o[e >> 2][4 * (e & 3)], st.o[e >> 2][4 * (e & 3) + 1], st.o[e >> 2][4 * (e & 3) + 2], st.o[e >> 2][4 * (e & 3) + 3]);
             }
             __syncthreads();
             if (half) return;
             const float2 theirs = ends[wave + 4][lane & 31];
             const float top = fmaxf(st.top, theirs.x), keep = rescale(st.top, top), take = rescale(theirs.x, top);
 #pragma unroll
-            for (int e = 0; e < 16 * OT; ++e) st.o[e >> 4][e & 15] = st.o[e >> 4][e & 15] * keep + other[e * 64 + lane] * take;
+            for (int e = 0; e < 4 * OT; ++e) {
+                const float4 x = other[e * 64 + lane];
+                float* o = (float*)&st.o[e >> 2] + 4 * (e & 3);
+                o[0] = o[0] * keep + x.x * take; o[1] = o[1] * keep + x.y * take; o[2] = o[2] * keep + x.z * take; o[3] = o[3] * keep + x.w * take;
+            }
             st.sum = st.sum * keep + theirs.y * take;
             st.top = top;
         }
@@ -477,8 +493,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
         constexpr int N = D / 16;                               // KiB of K (and of V) per tile
         const Fetch<D, false, N, 1> fetch_k(a.k_ts, 0);
         const Fetch<D, true, N, 1> fetch_v(a.v_ts, 0);
-        const char* at = lds + wave * (STAGE / 2);
-        const unsigned to = base + wave * (STAGE / 2);
+        const unsigned to = base + wave * (STAGE / 2), kp = k_piece<D>(), vp = v_piece<D>();
         Keys<32> keys{table, kb, vb, tile_limit, 0, -1};
         const int end = min(2 * t1, (tile_limit + 31) / 32);
         int i = 2 * t0 + wave;
@@ -501,12 +516,12 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
             x8 p[2];
             if (!PART) st.met = true;
             wait_loads<N>();
-            scores<E, D, 1>(at, qf, s);
+            scores<E, D, 1>(kp, to, qf, s);
             wait_lds();
             if (nxt.n) fetch_k(nxt.k, nxt.n, 32, to, 0);
             weights<E, D, 1, PART>(st, s, a.scale, seen, p);
             if (nxt.n) wait_loads<N>(); else wait_loads<0>();
-            weigh<E, D, 1, PART>(st, at + STAGE / 4, p, seen);
+            weigh<E, D, 1, PART>(st, vp, to + STAGE / 4, p, seen, to + STAGE / 4);
             wait_lds();
             if (nxt.n) fetch_v(nxt.v, nxt.n, 32, to + STAGE / 4, 0);
             cur = nxt;
@@ -538,44 +553,68 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
         }
     }
 
-    // out, or the part's share of it: a lane has runs of four elements of its row
+    // out, or the part's share of it
     const bool alone = PAGED && !prefix && piece == 0 && a.prefix_split && !has_group(a, r.seq);      // (all lanes look)
-    if (row >= rows) return;
-    const long at_row = (long)(r.q0 + token) * a.heads + head;
-    const int groups = few ? 4 * OT / WAVES : 4 * OT, g0 = few ? wave * (4 * OT / WAVES) : 0;
-    auto store = [&](auto&& put) {
-#pragma unroll
-        for (int i = 0; i < 4 * OT; ++i)
-            if (i < groups) {
-                const int g = g0 + i;                           // (run g: d = 32 (g / 4) + 8 (g % 4) + 4 h2)
-                put(32 * (g >> 2) + 8 * (g & 3) + 4 * h2, st.o[i >> 2][4 * (i & 3)], st.o[i >> 2][4 * (i & 3) + 1], st.o[i >> 2][4 * (i & 3) + 2], st.o[i >> 2][4 * (i & 3) + 3]);
-            }
-    };
-    if (!a.part_o) {
-        const float inv = no_key(st.top, st.sum) ? 0.f : 1.f / st.sum;
-        char* out = a.out + ((long)(r.q0 + token) * a.o_ts + (long)head * a.o_hs) * 2;
-        store([&](int d, float x, float y, float z, float w) { *reinterpret_cast<x4*>(out + 2 * d) = x4{(E)(x * inv), (E)(y * inv), (E)(z * inv), (E)(w * inv)}; });
-        if (a.lse && h2 == 0 && (!few || wave == 0)) a.lse[at_row] = log_sum(st.top, st.sum);
-    } else {
-        const long parts = (long)a.q_tokens * a.heads, slot = prefix ? piece : a.prefix_split + piece;
-        if (!no_key(st.top, st.sum)) {
-            float* out = a.part_o + (slot * parts + at_row) * D;
-            store([&](int d, float x, float y, float z, float w) { *reinterpret_cast<float4*>(out + d) = make_float4(x, y, z, w); });
+    const bool none = no_key(st.top, st.sum), mine = row < rows;
+    const float inv = none ? 0.f : 1.f / st.sum;
+    const long at_row = (long)(r.q0 + token) * a.heads + head, parts = (long)a.q_tokens * a.heads, slot = prefix ? piece : a.prefix_split + piece;
+    if (mine && h2 == 0 && (!few || wave == 0)) {
+        if (!a.part_o) {
+            if (a.lse) a.lse[at_row] = log_sum(st.top, st.sum);
+        } else {
+            a.part_ml[slot * parts + at_row] = make_float2(st.top, st.sum);
+            if (alone)                                          // a branch outside every group: nobody else writes what its prefix would give
+                for (int p = 0; p < a.prefix_split; ++p) a.part_ml[p * parts + at_row] = make_float2(-INFINITY, 0.f);
         }
-        if (h2 == 0 && (!few || wave == 0)) a.part_ml[slot * parts + at_row] = make_float2(st.top, st.sum);
-        // a branch outside every group: nobody else writes what its prefix would give
-        if (alone && h2 == 0 && (!few || wave == 0))
-            for (int p = 0; p < a.prefix_split; ++p) a.part_ml[p * parts + at_row] = make_float2(-INFINITY, 0.f);
     }
+    const long place = a.part_o ? ((slot * parts + at_row) * D) * 4 : ((long)(r.q0 + token) * a.o_ts + (long)head * a.o_hs) * 2;     // (a part without a key: its output is not read)
+    char* const out = a.part_o ? (char*)a.part_o : a.out;
+    const bool store = mine && !(a.part_o && none);
+    if (few) {
+        // a lane has runs of four elements of its row (run g: d = 32 (g / 4) + 8 (g % 4) + 4 h2), a wave its share of them
+        if (store)
+#pragma unroll
+            for (int i = 0; i < 4 * OT / WAVES; ++i) {
+                const int g = wave * (4 * OT / WAVES) + i, d = 32 * (g >> 2) + 8 * (g & 3) + 4 * h2;
+                const float x = st.o[i >> 2][4 * (i & 3)], y = st.o[i >> 2][4 * (i & 3) + 1], z = st.o[i >> 2][4 * (i & 3) + 2], w = st.o[i >> 2][4 * (i & 3) + 3];
+                if (a.part_o) *reinterpret_cast<float4*>(out + place + 4 * d) = make_float4(x, y, z, w);
+                else *reinterpret_cast<x4*>(out + place + 2 * d) = x4{(E)(x * inv), (E)(y * inv), (E)(z * inv), (E)(w * inv)};
+            }
+        return;
+    }
+    // 32 rows a wave, through its slice of LDS, so that whole rows are stored at once (8 bytes of each of 64 rows at a time: 2.2 us instead of
+    // less than one).  Piece c of row r lies at c ^ r.
+    if (HALVES == 1) __syncthreads();                           // (all have left the stages; after the halves' join they have)
+    if (h2 == 0) places[w4][lane] = store ? place : -1;
+    auto through = [&](auto put, auto bytes_of) {
+        constexpr int BYTES = decltype(bytes_of)::value, PER = D * BYTES / 16, ROWS = 64 / PER;      // an element's; pieces a row; rows an instruction
+        char* at = lds + w4 * 32 * D * BYTES;
+#pragma unroll
+        for (int g = 0; g < 4 * OT; ++g) {
+            const int d = 32 * (g >> 2) + 8 * (g & 3) + 4 * h2, c = d * BYTES / 16;
+            put(at + ((lane & 31) * PER + (c ^ (lane & 31 & (PER - 1)))) * 16 + d * BYTES % 16, st.o[g >> 2][4 * (g & 3)], st.o[g >> 2][4 * (g & 3) + 1], st.o[g >> 2][4 * (g & 3) + 2],
+                st.o[g >> 2][4 * (g & 3) + 3]);
+        }
+        wave_lds_order();
+#pragma unroll
+        for (int i = 0; i < 32 / ROWS; ++i) {
+            const int rr = i * ROWS + lane / PER, c = (lane % PER) ^ (rr & (PER - 1));
+            const long to = places[w4][rr];
+            const u32x4 x = *reinterpret_cast<const u32x4*>(at + (rr * PER + lane % PER) * 16);
+            if (to >= 0) *reinterpret_cast<u32x4*>(out + to + c * 16) = x;
+        }
+    };
+    if (a.part_o) through([](char* at, float x, float y, float z, float w) { *reinterpret_cast<float4*>(at) = make_float4(x, y, z, w); }, IC(4));
+    else through([&](char* at, float x, float y, float z, float w) { *reinterpret_cast<x4*>(at) = x4{(E)(x * inv), (E)(y * inv), (E)(z * inv), (E)(w * inv)}; }, IC(2));
 }
 
-// The parts of every row, joined: a group of D / 4 lanes takes each JOIN_WAYS-th of them, and the groups are joined in order.
-#define JOIN_WAYS 4
-template <class E, int D> __global__ __launch_bounds__(256) void kv_join_kernel(KvArgs a) {
+// The parts of every row, joined: a group of D / 4 lanes takes each WAYS-th of them, and the groups are joined in order.  (Four ways for many parts, which a row's chain of loads
+// would be long for; one, and more rows a workgroup, for few.)
+template <class E, int D, int WAYS> __global__ __launch_bounds__(256) void kv_join_kernel(KvArgs a) {
     typedef E x4 __attribute__((ext_vector_type(4)));
-    constexpr int LANES = D / 4, ROWS = 256 / LANES / JOIN_WAYS;
-    __shared__ float4 outs[JOIN_WAYS][ROWS][LANES];
-    __shared__ float sums[JOIN_WAYS][ROWS];
+    constexpr int LANES = D / 4, ROWS = 256 / LANES / WAYS;
+    __shared__ float4 outs[WAYS][ROWS][LANES];
+    __shared__ float sums[WAYS][ROWS];
     RowTile r;
     if (!find_tile(a, nullptr, a.n_seq, blockIdx.x, a.heads, ROWS, r, [](int, int&, int&) {})) return;
     const int rows = r.n * a.heads, n_parts = a.prefix_split + a.own_split;
@@ -586,7 +625,7 @@ template <class E, int D> __global__ __launch_bounds__(256) void kv_join_kernel(
     for (int p = 0; p < n_parts; ++p) top = fmaxf(top, a.part_ml[p * parts + at].x);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-    for (int p = way; p < n_parts; p += JOIN_WAYS) {
+    for (int p = way; p < n_parts; p += WAYS) {
         const float2 ml = a.part_ml[p * parts + at];
         if (no_key(ml.x, ml.y)) continue;                       // (its output was not written)
         const float keep = rescale(ml.x, top);
@@ -599,7 +638,7 @@ template <class E, int D> __global__ __launch_bounds__(256) void kv_join_kernel(
     __syncthreads();
     if (way || row >= rows) return;
 #pragma unroll
-    for (int w = 1; w < JOIN_WAYS; ++w) {
+    for (int w = 1; w < WAYS; ++w) {
         const float4 x = outs[w][i][l];
         o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
         sum += sums[w][i];
@@ -613,8 +652,9 @@ template <class E, int D> __global__ __launch_bounds__(256) void kv_join_kernel(
 template <class E, int D, bool PAGED> static void launch_kv(const KvArgs& a, hipStream_t s) {
     const unsigned grid = (unsigned)((a.prefix_tiles * (long)a.prefix_split + a.own_tiles * (long)a.own_split) * a.kv_heads);
     if (a.halves == 2) kv_attention_kernel<E, D, PAGED, 2><<<grid, 512, 0, s>>>(a); else kv_attention_kernel<E, D, PAGED, 1><<<grid, 256, 0, s>>>(a);
-    constexpr int ROWS = 256 / (D / 4) / JOIN_WAYS;
-    if (a.part_o) kv_join_kernel<E, D><<<(unsigned)(((long)a.q_tokens * a.heads + (ROWS - 1) * (long)a.n_seq) / ROWS), 256, 0, s>>>(a);
+    auto groups = [&](int rows) { return (unsigned)(((long)a.q_tokens * a.heads + (rows - 1) * (long)a.n_seq) / rows); };
+    if (!a.part_o) return;
+    if (a.own_split + a.prefix_split >= 6) kv_join_kernel<E, D, 4><<<groups(64 / (D / 4)), 256, 0, s>>>(a); else kv_join_kernel<E, D, 1><<<groups(256 / (D / 4)), 256, 0, s>>>(a);
 }
 template <bool PAGED> static void launch_kv(const KvArgs& a, int type, int head_dim, hipStream_t s) {
     if (type == BB_BF16) head_dim == 128 ? launch_kv<__bf16, 128, PAGED>(a, s) : launch_kv<__bf16, 64, PAGED>(a, s);
