@@ -336,7 +336,7 @@ int bb_debug_panel_quantize(const float* x_dev, int rows, int cols, void* panel_
 /* ---- operators around K,V ------------------------------------------------------------------------------
  * Rotary positions, attention over packed prompts, attention of branches that share a prefix over a paged cache.  As with the 8-bit operators no context is
  * needed, all work is enqueued on hip_stream (of the current device), nothing is allocated, memset or synchronised, and every call may be captured into a
- * graph.  Pointers are device memory unless they end in _host.  Malformed arguments: BB_EINVAL; too little workspace: BB_ENOMEM; a HIP error: BB_EHIP.
+ * graph.  Arguments come in a struct that the call reads before it returns; the pointers in it are device memory.  Malformed arguments: BB_EINVAL; too little workspace: BB_ENOMEM; a HIP error: BB_EHIP.
  *
  * Rows of heads: element d of head h of token t lies at data[t * x_token + h * x_head + d]; strides in elements, not negative (that over a single token or head is
  * ignored).  Strides of an output are such that no element lies twice (the larger at least what the smaller spans), and it shares no element with another tensor of the
@@ -359,43 +359,60 @@ int bb_rope_frequencies(double* freqs_host, int rot, double base, double factor,
  * (a, b) -> (a cos - b sin, a sin + b cos) * magnitude; the rest of the head is copied.  Angles in 64 bits, the turn in fp32, rounded once to `type` (BB_F32, BB_BF16,
  * BB_F16).  positions [tokens] int32 (may be negative), freqs [rot / 2] fp64.  q_out may be q itself (same pointer and strides), k_out k.  q_heads or k_heads may be 0
  * (the pointers are then ignored).  head_dim up to BB_ROPE_MAX_DIM, rot even, 0 .. head_dim. */
-int bb_rope(const void* q_dev, long q_token, long q_head, void* q_out_dev, long qo_token, long qo_head, int q_heads, const void* k_dev, long k_token, long k_head,
-            void* k_out_dev, long ko_token, long ko_head, int k_heads, const int32_t* positions_dev, const double* freqs_dev, int rot, int interleaved,
-            float magnitude, long tokens, int head_dim, int type, void* hip_stream);
+typedef struct {
+    const void* q; long q_token, q_head; void* q_out; long qo_token, qo_head, q_heads;
+    const void* k; long k_token, k_head; void* k_out; long ko_token, ko_head, k_heads;
+    const int32_t* positions; const double* freqs; long rot, interleaved; double magnitude;
+    long tokens, head_dim, type;
+} bb_rope_args;
+int bb_rope(const bb_rope_args* args_host, void* hip_stream);
 
 /* The same, with the turned keys and the values written to a paged cache: token t's to slot slots[t] = page * BB_PAGE_TOKENS + token in the page.  Tokens whose slot is
  * negative or beyond the last page stay out of the cache (their queries are turned all the same).  Slots of one call must differ; of tokens with the same slot
  * any may be what it holds afterwards, element by element. */
-int bb_rope_append(const void* q_dev, long q_token, long q_head, void* q_out_dev, long qo_token, long qo_head, int q_heads, const void* k_dev, long k_token, long k_head,
-                   const void* v_dev, long v_token, long v_head, int kv_heads, const int32_t* positions_dev, const double* freqs_dev, int rot, int interleaved,
-                   float magnitude, const int32_t* slots_dev, void* k_cache_dev, long kc_page, long kc_head, long kc_token, void* v_cache_dev, long vc_page,
-                   long vc_head, long vc_token, int n_pages, long tokens, int head_dim, int type, void* hip_stream);
+typedef struct {
+    const void* q; long q_token, q_head; void* q_out; long qo_token, qo_head, q_heads;
+    const void* k; long k_token, k_head; const void* v; long v_token, v_head, kv_heads;
+    const int32_t* positions; const double* freqs; long rot, interleaved; double magnitude;
+    const int32_t* slots;
+    void* k_cache; long kc_page, kc_head, kc_token; void* v_cache; long vc_page, vc_head, vc_token, pages;
+    long tokens, head_dim, type;
+} bb_rope_append_args;
+int bb_rope_append(const bb_rope_append_args* args_host, void* hip_stream);
 
 /* Attention over packed sequences: sequence s has the queries q_starts[s] .. q_starts[s + 1] - 1 of q_tokens and the keys k_starts[s] .. k_starts[s + 1] - 1 of k_tokens
- * (starts [n_seq + 1], ascending).  Query heads h * heads / kv_heads .. use kv head h.  out = softmax(scale q k^T) v over the keys that a query sees: query i of n
+ * (starts [sequences + 1], ascending).  Query heads h * heads / kv_heads .. use kv head h.  out = softmax(scale q k^T) v over the keys that a query sees: query i of n
  * stands at key position p = m - n + i of the m keys and sees all of them (block == 0), or those before the end of its block, j < (p / block + 1) * block, none if
  * p < 0 (block == 1: causal).  A query that sees no key gives zeros.  Tokens outside every sequence are left as they were.  lse (may be NULL):
  * [q_tokens][heads] fp32, contiguous, the natural logarithm of the sum of exp(scale q k) (-inf where no key is seen), for joining partial results.
  * type BB_BF16 or BB_F16; head_dim 64 or 128; scale > 0; all pointers of heads 16-byte aligned and their strides multiples of 8 elements, those between tokens of k and v at most 2^23.
  * NaN and infinities in keys and values that a query does not see do not reach it.
- * workspace_dev: at least bb_attention_workspace_bytes() of the same sizes, 256-byte aligned (may be NULL if that is 0), used by this call alone until its work is done. */
-size_t bb_attention_workspace_bytes(long q_tokens, long k_tokens, int n_seq, int heads, int kv_heads, int head_dim);
-int bb_attention(const void* q_dev, long q_token, long q_head, const void* k_dev, long k_token, long k_head, const void* v_dev, long v_token, long v_head,
-                 const int32_t* q_starts_dev, const int32_t* k_starts_dev, int n_seq, long q_tokens, long k_tokens, int heads, int kv_heads, int head_dim,
-                 int type, int block, float scale, void* out_dev, long o_token, long o_head, float* lse_dev, void* workspace_dev, size_t workspace_bytes,
-                 void* hip_stream);
+ * workspace_dev: at least bb_attention_workspace_bytes() of the same sizes (it looks at no pointer, stride, block or scale), 256-byte aligned (may be NULL if that is 0), used by this call
+ * alone until its work is done. */
+typedef struct {
+    const void* q; long q_token, q_head; const void* k; long k_token, k_head; const void* v; long v_token, v_head;
+    const int32_t *q_starts, *k_starts;
+    long sequences, q_tokens, k_tokens, heads, kv_heads, head_dim, type, block; double scale;
+    void* out; long o_token, o_head; float* lse;
+} bb_attention_args;
+size_t bb_attention_workspace_bytes(const bb_attention_args* args_host);
+int bb_attention(const bb_attention_args* args_host, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 
 /* Attention of branches over a paged cache, the prefix that a group of them shares read once for all.  Branch b has the queries q_starts[b] .. q_starts[b + 1] - 1, own_lens[b]
  * keys of its own in the pages own_pages[b * own_ld + 0 ..] and belongs to group g if group_starts[g] <= b < group_starts[g + 1]; the group's prefix is prefix_lens[g] keys in the
  * pages prefix_pages[g * prefix_ld + 0 ..].  A query sees its whole prefix, and of its branch's m own keys those that bb_attention describes (block counted from the
- * first own key).  own_width, prefix_width: columns of the tables, at most that many pages count.  n_groups == 0: no prefix (pointers ignored): plain attention over pages.
- * Both lengths may end inside a page; what lies behind them is not read.  Branches outside every group have no prefix.  The rest as in bb_attention. */
-size_t bb_shared_attention_workspace_bytes(long q_tokens, int n_branches, int n_groups, int own_width, int prefix_width, int heads, int kv_heads, int head_dim);
-int bb_shared_attention(const void* q_dev, long q_token, long q_head, const int32_t* q_starts_dev, int n_branches, long q_tokens, const void* k_cache_dev, long kc_page,
-                        long kc_head, long kc_token, const void* v_cache_dev, long vc_page, long vc_head, long vc_token, int n_pages, const int32_t* own_pages_dev,
-                        long own_ld, int own_width, const int32_t* own_lens_dev, const int32_t* prefix_pages_dev, long prefix_ld, int prefix_width,
-                        const int32_t* prefix_lens_dev, const int32_t* group_starts_dev, int n_groups, int heads, int kv_heads, int head_dim, int type, int block,
-                        float scale, void* out_dev, long o_token, long o_head, float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+ * first own key).  own_width, prefix_width: columns of the tables, at most that many pages count.  groups == 0: no prefix (pointers ignored): plain attention over pages.
+ * Both lengths may end inside a page; what lies behind them is not read.  Branches outside every group have no prefix; starts and group_starts ascend.  The rest as in bb_attention. */
+typedef struct {
+    const void* q; long q_token, q_head; const int32_t* q_starts; long branches, q_tokens;
+    const void* k_cache; long kc_page, kc_head, kc_token; const void* v_cache; long vc_page, vc_head, vc_token, pages;
+    const int32_t* own_pages; long own_ld, own_width; const int32_t* own_lens;
+    const int32_t* prefix_pages; long prefix_ld, prefix_width; const int32_t *prefix_lens, *group_starts; long groups;
+    long heads, kv_heads, head_dim, type, block; double scale;
+    void* out; long o_token, o_head; float* lse;
+} bb_shared_attention_args;
+size_t bb_shared_attention_workspace_bytes(const bb_shared_attention_args* args_host);
+int bb_shared_attention(const bb_shared_attention_args* args_host, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 
 /* Tests: on != 0 makes every later forward also store the fp32 logits of the rows that receive them (view's
  * logits_dev); off (the default) the logits exist only in the registers of the LM-head GEMM. */

@@ -1,6 +1,7 @@
 """ctypes binding with the same names as include/blockbatch.h (argument marshalling only)."""
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 import numpy as np
@@ -127,19 +128,12 @@ def load_library():
         lib.bb_gemm_int8.argtypes = [ptr, i64, ptr, ptr, i64, ptr, ptr, ptr, i64, i32, i32, i32, i32, ptr, C.c_size_t, ptr]
         lib.bb_gemm_int8_workspace_bytes.argtypes = [i32, i32, i32, i32]
         lib.bb_gemm_int8_workspace_bytes.restype = C.c_size_t
-        f64, f32, size = C.c_double, C.c_float, C.c_size_t
-        rows = [ptr, i64, i64]                                  # data, strides between tokens and heads
-        pages = [ptr, i64, i64, i64]                            # data, strides between pages, heads and tokens
+        f64, packed = C.c_double, C.c_char_p                    # (packed: a struct of the header as bytes)
         lib.bb_rope_frequencies.argtypes = [ptr, i32, f64, f64, f64, f64, f64]
-        lib.bb_rope.argtypes = [*rows, *rows, i32, *rows, *rows, i32, ptr, ptr, i32, i32, f32, i64, i32, i32, ptr]
-        lib.bb_rope_append.argtypes = [*rows, *rows, i32, *rows, *rows, i32, ptr, ptr, i32, i32, f32, ptr, *pages, *pages, i32, i64, i32, i32, ptr]
-        lib.bb_attention_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32]
-        lib.bb_attention_workspace_bytes.restype = size
-        lib.bb_attention.argtypes = [*rows, *rows, *rows, ptr, ptr, i32, i64, i64, i32, i32, i32, i32, i32, f32, *rows, ptr, ptr, size, ptr]
-        lib.bb_shared_attention_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32, i32, i32]
-        lib.bb_shared_attention_workspace_bytes.restype = size
-        lib.bb_shared_attention.argtypes = [*rows, ptr, i32, i64, *pages, *pages, i32, ptr, i64, i32, ptr, ptr, i64, i32, ptr, ptr, i32, i32, i32, i32, i32, i32, f32,
-                                            *rows, ptr, ptr, size, ptr]
+        lib.bb_rope.argtypes = lib.bb_rope_append.argtypes = [packed, ptr]
+        lib.bb_attention_workspace_bytes.argtypes = lib.bb_shared_attention_workspace_bytes.argtypes = [packed]
+        lib.bb_attention_workspace_bytes.restype = lib.bb_shared_attention_workspace_bytes.restype = C.c_size_t
+        lib.bb_attention.argtypes = lib.bb_shared_attention.argtypes = [packed, ptr, C.c_size_t, ptr]
         lib.bb_debug_gemm_int8_plan.argtypes = [i32, i32, i32, C.POINTER(i32)]
         lib.bb_debug_gemm_int8.argtypes = [ptr, ptr, ptr, ptr, i64, ptr, i32, i32, i32, i32, i32, ptr, ptr, C.c_size_t, ptr]
         lib.bb_debug_panel_quantize.argtypes = [ptr, i32, i32, ptr, C.c_size_t, ptr, ptr, ptr, ptr]
@@ -359,41 +353,48 @@ def rope_frequencies(rot, base=10000.0, factor=1.0, context=0, low=1.0, high=4.0
     return f.to(device)
 
 
-def _heads(t, what, dtype, tokens, heads, dim, device):
-    """Address and strides (between tokens, between heads) of rows of heads [tokens][heads][dim]."""
-    if t.dtype is not dtype or t.shape != (tokens, heads, dim) or t.device != device:
-        raise BBError(f"{what}: expected {dtype} {(tokens, heads, dim)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+# The header's argument structs, every field of eight bytes: a call packs its arguments into one of them at once (thirty arguments one by one cost ctypes 4 us).
+ROPE_ARGS = struct.Struct("7q7q2q2qd3q")
+ROPE_APPEND_ARGS = struct.Struct("7q7q2q2qd10q3q")
+ATTENTION_ARGS = struct.Struct("9q2q8qd3qq")
+SHARED_ATTENTION_ARGS = struct.Struct("6q9q4q6q5qd3qq")
+
+
+def _heads(t, what, dtype, shape, index):
+    """Address and strides (between tokens, between heads) of rows of heads [tokens][heads][dim] on GPU `index`."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        raise BBError(f"{what}: expected {dtype} {tuple(shape)} on cuda:{index}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     ts, hs, step = t.stride()
-    if step != 1 and dim > 1:
+    if step != 1 and shape[2] > 1:
         raise BBError(f"{what}: the elements of a head must be contiguous")
     return t.data_ptr(), ts, hs
 
 
-def _cache(t, what, dtype, pages, heads, dim, device):
+def _cache(t, what, dtype, shape, index):
     """Address and strides (between pages, heads, tokens) of a cache [pages][heads][PAGE_TOKENS][dim]."""
-    if t.dtype is not dtype or t.shape != (pages, heads, PAGE_TOKENS, dim) or t.device != device:
-        raise BBError(f"{what}: expected {dtype} {(pages, heads, PAGE_TOKENS, dim)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        raise BBError(f"{what}: expected {dtype} {tuple(shape)} on cuda:{index}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     ps, hs, ts, step = t.stride()
-    if step != 1 and dim > 1:
+    if step != 1 and shape[3] > 1:
         raise BBError(f"{what}: the elements of a head must be contiguous")
     return t.data_ptr(), ps, hs, ts
 
 
-def _table(t, what, rows, device):
+def _ints(t, what, n, index, dtype=None):
+    """Address of a contiguous vector of n elements (n None: at least one; returns their number too)."""
+    if t.dtype is not (dtype or _I32) or t.dim() != 1 or t.get_device() != index or (t.shape[0] != n if n is not None else t.shape[0] < 1) or not t.is_contiguous():
+        raise BBError(f"{what}: expected contiguous {dtype or _I32} ({'ranges + 1' if n is None else n},) on cuda:{index}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _table(t, what, rows, index):
     """Address, row distance and columns of a table of pages [rows][columns]."""
-    if t.dtype is not _I32 or t.dim() != 2 or t.shape[0] != rows or t.device != device:
-        raise BBError(f"{what}: expected torch.int32 ({rows}, pages) on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.dtype is not _I32 or t.dim() != 2 or t.shape[0] != rows or t.get_device() != index:
+        raise BBError(f"{what}: expected torch.int32 ({rows}, pages) on cuda:{index}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     ld, step = t.stride()
     if step != 1 and t.shape[1] > 1:
         raise BBError(f"{what}: the pages of a row must be contiguous")
     return t.data_ptr(), ld, t.shape[1]
-
-
-def _starts(t, what, device):
-    """Address and number of ranges of starts [ranges + 1]."""
-    if t.dtype is not _I32 or t.dim() != 1 or t.shape[0] < 1 or t.device != device or (t.shape[0] > 1 and t.stride(0) != 1):
-        raise BBError(f"{what}: expected contiguous torch.int32 (ranges + 1,) on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr(), t.shape[0] - 1
 
 
 def _three(t, what):
@@ -408,25 +409,28 @@ def rope(q, k, positions, freqs, interleaved=False, magnitude=1.0, q_out=None, k
     Stream as in quantize_rows."""
     if _torch is None:
         _ready()
-    dev, dtype = q.device, q.dtype
-    if stream is not None or dev.index is None or dev.index != _here():
-        return _elsewhere(dev, stream, lambda: rope(q, k, positions, freqs, interleaved, magnitude, q_out, k_out))
-    tokens, heads, dim = _three(q, "q")
-    t = _type(dtype, "q")
+    dev = q.get_device()
+    if stream is not None or dev < 0 or dev != _here():
+        return _elsewhere(q.device, stream, lambda: rope(q, k, positions, freqs, interleaved, magnitude, q_out, k_out))
+    dtype, shape = q.dtype, _three(q, "q")
+    tokens, heads, dim = shape
     if q_out is None:
         q_out = q
-    kv_heads, ks, kos = 0, (None, 0, 0), (None, 0, 0)
+    kv_heads, ks, kos = 0, (0, 0, 0), (0, 0, 0)
     if k is not None:
-        kv_heads = _three(k, "k")[1]
+        kv = _three(k, "k")
+        if kv[0] != tokens or kv[2] != dim:
+            raise BBError(f"k: expected [{tokens}][kv heads][{dim}], got {tuple(kv)}")
+        kv_heads = kv[1]
         if k_out is None:
             k_out = k
-        ks, kos = _heads(k, "k", dtype, tokens, kv_heads, dim, dev), _heads(k_out, "k_out", dtype, tokens, kv_heads, dim, dev)
+        ks, kos = _heads(k, "k", dtype, kv, dev), _heads(k_out, "k_out", dtype, kv, dev)
     elif k_out is not None:
         raise BBError("k_out without k")
-    rot = 2 * freqs.shape[0] if freqs.dim() else 0
-    rc = _LIB.bb_rope(*_heads(q, "q", dtype, tokens, heads, dim, dev), *_heads(q_out, "q_out", dtype, tokens, heads, dim, dev), heads, *ks, *kos, kv_heads,
-                      _vec(positions, "positions", _I32, tokens, dev), _vec(freqs, "freqs", _F64, rot // 2, dev), rot, interleaved, magnitude, tokens, dim, t,
-                      _raw_stream(dev.index))
+    half = freqs.shape[0] if freqs.dim() == 1 else -1
+    rc = _LIB.bb_rope(ROPE_ARGS.pack(*_heads(q, "q", dtype, shape, dev), *_heads(q_out, "q_out", dtype, shape, dev), heads, *ks, *kos, kv_heads,
+                                     _ints(positions, "positions", tokens, dev), _ints(freqs, "freqs", half, dev, _F64), 2 * half, interleaved, magnitude, tokens, dim,
+                                     _type(dtype, "q")), _raw_stream(dev))
     if rc:
         _done(rc, "bb_rope")
     return q_out, k_out
@@ -437,36 +441,49 @@ def rope_append(q, k, v, positions, freqs, k_cache, v_cache, slots, interleaved=
     slots (int32 [tokens], page * PAGE_TOKENS + token in the page; a negative one keeps its token out).  Returns q_out.  Stream as in quantize_rows."""
     if _torch is None:
         _ready()
-    dev, dtype = q.device, q.dtype
-    if stream is not None or dev.index is None or dev.index != _here():
-        return _elsewhere(dev, stream, lambda: rope_append(q, k, v, positions, freqs, k_cache, v_cache, slots, interleaved, magnitude, q_out))
-    tokens, heads, dim = _three(q, "q")
-    kv_heads, t = _three(k, "k")[1], _type(dtype, "q")
+    dev = q.get_device()
+    if stream is not None or dev < 0 or dev != _here():
+        return _elsewhere(q.device, stream, lambda: rope_append(q, k, v, positions, freqs, k_cache, v_cache, slots, interleaved, magnitude, q_out))
+    dtype, shape, kv = q.dtype, _three(q, "q"), _three(k, "k")
+    tokens, heads, dim = shape
+    if kv[0] != tokens or kv[2] != dim:
+        raise BBError(f"k: expected [{tokens}][kv heads][{dim}], got {tuple(kv)}")
     if q_out is None:
         q_out = q
-    pages = k_cache.shape[0] if k_cache.dim() else 0
-    rot = 2 * freqs.shape[0] if freqs.dim() else 0
-    rc = _LIB.bb_rope_append(*_heads(q, "q", dtype, tokens, heads, dim, dev), *_heads(q_out, "q_out", dtype, tokens, heads, dim, dev), heads,
-                             *_heads(k, "k", dtype, tokens, kv_heads, dim, dev), *_heads(v, "v", dtype, tokens, kv_heads, dim, dev), kv_heads,
-                             _vec(positions, "positions", _I32, tokens, dev), _vec(freqs, "freqs", _F64, rot // 2, dev), rot, interleaved, magnitude,
-                             _vec(slots, "slots", _I32, tokens, dev), *_cache(k_cache, "k_cache", dtype, pages, kv_heads, dim, dev),
-                             *_cache(v_cache, "v_cache", dtype, pages, kv_heads, dim, dev), pages, tokens, dim, t, _raw_stream(dev.index))
+    pages, kv_heads = k_cache.shape[0] if k_cache.dim() else 0, kv[1]
+    cache = (pages, kv_heads, PAGE_TOKENS, dim)
+    half = freqs.shape[0] if freqs.dim() == 1 else -1
+    rc = _LIB.bb_rope_append(ROPE_APPEND_ARGS.pack(*_heads(q, "q", dtype, shape, dev), *_heads(q_out, "q_out", dtype, shape, dev), heads, *_heads(k, "k", dtype, kv, dev),
+                                                   *_heads(v, "v", dtype, kv, dev), kv_heads, _ints(positions, "positions", tokens, dev),
+                                                   _ints(freqs, "freqs", half, dev, _F64), 2 * half, interleaved, magnitude, _ints(slots, "slots", tokens, dev),
+                                                   *_cache(k_cache, "k_cache", dtype, cache, dev), *_cache(v_cache, "v_cache", dtype, cache, dev), pages, tokens, dim,
+                                                   _type(dtype, "q")), _raw_stream(dev))
     if rc:
         _done(rc, "bb_rope_append")
     return q_out
 
 
-def _attention_outputs(q, out, lse, scale):
-    """Sizes of q, the outputs made where not given, and the scale."""
-    tokens, heads, dim = _three(q, "q")
+def _attention_outputs(q, shape, out, lse, dev):
+    """(address, strides) of out, made where not given, and the address of lse."""
     if out is None:
-        out = _torch.empty(tokens, heads, dim, dtype=q.dtype, device=q.device)
-    pl = None
+        out = _torch.empty(shape, dtype=q.dtype, device=q.device)
+    pl = 0
     if lse is not None:
-        if lse.dtype is not _F32 or lse.shape != (tokens, heads) or lse.device != q.device or not lse.is_contiguous():
-            raise BBError(f"lse: expected contiguous torch.float32 {(tokens, heads)} on {q.device}, got {lse.dtype} {tuple(lse.shape)} on {lse.device}")
+        if lse.dtype is not _F32 or lse.shape != shape[:2] or lse.get_device() != dev or not lse.is_contiguous():
+            raise BBError(f"lse: expected contiguous torch.float32 {tuple(shape[:2])} on cuda:{dev}, got {lse.dtype} {tuple(lse.shape)} on {lse.device}")
         pl = lse.data_ptr()
-    return tokens, heads, dim, out, pl, dim ** -0.5 if scale is None else scale
+    return out, (*_heads(out, "out", q.dtype, shape, dev), pl)
+
+
+def _attend(call, workspace_bytes, args, dev, what):
+    nbytes = workspace_bytes(args)
+    if nbytes:
+        ws = _torch.empty(nbytes, dtype=_torch.uint8, device=dev)       # (held until the call has been enqueued)
+        rc = call(args, ws.data_ptr(), nbytes, _raw_stream(dev))
+    else:
+        rc = call(args, None, 0, _raw_stream(dev))
+    if rc:
+        _done(rc, what)
 
 
 def attention(q, k, v, q_starts, k_starts=None, block=0, scale=None, out=None, lse=None, stream=None):
@@ -476,22 +493,20 @@ def attention(q, k, v, q_starts, k_starts=None, block=0, scale=None, out=None, l
     given); returns out.  Stream as in quantize_rows; a workspace, where the call needs one, is allocated on it for this call alone."""
     if _torch is None:
         _ready()
-    dev, dtype = q.device, q.dtype
-    if stream is not None or dev.index is None or dev.index != _here():
-        return _elsewhere(dev, stream, lambda: attention(q, k, v, q_starts, k_starts, block, scale, out, lse))
-    tokens, heads, dim, out, pl, scale = _attention_outputs(q, out, lse, scale)
-    k_tokens, kv_heads, _ = _three(k, "k")
-    qs, n = _starts(q_starts, "q_starts", dev)
-    ks, nk = (qs, n) if k_starts is None else _starts(k_starts, "k_starts", dev)
-    if nk != n:
-        raise BBError(f"q_starts gives {n} sequences, k_starts {nk}")
-    nbytes = _LIB.bb_attention_workspace_bytes(tokens, k_tokens, n, heads, kv_heads, dim)
-    ws = _torch.empty(nbytes, dtype=_torch.uint8, device=dev) if nbytes else None
-    rc = _LIB.bb_attention(*_heads(q, "q", dtype, tokens, heads, dim, dev), *_heads(k, "k", dtype, k_tokens, kv_heads, dim, dev),
-                           *_heads(v, "v", dtype, k_tokens, kv_heads, dim, dev), qs, ks, n, tokens, k_tokens, heads, kv_heads, dim, _type(dtype, "q"), block, scale,
-                           *_heads(out, "out", dtype, tokens, heads, dim, dev), pl, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(dev.index))
-    if rc:
-        _done(rc, "bb_attention")
+    dev = q.get_device()
+    if stream is not None or dev < 0 or dev != _here():
+        return _elsewhere(q.device, stream, lambda: attention(q, k, v, q_starts, k_starts, block, scale, out, lse))
+    dtype, shape, kv = q.dtype, _three(q, "q"), _three(k, "k")
+    tokens, heads, dim = shape
+    if kv[2] != dim:
+        raise BBError(f"k: expected [tokens][kv heads][{dim}], got {tuple(kv)}")
+    out, outs = _attention_outputs(q, shape, out, lse, dev)
+    qs = _ints(q_starts, "q_starts", None, dev)
+    n = q_starts.shape[0]
+    ks = qs if k_starts is None else _ints(k_starts, "k_starts", n, dev)
+    args = ATTENTION_ARGS.pack(*_heads(q, "q", dtype, shape, dev), *_heads(k, "k", dtype, kv, dev), *_heads(v, "v", dtype, kv, dev), qs, ks, n - 1, tokens, kv[0], heads, kv[1], dim,
+                               _type(dtype, "q"), block, dim ** -0.5 if scale is None else scale, *outs)
+    _attend(_LIB.bb_attention, _LIB.bb_attention_workspace_bytes, args, dev, "bb_attention")
     return out
 
 
@@ -503,33 +518,31 @@ def shared_attention(q, q_starts, k_cache, v_cache, own_pages, own_lens, prefix_
     block, scale, out, lse, stream and workspace as in attention (block counts from the first own key)."""
     if _torch is None:
         _ready()
-    dev, dtype = q.device, q.dtype
-    if stream is not None or dev.index is None or dev.index != _here():
-        return _elsewhere(dev, stream, lambda: shared_attention(q, q_starts, k_cache, v_cache, own_pages, own_lens, prefix_pages, prefix_lens, group_starts, block,
-                                                                scale, out, lse))
-    tokens, heads, dim, out, pl, scale = _attention_outputs(q, out, lse, scale)
-    if k_cache.dim() != 4:
-        raise BBError(f"k_cache: expected [pages][kv heads][{PAGE_TOKENS}][head_dim], got {tuple(k_cache.shape)}")
-    pages, kv_heads = k_cache.shape[:2]
-    qs, n = _starts(q_starts, "q_starts", dev)
-    own, own_ld, own_width = _table(own_pages, "own_pages", n, dev)
-    pre, pre_ld, pre_width, pre_lens, gs, groups = None, 0, 0, None, None, 0
+    dev = q.get_device()
+    if stream is not None or dev < 0 or dev != _here():
+        return _elsewhere(q.device, stream, lambda: shared_attention(q, q_starts, k_cache, v_cache, own_pages, own_lens, prefix_pages, prefix_lens, group_starts, block,
+                                                                     scale, out, lse))
+    dtype, shape = q.dtype, _three(q, "q")
+    tokens, heads, dim = shape
+    cache = k_cache.shape
+    if len(cache) != 4 or cache[2] != PAGE_TOKENS or cache[3] != dim:
+        raise BBError(f"k_cache: expected [pages][kv heads][{PAGE_TOKENS}][{dim}], got {tuple(cache)}")
+    out, outs = _attention_outputs(q, shape, out, lse, dev)
+    qs = _ints(q_starts, "q_starts", None, dev)
+    n = q_starts.shape[0] - 1
+    prefix = (0, 0, 0, 0, 0, 0)
     if group_starts is not None:
         if prefix_pages is None or prefix_lens is None:
             raise BBError("group_starts without prefix_pages and prefix_lens")
-        gs, groups = _starts(group_starts, "group_starts", dev)
-        pre, pre_ld, pre_width = _table(prefix_pages, "prefix_pages", groups, dev)
-        pre_lens = _vec(prefix_lens, "prefix_lens", _I32, groups, dev)
+        gs = _ints(group_starts, "group_starts", None, dev)
+        groups = group_starts.shape[0] - 1
+        prefix = (*_table(prefix_pages, "prefix_pages", groups, dev), _ints(prefix_lens, "prefix_lens", groups, dev), gs, groups)
     elif prefix_pages is not None or prefix_lens is not None:
         raise BBError("prefix_pages or prefix_lens without group_starts")
-    nbytes = _LIB.bb_shared_attention_workspace_bytes(tokens, n, groups, own_width, pre_width, heads, kv_heads, dim)
-    ws = _torch.empty(nbytes, dtype=_torch.uint8, device=dev) if nbytes else None
-    rc = _LIB.bb_shared_attention(*_heads(q, "q", dtype, tokens, heads, dim, dev), qs, n, tokens, *_cache(k_cache, "k_cache", dtype, pages, kv_heads, dim, dev),
-                                  *_cache(v_cache, "v_cache", dtype, pages, kv_heads, dim, dev), pages, own, own_ld, own_width,
-                                  _vec(own_lens, "own_lens", _I32, n, dev), pre, pre_ld, pre_width, pre_lens, gs, groups, heads, kv_heads, dim, _type(dtype, "q"), block, scale,
-                                  *_heads(out, "out", dtype, tokens, heads, dim, dev), pl, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(dev.index))
-    if rc:
-        _done(rc, "bb_shared_attention")
+    args = SHARED_ATTENTION_ARGS.pack(*_heads(q, "q", dtype, shape, dev), qs, n, tokens, *_cache(k_cache, "k_cache", dtype, cache, dev),
+                                      *_cache(v_cache, "v_cache", dtype, cache, dev), cache[0], *_table(own_pages, "own_pages", n, dev), _ints(own_lens, "own_lens", n, dev),
+                                      *prefix, heads, cache[1], dim, _type(dtype, "q"), block, dim ** -0.5 if scale is None else scale, *outs)
+    _attend(_LIB.bb_shared_attention, _LIB.bb_shared_attention_workspace_bytes, args, dev, "bb_shared_attention")
     return out
 
 

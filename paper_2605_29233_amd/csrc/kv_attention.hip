@@ -31,16 +31,28 @@ template <> struct Half<__bf16> {
     static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 
+// n / d by a product: exact for 0 <= n < 2^31, 1 <= d < 2^31.
+struct Divide {
+    unsigned m; int shift;
+    static Divide by(unsigned d) {
+        int l = 0;
+        while ((1u << l) < d) ++l;
+        return {(unsigned)(((1ull << (31 + l)) + d - 1) / d), 31 + l};
+    }
+    __device__ __forceinline__ int operator()(int n) const { return (int)((unsigned long long)(unsigned)n * m >> shift); }
+};
 struct KvArgs {
-    const char *q, *k, *v; char* out; float* lse;
-    long q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs, k_ps, v_ps;    // elements; k_ps, v_ps: between pages
     const int *q_starts, *k_starts;                                     // k_starts: packed keys (bb_attention)
     const int *own_pages, *own_lens, *prefix_pages, *prefix_lens, *group_starts;
+    const char *q, *k, *v; char* out; float* lse;
+    long q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs, k_ps, v_ps;    // elements; k_ps, v_ps: between pages
     long own_ld, prefix_ld;
     int q_tokens, k_tokens, n_seq, n_groups, n_pages, own_width, prefix_width;
     int heads, kv_heads, each, block;
     float scale;                                                        // times log2(e)
-    int own_tiles, own_split, prefix_tiles, prefix_split, halves;               // row tiles that the branches (groups) may have, parts that their keys are cut into
+    int own_tiles, own_split, prefix_tiles, prefix_split, halves;       // row tiles that the branches (groups) may have, parts that their keys are cut into.  No prefix tiles: a
+                                                                        // branch's items take its group's prefix before its own keys
+    Divide by_kv_heads, by_each, by_block, by_own_split, by_prefix_split;
     float* part_o; float2* part_ml;                                     // [part][token][head]: unscaled output; maximum (times log2(e)) and sum.  Null: a single part
 };
 #define KV_LEAST_TILES 2                // of 64 keys, a part of a row tile's keys
@@ -91,35 +103,40 @@ static __device__ __forceinline__ bool find_tile(const KvArgs& a, const int* __r
     return false;
 }
 
-// Whether a branch belongs to any group.
-static __device__ __forceinline__ bool has_group(const KvArgs& a, int seq) {
+// The group a branch belongs to, -1: none.
+static __device__ __forceinline__ int find_group(const KvArgs& a, int seq) {
     const int lane = threadIdx.x & 63;
     for (int b = 0; b < a.n_groups; b += 64) {
         const int i = b + lane;
-        if (__ballot(i < a.n_groups && a.group_starts[i] <= seq && seq < a.group_starts[i + 1])) return true;
+        const unsigned long long hit = __ballot(i < a.n_groups && a.group_starts[i] <= seq && seq < a.group_starts[i + 1]);
+        if (hit) return b + __builtin_ctzll(hit);
     }
-    return false;
+    return -1;
 }
+static __device__ __forceinline__ int paged_keys(int n, int width) { return min(max(n, 0), (int)min((long)width * BB_PAGE_TOKENS, 0x3FFFFFC0L)); }
 
-// Keys in tiles of KEYS tokens: pages, or packed.  The ids of 64 pages at a time stand in a register's lanes: a load per tile would have to be waited for, and
-// with it every fetch on its way.  A tile past the end, or of a page that is not in the cache, has no keys (n = 0).
-struct KeyTile { const char *k, *v; int key0, n; };
+// Keys in tiles of KEYS tokens: packed, or pages, those of a prefix before those of its own (a tile never holds both).  The ids of 64 pages at a time stand in a register's
+// lanes: a load per tile would have to be waited for, and with it every fetch on its way.  A tile past the end, or of a page that is not in the cache, has no keys (n = 0).
+struct KeyTile { const char *k, *v; int key0, n; bool own; };
 template <int KEYS> struct Keys {
-    const int* table;               // null: packed
+    const int *prefix, *own;        // page tables (both null: packed)
     const char *k, *v;              // of the kv head (packed: of the first key)
-    int m;                          // keys
+    int n_prefix, n_own;            // keys
     int ids, ids_at;                // page ids from ids_at on (-1: none yet)
     __device__ __forceinline__ KeyTile tile(const KvArgs& a, int i, int end) {
+        constexpr int PER_PAGE = BB_PAGE_TOKENS / KEYS;
         KeyTile t{};
         if (i >= end) return t;
-        t.key0 = i * KEYS;
+        const int prefix_pages = (n_prefix + BB_PAGE_TOKENS - 1) / BB_PAGE_TOKENS;
+        t.own = i >= prefix_pages * PER_PAGE;
+        t.key0 = (t.own ? i - prefix_pages * PER_PAGE : i) * KEYS;
         long k_at = (long)t.key0 * a.k_ts, v_at = (long)t.key0 * a.v_ts;
-        if (table) {
-            const int page = t.key0 / BB_PAGE_TOKENS, within = t.key0 % BB_PAGE_TOKENS;
+        if (own || prefix) {
+            const int page = i / PER_PAGE, within = i % PER_PAGE * KEYS;
             if (ids_at < 0 || page >= ids_at + 64) {
                 ids_at = page;
-                const int p = page + (int)(threadIdx.x & 63);
-                ids = p * BB_PAGE_TOKENS < m ? table[p] : -1;
+                const int p = page + (int)(threadIdx.x & 63), of_own = p - prefix_pages;
+                ids = of_own < 0 ? prefix[p] : of_own * BB_PAGE_TOKENS < n_own ? own[of_own] : -1;
             }
             const int id = __builtin_amdgcn_readlane(ids, page - ids_at);
             if ((unsigned)id >= (unsigned)a.n_pages) return t;
@@ -128,7 +145,7 @@ template <int KEYS> struct Keys {
         }
         t.k = k + k_at * 2;
         t.v = v + v_at * 2;
-        t.n = min(m - t.key0, KEYS);
+        t.n = max(min((t.own ? n_own : n_prefix) - t.key0, KEYS), 0);
         return t;
     }
 };
@@ -364,25 +381,25 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
     __shared__ long places[4][32];                          // where a wave's rows go (-1: nowhere)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h2 = lane >> 5, half = wave >> 2, w4 = wave & 3;
 
-    // Which item: the keys' parts of all kv heads are dealt to the XCDs (workgroups go to them round robin), so that the row tiles of one share an L2; last row tiles, which see
-    // the most keys, first.
+    // Which item: kv head fastest, then the parts of the keys, so that the row tiles of a part of a head's keys go to one XCD (workgroups go to them round robin) wherever their
+    // number is a multiple of eight, and share an L2; last row tiles, which see the most keys, first.
     int lin = blockIdx.x;
     const int prefix_items = a.prefix_tiles * a.prefix_split * a.kv_heads;
     const bool prefix = PAGED && lin < prefix_items;
     if (!prefix) lin -= prefix_items;
-    const int tiles = prefix ? a.prefix_tiles : a.own_tiles, split = prefix ? a.prefix_split : a.own_split, chunks = split * a.kv_heads;
-    const int g8 = min(chunks & -chunks, 8), per = chunks / g8, j = lin / g8;
-    const int chunk = lin % g8 + g8 * (j % per), kvh = chunk / split, piece = chunk - kvh * split;
+    const int split = prefix ? a.prefix_split : a.own_split, j = a.by_kv_heads(lin), kvh = lin - j * a.kv_heads, from_last = prefix ? a.by_prefix_split(j) : a.by_own_split(j);
+    const int piece = j - from_last * split;
     RowTile r;
     const int* lens = PAGED ? prefix ? a.prefix_lens : a.own_lens : a.k_starts;
-    if (!find_tile(a, prefix ? a.group_starts : nullptr, prefix ? a.n_groups : a.n_seq, tiles - 1 - j / per, a.each, KV_ROWS, r, [&](int i, int& x, int& y) { x = lens[i]; if (!PAGED) y = lens[i + 1]; }))
+    if (!find_tile(a, prefix ? a.group_starts : nullptr, prefix ? a.n_groups : a.n_seq, (prefix ? a.prefix_tiles : a.own_tiles) - 1 - from_last, a.each, KV_ROWS, r,
+                   [&](int i, int& x, int& y) { x = lens[i]; if (!PAGED) y = lens[i + 1]; }))
         return;
 
     // the lane's row
     const int rows = r.n * a.each, tile_rows = min(rows - r.tile * KV_ROWS, KV_ROWS);
     const bool few = tile_rows <= 32;
     const int row = r.tile * KV_ROWS + (few ? 0 : w4 * 32) + (lane & 31), row_in = min(row, rows - 1);
-    const int token = row_in / a.each, head = kvh * a.each + row_in - token * a.each;
+    const int token = a.by_each(row_in), head = kvh * a.each + row_in - token * a.each;
     x8 qf[ST];
     {
         const char* q = a.q + ((long)(r.q0 + token) * a.q_ts + (long)head * a.q_hs) * 2 + 16 * h2;
@@ -390,29 +407,37 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
         for (int s = 0; s < ST; ++s) qf[s] = *reinterpret_cast<const x8*>(q + 32 * s);
     }
 
-    // its keys, and how many of them the row sees
-    const int* table = nullptr;
-    int m, limit, tile_limit;
+    // its keys, and how many of its own the row sees
+    const int *prefix_table = nullptr, *own_table = nullptr;
+    int n_prefix = 0, m = 0;
     long first = 0;
     if (!PAGED) {
         first = min(max(r.x, 0), a.k_tokens);
         m = min(max(r.y, (int)first), a.k_tokens) - (int)first;
+    } else if (prefix) {
+        n_prefix = paged_keys(r.x, a.prefix_width);
+        prefix_table = a.prefix_pages + (long)r.seq * a.prefix_ld;
     } else {
-        m = min(max(r.x, 0), (int)min((long)(prefix ? a.prefix_width : a.own_width) * BB_PAGE_TOKENS, 0x7FFFFFC0L));
-        table = prefix ? a.prefix_pages + (long)r.seq * a.prefix_ld : a.own_pages + (long)r.seq * a.own_ld;
+        m = paged_keys(r.x, a.own_width);
+        own_table = a.own_pages + (long)r.seq * a.own_ld;
+        const int g = a.n_groups && !prefix_items ? find_group(a, r.seq) : -1;
+        if (g >= 0) {
+            n_prefix = __builtin_amdgcn_readfirstlane(paged_keys(a.prefix_lens[g], a.prefix_width));
+            prefix_table = a.prefix_pages + (long)g * a.prefix_ld;
+        }
     }
-    limit = tile_limit = m;
-    int all_limit = m;                                          // keys that every row of the tile sees
-    if (!prefix && a.block) {
+    int limit = m, tile_limit = m, all_limit = m;               // the lane's row; the last row of the tile; keys that every row of the tile sees
+    if (a.block) {
         auto limit_of = [&](int tok) {
             const int p = m - r.n + tok;
-            return p < 0 ? 0 : (int)min((long)m, ((long)(p / a.block) + 1) * a.block);
+            return p < 0 ? 0 : (int)min((long)m, ((long)a.by_block(p) + 1) * a.block);
         };
         limit = limit_of(token);
-        tile_limit = limit_of(min(r.tile * KV_ROWS + KV_ROWS - 1, rows - 1) / a.each);     // (limits ascend with the token)
-        all_limit = limit_of(r.tile * KV_ROWS / a.each);
+        tile_limit = limit_of(a.by_each(min(r.tile * KV_ROWS + KV_ROWS - 1, rows - 1)));   // (limits ascend with the token)
+        all_limit = limit_of(a.by_each(r.tile * KV_ROWS));
     }
     const int last_limit = __builtin_amdgcn_readlane(limit, 31);
+    auto seen = [&](const KeyTile& t) { return t.own ? limit - t.key0 : t.n; };
 
     RowState<D> st;
 #pragma unroll
@@ -423,7 +448,8 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
 
     const unsigned base = lds_offset(lds);
     const char *kb = a.k + ((long)kvh * a.k_hs + first * a.k_ts) * 2, *vb = a.v + ((long)kvh * a.v_hs + first * a.v_ts) * 2;
-    const int n_tiles = (tile_limit + 63) / 64, t0 = (int)((long)n_tiles * piece / split), t1 = (int)((long)n_tiles * (piece + 1) / split);
+    const int n_tiles = (n_prefix + 63) / 64 + (tile_limit + 63) / 64, t0 = split == 1 ? 0 : (int)((long)n_tiles * piece / split), t1 = split == 1 ? n_tiles : (int)((long)n_tiles * (piece + 1) / split);
+    const int whole = n_prefix / 64 + (n_prefix % 64 ? 0 : all_limit / 64);     // tiles that every row sees whole, from the first on
     // The queries have to be there before the loop: left to it, their wait would be one for the fetches that are on their way there, too.
     auto have_queries = [&]() {
 #pragma unroll
@@ -433,7 +459,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
         constexpr int N = D / 32;                               // KiB of K (and of V) per wave and tile
         const Fetch<D, false, N, 4> fetch_k(a.k_ts, w4);
         const Fetch<D, true, N, 4> fetch_v(a.v_ts, w4);
-        Keys<64> keys{table, kb, vb, tile_limit, 0, -1};
+        Keys<64> keys{prefix_table, own_table, kb, vb, n_prefix, tile_limit, 0, -1};
         const unsigned to = base + half * 2 * STAGE, kp = k_piece<D>(), vp = v_piece<D>();
         auto fetch = [&](const KeyTile& t, int stage) {
             if (t.n == 0) return;
@@ -444,7 +470,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
         fetch(cur, 0);
         have_queries();
         const bool live = w4 * 32 < tile_rows;
-        const int n_whole = min(max(all_limit / 64 - t0, 0), t1 - t0) / HALVES, n_all = (t1 - t0 + HALVES - 1) / HALVES;    // rounds: of tiles that every row sees whole, all
+        const int n_whole = min(max(whole - t0, 0), t1 - t0) / HALVES, n_all = (t1 - t0 + HALVES - 1) / HALVES;    // rounds: of tiles that every row sees whole, all
         int i = 0;
         auto round = [&](auto part) {
             constexpr bool PART = decltype(part)::value;
@@ -452,15 +478,14 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
             __syncthreads();                                    // the round's tiles are there, and all have left those before them: the next on their way into their place
             nxt = keys.tile(a, t0 + half + (i + 1) * HALVES, t1);
             fetch(nxt, i + 1 & 1);
-            if (live && cur.n && (!PART || cur.key0 < last_limit)) {
+            if (live && cur.n && (!PART || !cur.own || cur.key0 < last_limit)) {
                 const unsigned at = to + (i & 1) * STAGE;
-                const int seen = limit - cur.key0;
                 f32x16 s[2];
                 x8 p[4];
                 if (!PART) st.met = true;
                 scores<E, D, 2>(kp, at, qf, s);
-                weights<E, D, 2, PART>(st, s, a.scale, seen, p);
-                weigh<E, D, 2, PART>(st, vp, at + STAGE / 2, p, seen, at + STAGE / 2);
+                weights<E, D, 2, PART>(st, s, a.scale, seen(cur), p);
+                weigh<E, D, 2, PART>(st, vp, at + STAGE / 2, p, seen(cur), at + STAGE / 2);
             }
             cur = nxt;
         };
@@ -494,8 +519,8 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
         const Fetch<D, false, N, 1> fetch_k(a.k_ts, 0);
         const Fetch<D, true, N, 1> fetch_v(a.v_ts, 0);
         const unsigned to = base + wave * (STAGE / 2), kp = k_piece<D>(), vp = v_piece<D>();
-        Keys<32> keys{table, kb, vb, tile_limit, 0, -1};
-        const int end = min(2 * t1, (tile_limit + 31) / 32);
+        Keys<32> keys{prefix_table, own_table, kb, vb, n_prefix, tile_limit, 0, -1};
+        const int end = 2 * t1;
         int i = 2 * t0 + wave;
         auto next = [&]() {                                     // (tiles without keys are passed over)
             KeyTile t{};
@@ -510,7 +535,6 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
         have_queries();
         auto step = [&](auto part) {
             constexpr bool PART = decltype(part)::value;
-            const int seen = limit - cur.key0;
             nxt = next();
             f32x16 s[1];
             x8 p[2];
@@ -519,14 +543,14 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
             scores<E, D, 1>(kp, to, qf, s);
             wait_lds();
             if (nxt.n) fetch_k(nxt.k, nxt.n, 32, to, 0);
-            weights<E, D, 1, PART>(st, s, a.scale, seen, p);
+            weights<E, D, 1, PART>(st, s, a.scale, seen(cur), p);
             if (nxt.n) wait_loads<N>(); else wait_loads<0>();
-            weigh<E, D, 1, PART>(st, vp, to + STAGE / 4, p, seen, to + STAGE / 4);
+            weigh<E, D, 1, PART>(st, vp, to + STAGE / 4, p, seen(cur), to + STAGE / 4);
             wait_lds();
             if (nxt.n) fetch_v(nxt.v, nxt.n, 32, to + STAGE / 4, 0);
             cur = nxt;
         };
-        while (cur.n && cur.key0 + 32 <= all_limit) step(std::false_type{});
+        while (cur.n == 32 && (!cur.own || cur.key0 + 32 <= all_limit)) step(std::false_type{});
         while (cur.n) step(std::true_type{});
         // the waves' parts of the same rows: each brings its own to the largest maximum, then each sums its share of the output
         st.sum = sum_halves(st.sum);
@@ -554,7 +578,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
     }
 
     // out, or the part's share of it
-    const bool alone = PAGED && !prefix && piece == 0 && a.prefix_split && !has_group(a, r.seq);      // (all lanes look)
+    const bool alone = PAGED && !prefix && piece == 0 && a.prefix_split && find_group(a, r.seq) < 0;      // (all lanes look)
     const bool none = no_key(st.top, st.sum), mine = row < rows;
     const float inv = none ? 0.f : 1.f / st.sum;
     const long at_row = (long)(r.q0 + token) * a.heads + head, parts = (long)a.q_tokens * a.heads, slot = prefix ? piece : a.prefix_split + piece;
@@ -661,125 +685,123 @@ template <bool PAGED> static void launch_kv(const KvArgs& a, int type, int head_
     else head_dim == 128 ? launch_kv<half_t, 128, PAGED>(a, s) : launch_kv<half_t, 64, PAGED>(a, s);
 }
 
-static bool refuse_attention(long q_tokens, int n_seq, int heads, int kv_heads, int head_dim, int type, int block, float scale) {
+static bool refuse_attention(long q_tokens, long n_seq, long heads, long kv_heads, long head_dim, long type, long block, double scale) {
     return (type != BB_BF16 && type != BB_F16) || (head_dim != 64 && head_dim != 128) || q_tokens < 0 || q_tokens > BB_MAX_TOKENS || n_seq < 0 || n_seq > BB_MAX_TOKENS || heads < 1 ||
-           heads > BB_MAX_HEADS || kv_heads < 1 || heads % kv_heads || block < 0 || !(scale > 0) || !(scale < INFINITY);
+           heads > BB_MAX_HEADS || kv_heads < 1 || heads % kv_heads || block < 0 || block > 0x7FFFFFFF || !((float)scale > 0) || !((float)scale * 1.45f < INFINITY);
 }
-// How many row tiles there can be, whatever the lengths, and into how many parts the keys are cut: few enough that joining them costs little, so many that the chip has
-// work.  Lengths stand on the device: tables count with their width, packed keys with their mean.
+// How many row tiles there can be, whatever the lengths, and how their keys are shared out: into how many parts, to one or two halves of a workgroup, and whether a prefix is taken once
+// for its group, as parts of its own, or again by every branch before its own keys.  Lengths stand on the device: tables count with their width, packed keys with their mean, sequences
+// as equally long.  The least of a rough account of the time, us: ITEM for a workgroup's first loads and its last stores; a row tile on 64 keys ALONE on a CU, BOTH with another
+// workgroup on it, or, two of them, by two halves; the join's launch, and its bytes per us.
 static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim) {
+    const double ITEM = 4.5, NEXT = 1.5, BOTH = 2.0, ALONE = 1.15, HALVES = 2.15, MERGE = 1.5, JOIN = 4.5, JOIN_BYTES = 3e6;
+    static const int counts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32};
     const long rows = (long)a.q_tokens * a.each;
     const long own = (rows + (KV_ROWS - 1) * (long)a.n_seq) / KV_ROWS, pre = prefix_keys > 0 ? (rows + (KV_ROWS - 1) * (long)a.n_groups) / KV_ROWS : 0;
-    // (tiles that sequences of equal lengths would have)
     const long own_like = std::max(1L, a.n_seq * ((rows / a.n_seq + KV_ROWS - 1) / KV_ROWS)), pre_like = pre ? std::max(1L, a.n_groups * ((rows / a.n_groups + KV_ROWS - 1) / KV_ROWS)) : 0;
-    const long own_cols = std::max(1L, (own_keys + 63) / 64), pre_cols = std::max(1L, (prefix_keys + 63) / 64);
-    // us: a row tile on 64 keys where two workgroups share a CU / where one has it, what an item takes besides, the join's launch and its bytes per us
-    const double both = 2.0, alone = 1.3, item = 2.5, join = 3.0, join_bytes = 3e6;
-    const long most = std::max(own_cols, pre_cols);
-    long own_parts = 1, pre_parts = pre ? 1 : 0;
+    const long own_cols = std::max(1L, (own_keys + 63) / 64), pre_cols = (prefix_keys + 63) / 64;
+    const double scale = head_dim / 128.0;
+    long own_parts = 1, pre_parts = 0;
     double best = 0;
-    a.halves = 1;
-    for (int halves = 1; halves <= 2; ++halves)
-        for (long c = most, last = 0; c >= 1 && (c >= KV_LEAST_TILES || c == most); c = c * 7 / 8) {
-            const long op = std::min<long>((own_cols + c - 1) / c, KV_MOST_PARTS), pp = pre ? std::min<long>((pre_cols + c - 1) / c, KV_MOST_PARTS) : 0;
-            if (op + pp == last) continue;
-            last = op + pp;
-            auto rounds = [&](long cols, long parts) { return (double)(((cols + parts - 1) / parts + halves - 1) / halves); };
-            const double oc = rounds(own_cols, op), pc = pp ? rounds(pre_cols, pp) : 0, oi = (double)own_like * op * a.kv_heads, pi = (double)pre_like * pp * a.kv_heads;
-            const bool full = halves == 2 || oi + pi > 256;
-            const double u = full ? both : alone, all = (oi * (item + oc * u) + pi * (item + pc * u)) / (halves == 1 && full ? 512 : 256);
-            const double cost = std::max(all, item + u * std::max(oc, pc)) + (op + pp > 1 ? join + (double)rows * a.kv_heads * (op + pp) * head_dim * 8 / join_bytes : 0);
-            if (best == 0 || cost < best) { best = cost; own_parts = op; pre_parts = pp; a.halves = halves; }
-        }
-    if ((own * own_parts + pre * pre_parts) * a.kv_heads > 0x7FFFFFFF || ((long)a.q_tokens * a.heads + 3L * a.n_seq) / 2 > 0x7FFFFFFF) return false;
-    a.own_tiles = (int)own; a.own_split = (int)own_parts; a.prefix_tiles = (int)pre; a.prefix_split = (int)pre_parts;
+    for (int apart = 0; apart <= (pre ? 1 : 0); ++apart)
+        for (int halves = 1; halves <= 2; ++halves)
+            for (int parts : counts) {
+                // (apart: as many for the longer of the two, of that length for the other)
+                const long cols = apart ? std::max(own_cols, pre_cols) : own_cols + pre_cols, c = (cols + parts - 1) / parts;
+                if (parts > 1 && c < KV_LEAST_TILES) break;
+                const long op = apart ? std::min<long>((own_cols + c - 1) / c, parts) : parts, pp = apart ? std::min<long>((pre_cols + c - 1) / c, parts) : 0;
+                auto rounds = [&](long n, long of) { return (double)(((n + of - 1) / of + halves - 1) / halves); };
+                const double oc = rounds(apart ? own_cols : cols, op), pc = apart ? rounds(pre_cols, pp) : 0, oi = (double)own_like * op * a.kv_heads, pi = (double)pre_like * pp * a.kv_heads;
+                const bool full = oi + pi > 256;
+                const double u = scale * (halves == 2 ? HALVES : full ? BOTH : ALONE), slots = halves == 1 && full ? 512 : 256, next = NEXT + (halves == 2 ? MERGE : 0);
+                const double all = (oi * (next + oc * u) + pi * (next + pc * u)) / slots, longest = next + u * std::max(oc, pc);
+                const double cost = ITEM + std::max(all, longest) + (op + pp > 1 ? JOIN + (double)rows * a.kv_heads * (op + pp) * head_dim * 8 / JOIN_BYTES : 0);
+                if (best == 0 || cost < best) { best = cost; own_parts = op; pre_parts = pp; a.halves = halves; }
+            }
+    if ((own * own_parts + pre * pre_parts) * a.kv_heads > 0x7FFFFFFF || ((long)a.q_tokens * a.heads + 3L * a.n_seq) / 2 > 0x7FFFFFFF || rows + KV_ROWS > 0x7FFFFFFF) return false;
+    a.own_tiles = (int)own; a.own_split = (int)own_parts; a.prefix_tiles = pre_parts ? (int)pre : 0; a.prefix_split = (int)pre_parts;
+    a.by_kv_heads = Divide::by(a.kv_heads); a.by_each = Divide::by(a.each); a.by_block = Divide::by(std::max(a.block, 1)); a.by_own_split = Divide::by(a.own_split);
+    a.by_prefix_split = Divide::by(std::max(a.prefix_split, 1));
     return true;
 }
 static size_t parts_bytes(const KvArgs& a, int head_dim) {
     const size_t parts = a.own_split + a.prefix_split;
     return parts > 1 ? align_up((size_t)a.q_tokens * a.heads * parts * head_dim * 4, 256) + align_up((size_t)a.q_tokens * a.heads * parts * 8, 256) : 0;
 }
-static int place_parts(KvArgs& a, int head_dim, void* workspace_dev, size_t workspace_bytes) {
+template <bool PAGED> static int run_kv(KvArgs& a, int type, int head_dim, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
     const size_t need = parts_bytes(a, head_dim);
-    if (need == 0) return BB_OK;
-    if (workspace_bytes < need) return BB_ENOMEM;
-    if (!workspace_dev || (uintptr_t)workspace_dev % 256) return BB_EINVAL;
-    a.part_o = (float*)workspace_dev;
-    a.part_ml = (float2*)((char*)workspace_dev + align_up((size_t)a.q_tokens * a.heads * (a.own_split + a.prefix_split) * head_dim * 4, 256));
-    return BB_OK;
+    if (need > 0) {
+        if (workspace_bytes < need) return BB_ENOMEM;
+        if (!workspace_dev || (uintptr_t)workspace_dev % 256) return BB_EINVAL;
+        a.part_o = (float*)workspace_dev;
+        a.part_ml = (float2*)((char*)workspace_dev + align_up((size_t)a.q_tokens * a.heads * (a.own_split + a.prefix_split) * head_dim * 4, 256));
+    }
+    launch_kv<PAGED>(a, type, head_dim, (hipStream_t)hip_stream);
+    return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
 }
 // Within a tile offsets are of 32 bits.
 static bool far_rows(long ts) { return ts > 1 << 23; }
+static bool refuse_ints(const void* p) { return !p || (uintptr_t)p % 4; }
 
-static bool refuse_tables(int n_groups, int own_width, int prefix_width) {
-    return n_groups < 0 || n_groups > BB_MAX_TOKENS || own_width < 0 || own_width > BB_MAX_PAGES || prefix_width < 0 || prefix_width > BB_MAX_PAGES;
+static bool refuse_sizes(const bb_attention_args* x) {
+    return !x || refuse_attention(x->q_tokens, x->sequences, x->heads, x->kv_heads, x->head_dim, x->type, x->block, x->scale) || x->k_tokens < 0 || x->k_tokens > BB_MAX_TOKENS;
 }
-
-extern "C" size_t bb_attention_workspace_bytes(long q_tokens, long k_tokens, int n_seq, int heads, int kv_heads, int head_dim) {
-    if (refuse_attention(q_tokens, n_seq, heads, kv_heads, head_dim, BB_BF16, 0, 1.f) || k_tokens < 0 || k_tokens > BB_MAX_TOKENS || q_tokens == 0 || n_seq == 0) return 0;
+static bool plan(KvArgs& a, const bb_attention_args* x) {
+    a.n_seq = (int)x->sequences; a.q_tokens = (int)x->q_tokens; a.k_tokens = (int)x->k_tokens; a.heads = (int)x->heads; a.kv_heads = (int)x->kv_heads; a.each = a.heads / a.kv_heads;
+    a.block = (int)x->block; a.scale = (float)x->scale * 1.44269504089f;
+    return plan_parts(a, x->k_tokens / x->sequences, 0, (int)x->head_dim);
+}
+extern "C" size_t bb_attention_workspace_bytes(const bb_attention_args* x) {
     KvArgs a{};
-    a.q_tokens = (int)q_tokens; a.n_seq = n_seq; a.heads = heads; a.kv_heads = kv_heads; a.each = heads / kv_heads;
-    return plan_parts(a, k_tokens / n_seq, 0, head_dim) ? parts_bytes(a, head_dim) : 0;
+    return refuse_sizes(x) || x->q_tokens == 0 || x->sequences == 0 || !plan(a, x) ? 0 : parts_bytes(a, (int)x->head_dim);
 }
-
-extern "C" int bb_attention(const void* q_dev, long q_token, long q_head, const void* k_dev, long k_token, long k_head, const void* v_dev, long v_token, long v_head,
-                            const int32_t* q_starts_dev, const int32_t* k_starts_dev, int n_seq, long q_tokens, long k_tokens, int heads, int kv_heads, int head_dim,
-                            int type, int block, float scale, void* out_dev, long o_token, long o_head, float* lse_dev, void* workspace_dev, size_t workspace_bytes,
-                            void* hip_stream) {
-    if (refuse_attention(q_tokens, n_seq, heads, kv_heads, head_dim, type, block, scale) || k_tokens < 0 || k_tokens > BB_MAX_TOKENS) return BB_EINVAL;
-    if (q_tokens == 0 || n_seq == 0) return BB_OK;
-    if (!q_starts_dev || !k_starts_dev || (uintptr_t)q_starts_dev % 4 || (uintptr_t)k_starts_dev % 4 || (uintptr_t)lse_dev % 4) return BB_EINVAL;
-    const HeadView q = heads_view(q_dev, q_tokens, q_token, heads, q_head, head_dim, 2), o = heads_view(out_dev, q_tokens, o_token, heads, o_head, head_dim, 2);
+extern "C" int bb_attention(const bb_attention_args* x, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    if (refuse_sizes(x)) return BB_EINVAL;
+    if (x->q_tokens == 0 || x->sequences == 0) return BB_OK;
+    if (refuse_ints(x->q_starts) || refuse_ints(x->k_starts) || (uintptr_t)x->lse % 4) return BB_EINVAL;
+    const int heads = (int)x->heads, kv_heads = (int)x->kv_heads, dim = (int)x->head_dim;
+    const HeadView q = heads_view(x->q, x->q_tokens, x->q_token, heads, x->q_head, dim, 2), o = heads_view(x->out, x->q_tokens, x->o_token, heads, x->o_head, dim, 2);
+    const HeadView k = heads_view(x->k, x->k_tokens, x->k_token, kv_heads, x->k_head, dim, 2), v = heads_view(x->v, x->k_tokens, x->v_token, kv_heads, x->v_head, dim, 2);
     if (refuse_view(q) || refuse_pieces(q) || refuse_out_view(o) || refuse_pieces(o) || overlap(o, q)) return BB_EINVAL;
-    if (k_tokens > 0) {
-        const HeadView k = heads_view(k_dev, k_tokens, k_token, kv_heads, k_head, head_dim, 2), v = heads_view(v_dev, k_tokens, v_token, kv_heads, v_head, head_dim, 2);
-        if (refuse_view(k) || refuse_pieces(k) || refuse_view(v) || refuse_pieces(v) || far_rows(k.s[0]) || far_rows(v.s[0]) || overlap(o, k) || overlap(o, v)) return BB_EINVAL;
-    }
+    if (x->k_tokens > 0 && (refuse_view(k) || refuse_pieces(k) || refuse_view(v) || refuse_pieces(v) || far_rows(k.s[0]) || far_rows(v.s[0]) || overlap(o, k) || overlap(o, v))) return BB_EINVAL;
     KvArgs a{};
-    a.q = (const char*)q_dev; a.q_ts = q_token; a.q_hs = q_head; a.k = (const char*)k_dev; a.k_ts = k_tokens > 1 ? k_token : 0; a.k_hs = k_head;
-    a.v = (const char*)v_dev; a.v_ts = k_tokens > 1 ? v_token : 0; a.v_hs = v_head; a.out = (char*)out_dev; a.o_ts = o_token; a.o_hs = o_head; a.lse = lse_dev;
-    a.q_starts = q_starts_dev; a.k_starts = k_starts_dev; a.n_seq = n_seq; a.q_tokens = (int)q_tokens; a.k_tokens = (int)k_tokens;
-    a.heads = heads; a.each = heads / kv_heads; a.block = block; a.scale = scale * 1.44269504089f;
-    a.kv_heads = kv_heads;
-    if (!plan_parts(a, k_tokens / n_seq, 0, head_dim)) return BB_EINVAL;
-    if (const int rc = place_parts(a, head_dim, workspace_dev, workspace_bytes)) return rc;
-    launch_kv<false>(a, type, head_dim, (hipStream_t)hip_stream);
-    return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
+    if (!plan(a, x)) return BB_EINVAL;
+    // (strides as the views have them: none over a single token or head)
+    a.q = (const char*)x->q; a.q_ts = q.s[0]; a.q_hs = q.s[1]; a.k = (const char*)x->k; a.k_ts = k.s[0]; a.k_hs = k.s[1]; a.v = (const char*)x->v; a.v_ts = v.s[0]; a.v_hs = v.s[1];
+    a.out = (char*)x->out; a.o_ts = o.s[0]; a.o_hs = o.s[1]; a.lse = x->lse; a.q_starts = x->q_starts; a.k_starts = x->k_starts;
+    return run_kv<false>(a, (int)x->type, dim, workspace_dev, workspace_bytes, hip_stream);
 }
 
-extern "C" size_t bb_shared_attention_workspace_bytes(long q_tokens, int n_branches, int n_groups, int own_width, int prefix_width, int heads, int kv_heads, int head_dim) {
-    if (refuse_attention(q_tokens, n_branches, heads, kv_heads, head_dim, BB_BF16, 0, 1.f) || refuse_tables(n_groups, own_width, prefix_width) || q_tokens == 0 || n_branches == 0) return 0;
-    KvArgs a{};
-    a.q_tokens = (int)q_tokens; a.n_seq = n_branches; a.n_groups = n_groups; a.heads = heads; a.kv_heads = kv_heads; a.each = heads / kv_heads;
-    return plan_parts(a, 64L * own_width, n_groups ? 64L * prefix_width : 0, head_dim) ? parts_bytes(a, head_dim) : 0;
+static bool refuse_sizes(const bb_shared_attention_args* x) {
+    return !x || refuse_attention(x->q_tokens, x->branches, x->heads, x->kv_heads, x->head_dim, x->type, x->block, x->scale) || x->groups < 0 || x->groups > BB_MAX_TOKENS ||
+           x->own_width < 0 || x->own_width > BB_MAX_PAGES || (x->groups > 0 && (x->prefix_width < 0 || x->prefix_width > BB_MAX_PAGES));
 }
-
-extern "C" int bb_shared_attention(const void* q_dev, long q_token, long q_head, const int32_t* q_starts_dev, int n_branches, long q_tokens, const void* k_cache_dev, long kc_page,
-                                   long kc_head, long kc_token, const void* v_cache_dev, long vc_page, long vc_head, long vc_token, int n_pages, const int32_t* own_pages_dev,
-                                   long own_ld, int own_width, const int32_t* own_lens_dev, const int32_t* prefix_pages_dev, long prefix_ld, int prefix_width,
-                                   const int32_t* prefix_lens_dev, const int32_t* group_starts_dev, int n_groups, int heads, int kv_heads, int head_dim, int type, int block,
-                                   float scale, void* out_dev, long o_token, long o_head, float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
-    if (refuse_attention(q_tokens, n_branches, heads, kv_heads, head_dim, type, block, scale) || refuse_tables(n_groups, own_width, prefix_width) || n_pages < 1 || n_pages > BB_MAX_PAGES || (n_branches > 1 && own_ld < 0) || (n_groups > 1 && prefix_ld < 0))
-        return BB_EINVAL;
-    if (q_tokens == 0 || n_branches == 0) return BB_OK;
-    if (!q_starts_dev || !own_lens_dev || (own_width > 0 && !own_pages_dev) || (uintptr_t)q_starts_dev % 4 || (uintptr_t)own_pages_dev % 4 || (uintptr_t)own_lens_dev % 4 ||
-        (uintptr_t)lse_dev % 4) return BB_EINVAL;
-    if (n_groups > 0 && (!prefix_lens_dev || !group_starts_dev || (prefix_width > 0 && !prefix_pages_dev) || (uintptr_t)prefix_pages_dev % 4 || (uintptr_t)prefix_lens_dev % 4 ||
-                         (uintptr_t)group_starts_dev % 4)) return BB_EINVAL;
-    const HeadView q = heads_view(q_dev, q_tokens, q_token, heads, q_head, head_dim, 2), o = heads_view(out_dev, q_tokens, o_token, heads, o_head, head_dim, 2);
-    const HeadView k = pages_view(k_cache_dev, n_pages, kc_page, kv_heads, kc_head, kc_token, head_dim, 2);
-    const HeadView v = pages_view(v_cache_dev, n_pages, vc_page, kv_heads, vc_head, vc_token, head_dim, 2);
+static bool plan(KvArgs& a, const bb_shared_attention_args* x) {
+    a.n_seq = (int)x->branches; a.q_tokens = (int)x->q_tokens; a.heads = (int)x->heads; a.kv_heads = (int)x->kv_heads; a.each = a.heads / a.kv_heads;
+    a.block = (int)x->block; a.scale = (float)x->scale * 1.44269504089f;
+    a.own_width = (int)x->own_width; a.n_groups = (int)x->groups; a.prefix_width = x->groups ? (int)x->prefix_width : 0;
+    return plan_parts(a, 64L * a.own_width, 64L * a.prefix_width, (int)x->head_dim);
+}
+extern "C" size_t bb_shared_attention_workspace_bytes(const bb_shared_attention_args* x) {
+    KvArgs a{};
+    return refuse_sizes(x) || x->q_tokens == 0 || x->branches == 0 || !plan(a, x) ? 0 : parts_bytes(a, (int)x->head_dim);
+}
+extern "C" int bb_shared_attention(const bb_shared_attention_args* x, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    if (refuse_sizes(x) || x->pages < 1 || x->pages > BB_MAX_PAGES || (x->branches > 1 && x->own_ld < 0) || (x->groups > 1 && x->prefix_ld < 0) ||
+        x->own_ld > HEADS_MAX_STRIDE || (x->groups > 0 && x->prefix_ld > HEADS_MAX_STRIDE)) return BB_EINVAL;
+    if (x->q_tokens == 0 || x->branches == 0) return BB_OK;
+    if (refuse_ints(x->q_starts) || refuse_ints(x->own_lens) || (x->own_width > 0 && refuse_ints(x->own_pages)) || (uintptr_t)x->lse % 4) return BB_EINVAL;
+    if (x->groups > 0 && (refuse_ints(x->prefix_lens) || refuse_ints(x->group_starts) || (x->prefix_width > 0 && refuse_ints(x->prefix_pages)))) return BB_EINVAL;
+    const int heads = (int)x->heads, kv_heads = (int)x->kv_heads, dim = (int)x->head_dim;
+    const HeadView q = heads_view(x->q, x->q_tokens, x->q_token, heads, x->q_head, dim, 2), o = heads_view(x->out, x->q_tokens, x->o_token, heads, x->o_head, dim, 2);
+    const HeadView k = pages_view(x->k_cache, x->pages, x->kc_page, kv_heads, x->kc_head, x->kc_token, dim, 2), v = pages_view(x->v_cache, x->pages, x->vc_page, kv_heads, x->vc_head, x->vc_token, dim, 2);
     if (refuse_view(q) || refuse_pieces(q) || refuse_out_view(o) || refuse_pieces(o) || refuse_view(k) || refuse_pieces(k) || refuse_view(v) || refuse_pieces(v) ||
-        far_rows(kc_token) || far_rows(vc_token) || overlap(o, q) || overlap(o, k) || overlap(o, v)) return BB_EINVAL;
+        far_rows(x->kc_token) || far_rows(x->vc_token) || overlap(o, q) || overlap(o, k) || overlap(o, v)) return BB_EINVAL;
     KvArgs a{};
-    a.q = (const char*)q_dev; a.q_ts = q_token; a.q_hs = q_head; a.k = (const char*)k_cache_dev; a.k_ps = kc_page; a.k_ts = kc_token; a.k_hs = kc_head;
-    a.v = (const char*)v_cache_dev; a.v_ps = vc_page; a.v_ts = vc_token; a.v_hs = vc_head; a.out = (char*)out_dev; a.o_ts = o_token; a.o_hs = o_head; a.lse = lse_dev;
-    a.q_starts = q_starts_dev; a.n_seq = n_branches; a.q_tokens = (int)q_tokens; a.own_pages = own_pages_dev; a.own_ld = own_ld; a.own_lens = own_lens_dev; a.own_width = own_width;
-    a.prefix_pages = prefix_pages_dev; a.prefix_ld = prefix_ld; a.prefix_lens = prefix_lens_dev; a.prefix_width = prefix_width; a.group_starts = group_starts_dev; a.n_groups = n_groups;
-    a.n_pages = n_pages; a.heads = heads; a.each = heads / kv_heads; a.block = block; a.scale = scale * 1.44269504089f;
-    a.kv_heads = kv_heads;
-    if (!plan_parts(a, 64L * own_width, n_groups ? 64L * prefix_width : 0, head_dim)) return BB_EINVAL;
-    if (const int rc = place_parts(a, head_dim, workspace_dev, workspace_bytes)) return rc;
-    launch_kv<true>(a, type, head_dim, (hipStream_t)hip_stream);
-    return hipGetLastError() == hipSuccess ? BB_OK : BB_EHIP;
+    if (!plan(a, x)) return BB_EINVAL;
+    a.q = (const char*)x->q; a.q_ts = q.s[0]; a.q_hs = q.s[1]; a.k = (const char*)x->k_cache; a.k_ps = k.s[0]; a.k_hs = k.s[1]; a.k_ts = k.s[2];
+    a.v = (const char*)x->v_cache; a.v_ps = v.s[0]; a.v_hs = v.s[1]; a.v_ts = v.s[2]; a.out = (char*)x->out; a.o_ts = o.s[0]; a.o_hs = o.s[1]; a.lse = x->lse;
+    a.q_starts = x->q_starts; a.own_pages = x->own_pages; a.own_ld = x->branches > 1 ? x->own_ld : 0; a.own_lens = x->own_lens;
+    a.prefix_pages = x->prefix_pages; a.prefix_ld = x->groups > 1 ? x->prefix_ld : 0; a.prefix_lens = x->prefix_lens; a.group_starts = x->group_starts; a.n_pages = (int)x->pages;
+    return run_kv<true>(a, (int)x->type, dim, workspace_dev, workspace_bytes, hip_stream);
 }

@@ -190,50 +190,49 @@ extern "C" int bb_rope_frequencies(double* freqs_host, int rot, double base, dou
     return BB_OK;
 }
 
-static bool refuse_turn(const int32_t* positions, const double* freqs, int rot, float magnitude, long tokens, int q_heads, int kv_heads, int dim, int type) {
+// What both entries have in common.
+static bool refuse_turn(const int32_t* positions, const double* freqs, long rot, double magnitude, long tokens, long q_heads, long kv_heads, long dim, long type) {
     return (type != BB_F32 && type != BB_BF16 && type != BB_F16) || dim < 1 || dim > BB_ROPE_MAX_DIM || rot < 0 || rot > dim || rot % 2 || tokens < 0 || tokens > BB_MAX_TOKENS ||
-           q_heads < 0 || kv_heads < 0 || q_heads > BB_MAX_HEADS || kv_heads > BB_MAX_HEADS || !(fabsf(magnitude) < INFINITY) ||
+           q_heads < 0 || kv_heads < 0 || q_heads > BB_MAX_HEADS || kv_heads > BB_MAX_HEADS || !(fabs(magnitude) <= 3e38) ||
            (tokens > 0 && (!positions || (uintptr_t)positions % 4 || (rot > 0 && (!freqs || (uintptr_t)freqs % 8))));
 }
-
-extern "C" int bb_rope(const void* q_dev, long q_token, long q_head, void* q_out_dev, long qo_token, long qo_head, int q_heads, const void* k_dev, long k_token, long k_head,
-                       void* k_out_dev, long ko_token, long ko_head, int k_heads, const int32_t* positions_dev, const double* freqs_dev, int rot, int interleaved,
-                       float magnitude, long tokens, int head_dim, int type, void* hip_stream) {
-    if (refuse_turn(positions_dev, freqs_dev, rot, magnitude, tokens, q_heads, k_heads, head_dim, type)) return BB_EINVAL;
-    if (tokens == 0 || q_heads + k_heads == 0) return BB_OK;
-    const int size = type == BB_F32 ? 4 : 2;
-    const HeadView q = heads_view(q_dev, tokens, q_token, q_heads, q_head, head_dim, size), k = heads_view(k_dev, tokens, k_token, k_heads, k_head, head_dim, size);
-    const HeadView qo = heads_view(q_out_dev, tokens, qo_token, q_heads, qo_head, head_dim, size), ko = heads_view(k_out_dev, tokens, ko_token, k_heads, ko_head, head_dim, size);
-    if (q_heads && (refuse_view(q) || refuse_out_view(qo) || (!same_rows(q, qo) && overlap(q, qo)))) return BB_EINVAL;
-    if (k_heads && (refuse_view(k) || refuse_out_view(ko) || (!same_rows(k, ko) && overlap(k, ko)))) return BB_EINVAL;
-    if (q_heads && k_heads && (overlap(qo, ko) || overlap(q, ko) || overlap(k, qo))) return BB_EINVAL;
-    RopeArgs a{};
-    a.q = (const char*)q_dev; a.q_ts = q_token; a.q_hs = q_head; a.qo = (char*)q_out_dev; a.qo_ts = qo_token; a.qo_hs = qo_head; a.q_heads = q_heads;
-    a.k = (const char*)k_dev; a.k_ts = k_token; a.k_hs = k_head; a.ko = (char*)k_out_dev; a.ko_ts = ko_token; a.ko_hs = ko_head; a.k_heads = k_heads;
-    a.positions = positions_dev; a.freqs = freqs_dev; a.rot = rot; a.interleaved = interleaved; a.magnitude = magnitude; a.tokens = tokens; a.dim = head_dim;
-    return launch_rope(a, type, (hipStream_t)hip_stream);
+template <class A> static void common_args(RopeArgs& a, const A* x) {
+    a.q = (const char*)x->q; a.q_ts = x->q_token; a.q_hs = x->q_head; a.qo = (char*)x->q_out; a.qo_ts = x->qo_token; a.qo_hs = x->qo_head; a.q_heads = (int)x->q_heads;
+    a.k = (const char*)x->k; a.k_ts = x->k_token; a.k_hs = x->k_head;
+    a.positions = x->positions; a.freqs = x->freqs; a.rot = (int)x->rot; a.interleaved = x->interleaved != 0; a.magnitude = (float)x->magnitude; a.tokens = x->tokens; a.dim = (int)x->head_dim;
 }
 
-extern "C" int bb_rope_append(const void* q_dev, long q_token, long q_head, void* q_out_dev, long qo_token, long qo_head, int q_heads, const void* k_dev, long k_token, long k_head,
-                              const void* v_dev, long v_token, long v_head, int kv_heads, const int32_t* positions_dev, const double* freqs_dev, int rot, int interleaved,
-                              float magnitude, const int32_t* slots_dev, void* k_cache_dev, long kc_page, long kc_head, long kc_token, void* v_cache_dev, long vc_page,
-                              long vc_head, long vc_token, int n_pages, long tokens, int head_dim, int type, void* hip_stream) {
-    if (refuse_turn(positions_dev, freqs_dev, rot, magnitude, tokens, q_heads, kv_heads, head_dim, type) || kv_heads < 1 || n_pages < 1 || n_pages > BB_MAX_PAGES) return BB_EINVAL;
-    if (tokens == 0) return BB_OK;
-    const int size = type == BB_F32 ? 4 : 2;
-    const HeadView q = heads_view(q_dev, tokens, q_token, q_heads, q_head, head_dim, size), qo = heads_view(q_out_dev, tokens, qo_token, q_heads, qo_head, head_dim, size);
-    const HeadView k = heads_view(k_dev, tokens, k_token, kv_heads, k_head, head_dim, size), v = heads_view(v_dev, tokens, v_token, kv_heads, v_head, head_dim, size);
-    const HeadView kc = pages_view(k_cache_dev, n_pages, kc_page, kv_heads, kc_head, kc_token, head_dim, size);
-    const HeadView vc = pages_view(v_cache_dev, n_pages, vc_page, kv_heads, vc_head, vc_token, head_dim, size);
-    if (!slots_dev || (uintptr_t)slots_dev % 4 || refuse_view(k) || refuse_view(v) || refuse_out_view(kc) || refuse_out_view(vc)) return BB_EINVAL;
-    if (overlap(kc, vc) || overlap(kc, k) || overlap(kc, v) || overlap(vc, k) || overlap(vc, v)) return BB_EINVAL;
-    if (q_heads && (refuse_view(q) || refuse_out_view(qo) || (!same_rows(q, qo) && overlap(q, qo)) || overlap(qo, k) || overlap(qo, v) || overlap(qo, kc) || overlap(qo, vc) ||
-                    overlap(q, kc) || overlap(q, vc))) return BB_EINVAL;
+extern "C" int bb_rope(const bb_rope_args* x, void* hip_stream) {
+    if (!x || refuse_turn(x->positions, x->freqs, x->rot, x->magnitude, x->tokens, x->q_heads, x->k_heads, x->head_dim, x->type)) return BB_EINVAL;
+    if (x->tokens == 0 || x->q_heads + x->k_heads == 0) return BB_OK;
+    const int size = x->type == BB_F32 ? 4 : 2, dim = (int)x->head_dim;
+    const HeadView q = heads_view(x->q, x->tokens, x->q_token, (int)x->q_heads, x->q_head, dim, size), qo = heads_view(x->q_out, x->tokens, x->qo_token, (int)x->q_heads, x->qo_head, dim, size);
+    const HeadView k = heads_view(x->k, x->tokens, x->k_token, (int)x->k_heads, x->k_head, dim, size), ko = heads_view(x->k_out, x->tokens, x->ko_token, (int)x->k_heads, x->ko_head, dim, size);
+    if (x->q_heads && (refuse_view(q) || refuse_out_view(qo) || (!same_rows(q, qo) && overlap(q, qo)))) return BB_EINVAL;
+    if (x->k_heads && (refuse_view(k) || refuse_out_view(ko) || (!same_rows(k, ko) && overlap(k, ko)))) return BB_EINVAL;
+    if (x->q_heads && x->k_heads && (overlap(qo, ko) || overlap(q, ko) || overlap(k, qo))) return BB_EINVAL;
     RopeArgs a{};
-    a.q = (const char*)q_dev; a.q_ts = q_token; a.q_hs = q_head; a.qo = (char*)q_out_dev; a.qo_ts = qo_token; a.qo_hs = qo_head; a.q_heads = q_heads;
-    a.k = (const char*)k_dev; a.k_ts = k_token; a.k_hs = k_head; a.ko = (char*)k_cache_dev; a.ko_ps = kc_page; a.ko_ts = kc_token; a.ko_hs = kc_head; a.k_heads = kv_heads;
-    a.v = (const char*)v_dev; a.v_ts = v_token; a.v_hs = v_head; a.vo = (char*)v_cache_dev; a.vo_ps = vc_page; a.vo_ts = vc_token; a.vo_hs = vc_head;
-    a.positions = positions_dev; a.freqs = freqs_dev; a.rot = rot; a.interleaved = interleaved; a.magnitude = magnitude; a.slots = slots_dev; a.n_slots = (long)n_pages * 64;
-    a.tokens = tokens; a.dim = head_dim;
-    return launch_rope(a, type, (hipStream_t)hip_stream);
+    common_args(a, x);
+    a.ko = (char*)x->k_out; a.ko_ts = x->ko_token; a.ko_hs = x->ko_head; a.k_heads = (int)x->k_heads;
+    return launch_rope(a, (int)x->type, (hipStream_t)hip_stream);
+}
+
+extern "C" int bb_rope_append(const bb_rope_append_args* x, void* hip_stream) {
+    if (!x || refuse_turn(x->positions, x->freqs, x->rot, x->magnitude, x->tokens, x->q_heads, x->kv_heads, x->head_dim, x->type) || x->kv_heads < 1 || x->pages < 1 || x->pages > BB_MAX_PAGES)
+        return BB_EINVAL;
+    if (x->tokens == 0) return BB_OK;
+    const int size = x->type == BB_F32 ? 4 : 2, dim = (int)x->head_dim, kv = (int)x->kv_heads;
+    const HeadView q = heads_view(x->q, x->tokens, x->q_token, (int)x->q_heads, x->q_head, dim, size), qo = heads_view(x->q_out, x->tokens, x->qo_token, (int)x->q_heads, x->qo_head, dim, size);
+    const HeadView k = heads_view(x->k, x->tokens, x->k_token, kv, x->k_head, dim, size), v = heads_view(x->v, x->tokens, x->v_token, kv, x->v_head, dim, size);
+    const HeadView kc = pages_view(x->k_cache, x->pages, x->kc_page, kv, x->kc_head, x->kc_token, dim, size), vc = pages_view(x->v_cache, x->pages, x->vc_page, kv, x->vc_head, x->vc_token, dim, size);
+    if (!x->slots || (uintptr_t)x->slots % 4 || refuse_view(k) || refuse_view(v) || refuse_out_view(kc) || refuse_out_view(vc)) return BB_EINVAL;
+    if (overlap(kc, vc) || overlap(kc, k) || overlap(kc, v) || overlap(vc, k) || overlap(vc, v)) return BB_EINVAL;
+    if (x->q_heads && (refuse_view(q) || refuse_out_view(qo) || (!same_rows(q, qo) && overlap(q, qo)) || overlap(qo, k) || overlap(qo, v) || overlap(qo, kc) || overlap(qo, vc) ||
+                       overlap(q, kc) || overlap(q, vc))) return BB_EINVAL;
+    RopeArgs a{};
+    common_args(a, x);
+    a.ko = (char*)x->k_cache; a.ko_ps = x->kc_page; a.ko_ts = x->kc_token; a.ko_hs = x->kc_head; a.k_heads = kv;
+    a.v = (const char*)x->v; a.v_ts = x->v_token; a.v_hs = x->v_head; a.vo = (char*)x->v_cache; a.vo_ps = x->vc_page; a.vo_ts = x->vc_token; a.vo_hs = x->vc_head;
+    a.slots = x->slots; a.n_slots = x->pages * BB_PAGE_TOKENS;
+    return launch_rope(a, (int)x->type, (hipStream_t)hip_stream);
 }

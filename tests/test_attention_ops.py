@@ -1,10 +1,13 @@
 """Attention over packed prompts and attention of branches that share a prefix, against their definitions in 64 bits, row by row: types, heads, lengths, masks, rows that
 see nothing, pages that end inside a tile, values that must not be read, strides, streams, graphs and refusals.  Tolerances: kv_oracle.rows_of."""
+import os
+import re
+
 import pytest
 import torch
 
 import paper_2605_29233_amd as bb
-from paper_2605_29233_amd import BBError
+from paper_2605_29233_amd import BBError, binding
 from kv_oracle import DEV, PAGE, TYPES, attention, check, gen, ints, rnd, shared, starts
 
 HEADS = [(4, 4, 64), (6, 2, 128), (7, 1, 64), (3, 3, 128)]
@@ -408,32 +411,52 @@ def test_nothing_to_do():
     assert (out == 9).all()
 
 
+def test_argument_structs_are_packed_as_the_header_has_them():
+    """Every field has eight bytes, and the doubles stand where the binding packs them."""
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "blockbatch.h")).read()
+    for name, packed in (("rope", binding.ROPE_ARGS), ("rope_append", binding.ROPE_APPEND_ARGS), ("attention", binding.ATTENTION_ARGS), ("shared_attention", binding.SHARED_ATTENTION_ARGS)):
+        body = re.search(r"typedef struct \{([^}]*)\} bb_%s_args;" % name, header).group(1)
+        kinds = ""
+        for field in body.split(";"):
+            for _ in field.split(",") if field.strip() else ():
+                kinds += "d" if re.search(r"\bdouble (?!\*)", field) and "*" not in field else "q"
+        packed_kinds = "".join(int(n or 1) * c for n, c in re.findall(r"(\d*)([qd])", packed.format))
+        assert kinds == packed_kinds, name
+        assert packed.size == 8 * len(kinds)
+
+
 def test_c_entries_refuse_before_touching_a_device():
     """Every call below is refused on the host (the pointers are never followed)."""
     lib = bb.load_library()
     p = 1 << 20
     good = dict(q=p, qt=256, qh=64, k=2 * p, kt=128, kh=64, v=3 * p, vt=128, vh=64, qs=4 * p, ks=5 * p, n=2, qn=8, kn=9, heads=4, kv=2, dim=64, type=1, block=1, scale=0.1, o=6 * p,
-                ot=256, oh=64, lse=None, ws=None, wn=0, s=None)
+                ot=256, oh=64, lse=0)
 
     def call(**kw):
-        return lib.bb_attention(*dict(good, **kw).values())
+        return lib.bb_attention(binding.ATTENTION_ARGS.pack(*dict(good, **kw).values()), None, 0, None)
 
-    assert call(qn=0) == 0 and call(n=0) == 0
-    for bad in (dict(q=None), dict(q=p + 2), dict(qt=250), dict(qh=4), dict(k=None), dict(k=2 * p + 8), dict(kt=1 << 24), dict(v=None), dict(vh=65), dict(qs=None), dict(ks=None),
-                dict(qs=4 * p + 1), dict(n=-1), dict(qn=-1), dict(kn=-1), dict(qn=1 << 31), dict(heads=3), dict(heads=0), dict(kv=0), dict(heads=4096, kv=2), dict(dim=96), dict(dim=0),
-                dict(type=0), dict(type=7), dict(block=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(o=None), dict(ot=128), dict(oh=0),
-                dict(o=p), dict(o=2 * p), dict(o=3 * p + 128), dict(lse=6), dict(qt=-8)):
+    assert call(qn=0) == 0 and call(n=0) == 0 and lib.bb_attention(None, None, 0, None) == -1 and lib.bb_attention_workspace_bytes(None) == 0
+    for bad in (dict(q=0), dict(q=p + 2), dict(qt=250), dict(qh=4), dict(k=0), dict(k=2 * p + 8), dict(kt=1 << 24), dict(v=0), dict(vh=65), dict(qs=0), dict(ks=0),
+                dict(qs=4 * p + 1), dict(n=-1), dict(qn=-1), dict(kn=-1), dict(qn=1 << 31), dict(n=1 << 33), dict(heads=3), dict(heads=0), dict(kv=0), dict(heads=4096, kv=2), dict(dim=96),
+                dict(dim=0), dict(type=0), dict(type=7), dict(block=-1), dict(block=1 << 31), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
+                dict(scale=1e39), dict(scale=1e-60), dict(o=0), dict(ot=128), dict(oh=0), dict(o=p), dict(o=2 * p), dict(o=3 * p + 128), dict(lse=6), dict(qt=-8), dict(qt=1 << 50)):
         assert call(**bad) == -1, bad
+    # work that wants its keys in parts wants a workspace for them
+    large = dict(good, qn=16, kn=100000, n=1, k=1 << 32, v=1 << 33)
+    args = binding.ATTENTION_ARGS.pack(*large.values())
+    need = lib.bb_attention_workspace_bytes(args)
+    assert need > 0 and lib.bb_attention(args, None, 0, None) == -3 and lib.bb_attention(args, 256 * p, need - 1, None) == -3
+    assert lib.bb_attention(args, None, need, None) == -1 and lib.bb_attention(args, 256 * p + 128, need, None) == -1
     good = dict(q=p, qt=256, qh=64, qs=4 * p, n=2, qn=8, k=16 * p, kp=8192, kh=4096, kt=64, v=32 * p, vp=8192, vh=4096, vt=64, pages=4, own=5 * p, old=3, ow=3, lens=6 * p, pre=7 * p, pld=3,
-                pw=3, pl=8 * p, gs=9 * p, g=1, heads=4, kv=2, dim=64, type=1, block=1, scale=0.1, o=10 * p, ot=256, oh=64, lse=None, ws=None, wn=0, s=None)
+                pw=3, pl=8 * p, gs=9 * p, g=1, heads=4, kv=2, dim=64, type=1, block=1, scale=0.1, o=10 * p, ot=256, oh=64, lse=0)
 
     def call(**kw):
-        return lib.bb_shared_attention(*dict(good, **kw).values())
+        return lib.bb_shared_attention(binding.SHARED_ATTENTION_ARGS.pack(*dict(good, **kw).values()), None, 0, None)
 
-    assert call(qn=0) == 0 and call(n=0) == 0
-    for bad in (dict(q=None), dict(qs=None), dict(k=None), dict(k=16 * p + 2), dict(kp=100), dict(kt=1 << 24), dict(v=None), dict(pages=0), dict(pages=1 << 26), dict(own=None), dict(own=5 * p + 2),
-                dict(old=-1), dict(ow=-1), dict(lens=None), dict(pre=None), dict(pld=-1, g=2), dict(pw=-1), dict(pl=None), dict(gs=None), dict(g=-1), dict(heads=5), dict(dim=32), dict(type=0),
-                dict(block=-2), dict(scale=0.0), dict(o=None), dict(o=16 * p), dict(o=p), dict(ot=64), dict(o=10 * p + 2)):
+    assert call(qn=0) == 0 and call(n=0) == 0 and lib.bb_shared_attention(None, None, 0, None) == -1 and lib.bb_shared_attention_workspace_bytes(None) == 0
+    for bad in (dict(q=0), dict(qs=0), dict(k=0), dict(k=16 * p + 2), dict(kp=100), dict(kt=1 << 24), dict(v=0), dict(pages=0), dict(pages=1 << 26), dict(own=0), dict(own=5 * p + 2),
+                dict(old=-1), dict(ow=-1), dict(ow=1 << 33), dict(lens=0), dict(pre=0), dict(pld=-1, g=2), dict(pw=-1), dict(pl=0), dict(gs=0), dict(g=-1), dict(heads=5), dict(dim=32),
+                dict(type=0), dict(block=-2), dict(scale=0.0), dict(o=0), dict(o=16 * p), dict(o=p), dict(ot=64), dict(o=10 * p + 2)):
         assert call(**bad) == -1, bad
 
 

@@ -1,13 +1,12 @@
 """Rotary positions against their formula in 64 bits: both pairings, part of the head, far and negative positions, strides, in place, into a paged cache;
 what they refuse and what they leave alone.  Tolerances: kv_oracle.turned."""
-import ctypes as C
 import math
 
 import pytest
 import torch
 
 import paper_2605_29233_amd as bb
-from paper_2605_29233_amd import BBError
+from paper_2605_29233_amd import BBError, binding
 from kv_oracle import DEV, PAGE, TYPES, close, gen, ints, rnd, turned
 
 
@@ -163,26 +162,26 @@ def test_c_entry_refuses_before_touching_a_device():
     """Every call below is refused on the host (the pointers are never followed)."""
     lib = bb.load_library()
     p = 1 << 20
-    good = dict(q=p, qt=256, qh=64, qo=2 * p, qot=256, qoh=64, nq=4, k=3 * p, kt=128, kh=64, ko=4 * p, kot=128, koh=64, nk=2, pos=5 * p, f=6 * p, rot=64, il=0, mag=1.0, n=8, dim=64,
-                type=1, s=None)
+    good = dict(q=p, qt=256, qh=64, qo=2 * p, qot=256, qoh=64, nq=4, k=3 * p, kt=128, kh=64, ko=4 * p, kot=128, koh=64, nk=2, pos=5 * p, f=6 * p, rot=64, il=0, mag=1.0, n=8, dim=64, type=1)
 
     def call(**kw):
-        return lib.bb_rope(*dict(good, **kw).values())
+        return lib.bb_rope(binding.ROPE_ARGS.pack(*dict(good, **kw).values()), None)
 
-    assert call(n=0) == 0 and call(nq=0, nk=0) == 0
-    for bad in (dict(q=None), dict(q=p + 1), dict(qo=None), dict(k=None), dict(ko=4 * p + 1), dict(pos=None), dict(pos=5 * p + 2), dict(f=None), dict(f=6 * p + 4), dict(rot=63), dict(rot=66),
-                dict(rot=-2), dict(dim=0), dict(dim=2048, rot=64), dict(type=3), dict(type=-1), dict(n=-1), dict(nq=-1), dict(nk=5000), dict(mag=float("nan")), dict(mag=float("inf")),
-                dict(qt=-1), dict(qt=1 << 45), dict(qot=0), dict(qot=100), dict(qoh=32), dict(qo=p + 2), dict(qo=p, qot=512), dict(ko=2 * p), dict(ko=p), dict(qo=3 * p)):
+    assert call(n=0) == 0 and call(nq=0, nk=0) == 0 and lib.bb_rope(None, None) == -1 and lib.bb_rope_append(None, None) == -1
+    for bad in (dict(q=0), dict(q=p + 1), dict(qo=0), dict(k=0), dict(ko=4 * p + 1), dict(pos=0), dict(pos=5 * p + 2), dict(f=0), dict(f=6 * p + 4), dict(rot=63), dict(rot=66),
+                dict(rot=-2), dict(dim=0), dict(dim=2048, rot=64), dict(type=3), dict(type=-1), dict(n=-1), dict(n=1 << 40), dict(nq=-1), dict(nk=5000), dict(nq=1 << 32), dict(mag=float("nan")),
+                dict(mag=float("inf")), dict(mag=1e39), dict(qt=-1), dict(qt=1 << 45), dict(qt=1 << 62), dict(qot=0), dict(qot=100), dict(qoh=32), dict(qo=p + 2), dict(qo=p, qot=512),
+                dict(ko=2 * p), dict(ko=p), dict(qo=3 * p), dict(rot=1 << 33), dict(dim=1 << 32), dict(type=1 << 32)):
         assert call(**bad) == -1, bad
     good = dict(q=p, qt=256, qh=64, qo=2 * p, qot=256, qoh=64, nq=4, k=3 * p, kt=128, kh=64, v=4 * p, vt=128, vh=64, nk=2, pos=5 * p, f=6 * p, rot=64, il=0, mag=1.0, slots=7 * p,
-                kc=16 * p, kcp=8192, kch=4096, kct=64, vc=32 * p, vcp=8192, vch=4096, vct=64, pages=4, n=8, dim=64, type=1, s=None)
+                kc=16 * p, kcp=8192, kch=4096, kct=64, vc=32 * p, vcp=8192, vch=4096, vct=64, pages=4, n=8, dim=64, type=1)
 
     def call(**kw):
-        return lib.bb_rope_append(*dict(good, **kw).values())
+        return lib.bb_rope_append(binding.ROPE_APPEND_ARGS.pack(*dict(good, **kw).values()), None)
 
     assert call(n=0) == 0
-    for bad in (dict(slots=None), dict(slots=7 * p + 1), dict(kc=None), dict(vc=None), dict(v=None), dict(pages=0), dict(pages=1 << 26), dict(nk=0), dict(kcp=4096), dict(kct=32), dict(vch=64),
-                dict(vc=16 * p), dict(kc=4 * p), dict(qo=16 * p), dict(kc=16 * p + 1), dict(qo=3 * p)):
+    for bad in (dict(slots=0), dict(slots=7 * p + 1), dict(kc=0), dict(vc=0), dict(v=0), dict(pages=0), dict(pages=1 << 26), dict(pages=1 << 33), dict(nk=0), dict(kcp=4096), dict(kct=32),
+                dict(vch=64), dict(vc=16 * p), dict(kc=4 * p), dict(qo=16 * p), dict(kc=16 * p + 1), dict(qo=3 * p), dict(kcp=-8192)):
         assert call(**bad) == -1, bad
 
 
