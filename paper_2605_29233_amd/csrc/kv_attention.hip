@@ -120,31 +120,40 @@ static __device__ __forceinline__ int paged_keys(int n, int width) { return min(
 struct KeyTile { const char *k, *v; int key0, n; bool own; };
 template <int KEYS> struct Keys {
     const int *prefix, *own;        // page tables (both null: packed)
-    const char *k, *v;              // of the kv head (packed: of the first key)
-    int n_prefix, n_own;            // keys
+    const char *k, *v;              // of the kv head; packed: of the next tile's first key, as tiles are asked for in order, `step` apart
+    int n_prefix, n_own, step;      // keys
+    long k_step, v_step;            // packed: bytes to the next tile
     int ids, ids_at;                // page ids from ids_at on (-1: none yet)
+    __device__ __forceinline__ Keys(const KvArgs& a, const int* prefix, const int* own, const char* k, const char* v, int n_prefix, int n_own, int first, int step)
+        : prefix(prefix), own(own), k(k), v(v), n_prefix(n_prefix), n_own(n_own), step(step), k_step(0), v_step(0), ids(0), ids_at(-1) {
+        if (prefix || own) return;
+        this->k += (long)first * KEYS * a.k_ts * 2; this->v += (long)first * KEYS * a.v_ts * 2;
+        k_step = (long)step * KEYS * a.k_ts * 2; v_step = (long)step * KEYS * a.v_ts * 2;
+    }
     __device__ __forceinline__ KeyTile tile(const KvArgs& a, int i, int end) {
         constexpr int PER_PAGE = BB_PAGE_TOKENS / KEYS;
         KeyTile t{};
         if (i >= end) return t;
-        const int prefix_pages = (n_prefix + BB_PAGE_TOKENS - 1) / BB_PAGE_TOKENS;
+        if (!prefix && !own) {
+            t.own = true;
+            t.key0 = i * KEYS;
+            t.k = k; t.v = v;
+            k += k_step; v += v_step;
+            t.n = max(min(n_own - t.key0, KEYS), 0);            // (the second 32 of the last 64 may be none)
+            return t;
+        }
+        const int prefix_pages = (n_prefix + BB_PAGE_TOKENS - 1) / BB_PAGE_TOKENS, page = i / PER_PAGE, within = i % PER_PAGE * KEYS;
         t.own = i >= prefix_pages * PER_PAGE;
         t.key0 = (t.own ? i - prefix_pages * PER_PAGE : i) * KEYS;
-        long k_at = (long)t.key0 * a.k_ts, v_at = (long)t.key0 * a.v_ts;
-        if (own || prefix) {
-            const int page = i / PER_PAGE, within = i % PER_PAGE * KEYS;
-            if (ids_at < 0 || page >= ids_at + 64) {
-                ids_at = page;
-                const int p = page + (int)(threadIdx.x & 63), of_own = p - prefix_pages;
-                ids = of_own < 0 ? prefix[p] : of_own * BB_PAGE_TOKENS < n_own ? own[of_own] : -1;
-            }
-            const int id = __builtin_amdgcn_readlane(ids, page - ids_at);
-            if ((unsigned)id >= (unsigned)a.n_pages) return t;
-            k_at = (long)id * a.k_ps + (long)within * a.k_ts;
-            v_at = (long)id * a.v_ps + (long)within * a.v_ts;
+        if (ids_at < 0 || page >= ids_at + 64) {
+            ids_at = page;
+            const int p = page + (int)(threadIdx.x & 63), of_own = p - prefix_pages;
+            ids = of_own < 0 ? prefix[p] : of_own * BB_PAGE_TOKENS < n_own ? own[of_own] : -1;
         }
-        t.k = k + k_at * 2;
-        t.v = v + v_at * 2;
+        const int id = __builtin_amdgcn_readlane(ids, page - ids_at);
+        if ((unsigned)id >= (unsigned)a.n_pages) return t;
+        t.k = k + ((long)id * a.k_ps + (long)within * a.k_ts) * 2;
+        t.v = v + ((long)id * a.v_ps + (long)within * a.v_ts) * 2;
         t.n = max(min((t.own ? n_own : n_prefix) - t.key0, KEYS), 0);
         return t;
     }
@@ -168,9 +177,12 @@ template <int D, bool V, int N, int STEP> struct Fetch {
             off[i] = (unsigned)(row - i * ROWS) * (unsigned)ts2 + piece_of(row);
         }
     }
+    // (a buffer load takes the KiB's distance from a scalar register, where a pointer would be added up for each)
     __device__ __forceinline__ void whole(const char* src, unsigned lds, int first) const {
+        const unsigned long long at = (unsigned long long)src;
+        const u32x4 from = {(unsigned)at, (unsigned)(at >> 32) & 0xFFFFu, 0xFFFFFFFFu, 0x00027000u};
 #pragma unroll
-        for (int u = 0; u < N; ++u) load_to_lds<0>(src + (long)(u * STEP * ROWS) * ts2, off[u % KINDS], lds + (u * STEP + first) * 1024);
+        for (int u = 0; u < N; ++u) buffer_to_lds(from, off[u % KINDS], (unsigned)(u * STEP * ROWS) * (unsigned)ts2, lds + (u * STEP + first) * 1024);
     }
     // a tile that ends early: rows past its end as its last one
     __device__ __forceinline__ void some(const char* src, int n, unsigned lds, int first) const {
@@ -379,7 +391,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
     __shared__ __attribute__((aligned(1024))) char lds[HALVES * 2 * STAGE];
     __shared__ float2 ends[WAVES][32];                      // the waves' maxima and sums
     __shared__ long places[4][32];                          // where a wave's rows go (-1: nowhere)
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h2 = lane >> 5, half = wave >> 2, w4 = wave & 3;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h2 = lane >> 5, half = HALVES == 1 ? 0 : wave >> 2, w4 = HALVES == 1 ? wave : wave & 3;
 
     // Which item: kv head fastest, then the parts of the keys, so that the row tiles of a part of a head's keys go to one XCD (workgroups go to them round robin) wherever their
     // number is a multiple of eight, and share an L2; last row tiles, which see the most keys, first.
@@ -459,7 +471,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
         constexpr int N = D / 32;                               // KiB of K (and of V) per wave and tile
         const Fetch<D, false, N, 4> fetch_k(a.k_ts, w4);
         const Fetch<D, true, N, 4> fetch_v(a.v_ts, w4);
-        Keys<64> keys{prefix_table, own_table, kb, vb, n_prefix, tile_limit, 0, -1};
+        Keys<64> keys(a, prefix_table, own_table, kb, vb, n_prefix, tile_limit, t0 + half, HALVES);
         const unsigned to = base + half * 2 * STAGE, kp = k_piece<D>(), vp = v_piece<D>();
         auto fetch = [&](const KeyTile& t, int stage) {
             if (t.n == 0) return;
@@ -472,14 +484,14 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
         const bool live = w4 * 32 < tile_rows;
         const int n_whole = min(max(whole - t0, 0), t1 - t0) / HALVES, n_all = (t1 - t0 + HALVES - 1) / HALVES;    // rounds: of tiles that every row sees whole, all
         int i = 0;
-        auto round = [&](auto part) {
+        auto round = [&](auto part, int stage) {
             constexpr bool PART = decltype(part)::value;
             wait_loads<0>();
             __syncthreads();                                    // the round's tiles are there, and all have left those before them: the next on their way into their place
             nxt = keys.tile(a, t0 + half + (i + 1) * HALVES, t1);
-            fetch(nxt, i + 1 & 1);
+            fetch(nxt, 1 - stage);
             if (live && cur.n && (!PART || !cur.own || cur.key0 < last_limit)) {
-                const unsigned at = to + (i & 1) * STAGE;
+                const unsigned at = to + stage * STAGE;
                 f32x16 s[2];
                 x8 p[4];
                 if (!PART) st.met = true;
@@ -488,9 +500,11 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
                 weigh<E, D, 2, PART>(st, vp, at + STAGE / 2, p, seen(cur), at + STAGE / 2);
             }
             cur = nxt;
+            ++i;
         };
-        for (; i < n_whole; ++i) round(std::false_type{});
-        for (; i < n_all; ++i) round(std::true_type{});
+        while (i + 1 < n_whole) { round(std::false_type{}, 0); round(std::false_type{}, 1); }      // (two, so that places in LDS are constants)
+        if (i < n_whole) round(std::false_type{}, 0);
+        while (i < n_all) round(std::true_type{}, i & 1);
         st.sum = sum_halves(st.sum);
         finish(st);
         if constexpr (HALVES == 2) {
@@ -519,7 +533,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
         const Fetch<D, false, N, 1> fetch_k(a.k_ts, 0);
         const Fetch<D, true, N, 1> fetch_v(a.v_ts, 0);
         const unsigned to = base + wave * (STAGE / 2), kp = k_piece<D>(), vp = v_piece<D>();
-        Keys<32> keys{prefix_table, own_table, kb, vb, n_prefix, tile_limit, 0, -1};
+        Keys<32> keys(a, prefix_table, own_table, kb, vb, n_prefix, tile_limit, 2 * t0 + wave, WAVES);
         const int end = 2 * t1;
         int i = 2 * t0 + wave;
         auto next = [&]() {                                     // (tiles without keys are passed over)
@@ -691,10 +705,10 @@ static bool refuse_attention(long q_tokens, long n_seq, long heads, long kv_head
 }
 // How many row tiles there can be, whatever the lengths, and how their keys are shared out: into how many parts, to one or two halves of a workgroup, and whether a prefix is taken once
 // for its group, as parts of its own, or again by every branch before its own keys.  Lengths stand on the device: tables count with their width, packed keys with their mean, sequences
-// as equally long.  The least of a rough account of the time, us: ITEM for a workgroup's first loads and its last stores; a row tile on 64 keys ALONE on a CU, BOTH with another
+// as equally long, the longest half as long again.  The least of a rough account of the time, us: ITEM for a workgroup's first loads and its last stores; a row tile on 64 keys ALONE on a CU, BOTH with another
 // workgroup on it, or, two of them, by two halves; the join's launch, and its bytes per us.
 static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim) {
-    const double ITEM = 4.5, NEXT = 1.5, BOTH = 2.0, ALONE = 1.15, HALVES = 2.15, MERGE = 1.5, JOIN = 4.5, JOIN_BYTES = 3e6;
+    const double ITEM = 4.5, NEXT = 1.5, BOTH = 2.0, ALONE = 1.15, MERGE = 1.5, JOIN = 4.5, JOIN_BYTES = 3e6;
     static const int counts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32};
     const long rows = (long)a.q_tokens * a.each;
     const long own = (rows + (KV_ROWS - 1) * (long)a.n_seq) / KV_ROWS, pre = prefix_keys > 0 ? (rows + (KV_ROWS - 1) * (long)a.n_groups) / KV_ROWS : 0;
@@ -713,8 +727,8 @@ static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim)
                 auto rounds = [&](long n, long of) { return (double)(((n + of - 1) / of + halves - 1) / halves); };
                 const double oc = rounds(apart ? own_cols : cols, op), pc = apart ? rounds(pre_cols, pp) : 0, oi = (double)own_like * op * a.kv_heads, pi = (double)pre_like * pp * a.kv_heads;
                 const bool full = oi + pi > 256;
-                const double u = scale * (halves == 2 ? HALVES : full ? BOTH : ALONE), slots = halves == 1 && full ? 512 : 256, next = NEXT + (halves == 2 ? MERGE : 0);
-                const double all = (oi * (next + oc * u) + pi * (next + pc * u)) / slots, longest = next + u * std::max(oc, pc);
+                const double u = scale * (halves == 2 ? full ? 1.15 * BOTH : 0.9 * BOTH : full ? BOTH : ALONE), slots = halves == 1 && full ? 512 : 256, next = NEXT + (halves == 2 ? MERGE : 0);
+                const double all = (oi * (next + oc * u) + pi * (next + pc * u)) / slots, longest = next + u * std::max(oc, pc) * (a.n_seq > 1 ? 1.5 : 1);
                 const double cost = ITEM + std::max(all, longest) + (op + pp > 1 ? JOIN + (double)rows * a.kv_heads * (op + pp) * head_dim * 8 / JOIN_BYTES : 0);
                 if (best == 0 || cost < best) { best = cost; own_parts = op; pre_parts = pp; a.halves = halves; }
             }

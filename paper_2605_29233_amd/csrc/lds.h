@@ -17,6 +17,11 @@ static __device__ __forceinline__ void load_dwords_to_lds(const char* src, unsig
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
                  ::"s"(dst), "v"(lane4), "s"(src) : "m0", "memory");
 }
+// As load_to_lds, from a buffer (its descriptor, a lane's offset and a common one).
+static __device__ __forceinline__ void buffer_to_lds(u32x4 from, unsigned lane_offset, unsigned offset, unsigned dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 ::"s"(dst), "v"(lane_offset), "s"(from), "s"(offset) : "m0", "memory");
+}
 // load_to_lds if i < n only (a branch inside the assembly: one in the loop body would split the pipeline's block).
 static __device__ __forceinline__ void load_to_lds_below(unsigned i, unsigned n, const char* src, unsigned lane16, unsigned dst) {
     asm volatile("s_cmp_ge_u32 %3, %4\n\ts_cbranch_scc1 1f\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n1:"
