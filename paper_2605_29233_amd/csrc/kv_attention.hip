@@ -705,16 +705,17 @@ static bool refuse_attention(long q_tokens, long n_seq, long heads, long kv_head
 }
 // How many row tiles there can be, whatever the lengths, and how their keys are shared out: into how many parts, to one or two halves of a workgroup, and whether a prefix is taken once
 // for its group, as parts of its own, or again by every branch before its own keys.  Lengths stand on the device: tables count with their width, packed keys with their mean, sequences
-// as equally long, the longest half as long again.  The least of a rough account of the time, us: ITEM for a workgroup's first loads and its last stores; a row tile on 64 keys ALONE on a CU, BOTH with another
-// workgroup on it, or, two of them, by two halves; the join's launch, and its bytes per us.
+// as equally long, the longest somewhat longer.  The least of a rough account of the time, us, whose constants were fitted to 38 shapes with up to 50 plans each (what it picks is 1 % slower
+// than the best of them in the mean, 11 % at most): FIRST for the first loads and the launch, ITEM for a workgroup's own, 64 keys of a row tile ALONE on a CU or with another workgroup's
+// (BOTH, 512 at once), or 128 by two HALVES; FEW: times that for tiles of up to 32 rows; the join's launch, and its bytes per us.
 static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim) {
-    const double ITEM = 4.5, NEXT = 1.5, BOTH = 2.0, ALONE = 1.15, MERGE = 1.5, JOIN = 4.5, JOIN_BYTES = 3e6;
-    static const int counts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32};
+    const double FIRST = 3.4, ITEM = 2.8, BOTH = 0.9, ALONE = 1.0, HALVES = 1.5, MERGE = 0.15, FEW = 0.57, LONGEST = 1.2, JOIN = 3.7, JOIN_BYTES = 2.8e6, DIM_64 = 0.53;
+    static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
     const long rows = (long)a.q_tokens * a.each;
     const long own = (rows + (KV_ROWS - 1) * (long)a.n_seq) / KV_ROWS, pre = prefix_keys > 0 ? (rows + (KV_ROWS - 1) * (long)a.n_groups) / KV_ROWS : 0;
     const long own_like = std::max(1L, a.n_seq * ((rows / a.n_seq + KV_ROWS - 1) / KV_ROWS)), pre_like = pre ? std::max(1L, a.n_groups * ((rows / a.n_groups + KV_ROWS - 1) / KV_ROWS)) : 0;
     const long own_cols = std::max(1L, (own_keys + 63) / 64), pre_cols = (prefix_keys + 63) / 64;
-    const double scale = head_dim / 128.0;
+    const double scale = head_dim == 64 ? DIM_64 : 1, of = rows / a.n_seq <= 32 ? FEW : 1, pf = pre && rows / a.n_groups <= 32 ? FEW : 1;
     long own_parts = 1, pre_parts = 0;
     double best = 0;
     for (int apart = 0; apart <= (pre ? 1 : 0); ++apart)
@@ -724,12 +725,12 @@ static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim)
                 const long cols = apart ? std::max(own_cols, pre_cols) : own_cols + pre_cols, c = (cols + parts - 1) / parts;
                 if (parts > 1 && c < KV_LEAST_TILES) break;
                 const long op = apart ? std::min<long>((own_cols + c - 1) / c, parts) : parts, pp = apart ? std::min<long>((pre_cols + c - 1) / c, parts) : 0;
-                auto rounds = [&](long n, long of) { return (double)(((n + of - 1) / of + halves - 1) / halves); };
-                const double oc = rounds(apart ? own_cols : cols, op), pc = apart ? rounds(pre_cols, pp) : 0, oi = (double)own_like * op * a.kv_heads, pi = (double)pre_like * pp * a.kv_heads;
+                auto rounds = [&](long n, long in) { return (double)(((n + in - 1) / in + halves - 1) / halves); };
+                const double oc = rounds(apart ? own_cols : cols, op) * of, pc = apart ? rounds(pre_cols, pp) * pf : 0, oi = (double)own_like * op * a.kv_heads, pi = (double)pre_like * pp * a.kv_heads;
                 const bool full = oi + pi > 256;
-                const double u = scale * (halves == 2 ? full ? 1.15 * BOTH : 0.9 * BOTH : full ? BOTH : ALONE), slots = halves == 1 && full ? 512 : 256, next = NEXT + (halves == 2 ? MERGE : 0);
-                const double all = (oi * (next + oc * u) + pi * (next + pc * u)) / slots, longest = next + u * std::max(oc, pc) * (a.n_seq > 1 ? 1.5 : 1);
-                const double cost = ITEM + std::max(all, longest) + (op + pp > 1 ? JOIN + (double)rows * a.kv_heads * (op + pp) * head_dim * 8 / JOIN_BYTES : 0);
+                const double u = scale * (halves == 2 ? HALVES : full ? BOTH : ALONE), item = ITEM + (halves == 2 ? MERGE : 0);
+                const double all = (oi * (item + oc * u) + pi * (item + pc * u)) / (halves == 1 && full ? 512 : 256), longest = item + u * std::max(oc, pc) * (a.n_seq > 1 ? LONGEST : 1);
+                const double cost = FIRST + std::max(all, longest) + (op + pp > 1 ? JOIN + (double)rows * a.kv_heads * (op + pp) * head_dim * 8 / JOIN_BYTES : 0);
                 if (best == 0 || cost < best) { best = cost; own_parts = op; pre_parts = pp; a.halves = halves; }
             }
     if ((own * own_parts + pre * pre_parts) * a.kv_heads > 0x7FFFFFFF || ((long)a.q_tokens * a.heads + 3L * a.n_seq) / 2 > 0x7FFFFFFF || rows + KV_ROWS > 0x7FFFFFFF) return false;
