@@ -381,9 +381,9 @@ def _cache(t, what, dtype, shape, index):
 
 
 def _ints(t, what, n, index, dtype=None):
-    """Address of a contiguous vector of n elements (n None: at least one; returns their number too)."""
-    if t.dtype is not (dtype or _I32) or t.dim() != 1 or t.get_device() != index or (t.shape[0] != n if n is not None else t.shape[0] < 1) or not t.is_contiguous():
-        raise BBError(f"{what}: expected contiguous {dtype or _I32} ({'ranges + 1' if n is None else n},) on cuda:{index}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    """Address of a contiguous vector of n elements."""
+    if t.dtype is not (dtype or _I32) or t.shape != (n,) or t.get_device() != index or not t.is_contiguous():
+        raise BBError(f"{what}: expected contiguous {dtype or _I32} ({n},) on cuda:{index}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
@@ -397,10 +397,19 @@ def _table(t, what, rows, index):
     return t.data_ptr(), ld, t.shape[1]
 
 
+def _ranges(t, what):
+    """Elements of a vector of starts, one more than it has ranges."""
+    n = len(t)
+    if n < 1:
+        raise BBError(f"{what}: expected (ranges + 1,) starts, got {tuple(t.shape)}")
+    return n
+
+
 def _three(t, what):
-    if t.dim() != 3:
-        raise BBError(f"{what}: expected [tokens][heads][head_dim], got {tuple(t.shape)}")
-    return t.shape
+    shape = t.shape
+    if len(shape) != 3:
+        raise BBError(f"{what}: expected [tokens][heads][head_dim], got {tuple(shape)}")
+    return shape
 
 
 def rope(q, k, positions, freqs, interleaved=False, magnitude=1.0, q_out=None, k_out=None, stream=None):
@@ -427,7 +436,7 @@ def rope(q, k, positions, freqs, interleaved=False, magnitude=1.0, q_out=None, k
         ks, kos = _heads(k, "k", dtype, kv, dev), _heads(k_out, "k_out", dtype, kv, dev)
     elif k_out is not None:
         raise BBError("k_out without k")
-    half = freqs.shape[0] if freqs.dim() == 1 else -1
+    half = len(freqs)
     rc = _LIB.bb_rope(ROPE_ARGS.pack(*_heads(q, "q", dtype, shape, dev), *_heads(q_out, "q_out", dtype, shape, dev), heads, *ks, *kos, kv_heads,
                                      _ints(positions, "positions", tokens, dev), _ints(freqs, "freqs", half, dev, _F64), 2 * half, interleaved, magnitude, tokens, dim,
                                      _type(dtype, "q")), _raw_stream(dev))
@@ -452,7 +461,7 @@ def rope_append(q, k, v, positions, freqs, k_cache, v_cache, slots, interleaved=
         q_out = q
     pages, kv_heads = k_cache.shape[0] if k_cache.dim() else 0, kv[1]
     cache = (pages, kv_heads, PAGE_TOKENS, dim)
-    half = freqs.shape[0] if freqs.dim() == 1 else -1
+    half = len(freqs)
     rc = _LIB.bb_rope_append(ROPE_APPEND_ARGS.pack(*_heads(q, "q", dtype, shape, dev), *_heads(q_out, "q_out", dtype, shape, dev), heads, *_heads(k, "k", dtype, kv, dev),
                                                    *_heads(v, "v", dtype, kv, dev), kv_heads, _ints(positions, "positions", tokens, dev),
                                                    _ints(freqs, "freqs", half, dev, _F64), 2 * half, interleaved, magnitude, _ints(slots, "slots", tokens, dev),
@@ -501,8 +510,8 @@ def attention(q, k, v, q_starts, k_starts=None, block=0, scale=None, out=None, l
     if kv[2] != dim:
         raise BBError(f"k: expected [tokens][kv heads][{dim}], got {tuple(kv)}")
     out, outs = _attention_outputs(q, shape, out, lse, dev)
-    qs = _ints(q_starts, "q_starts", None, dev)
-    n = q_starts.shape[0]
+    n = _ranges(q_starts, "q_starts")
+    qs = _ints(q_starts, "q_starts", n, dev)
     ks = qs if k_starts is None else _ints(k_starts, "k_starts", n, dev)
     args = ATTENTION_ARGS.pack(*_heads(q, "q", dtype, shape, dev), *_heads(k, "k", dtype, kv, dev), *_heads(v, "v", dtype, kv, dev), qs, ks, n - 1, tokens, kv[0], heads, kv[1], dim,
                                _type(dtype, "q"), block, dim ** -0.5 if scale is None else scale, *outs)
@@ -528,14 +537,16 @@ def shared_attention(q, q_starts, k_cache, v_cache, own_pages, own_lens, prefix_
     if len(cache) != 4 or cache[2] != PAGE_TOKENS or cache[3] != dim:
         raise BBError(f"k_cache: expected [pages][kv heads][{PAGE_TOKENS}][{dim}], got {tuple(cache)}")
     out, outs = _attention_outputs(q, shape, out, lse, dev)
-    qs = _ints(q_starts, "q_starts", None, dev)
-    n = q_starts.shape[0] - 1
+    n = _ranges(q_starts, "q_starts")
+    qs = _ints(q_starts, "q_starts", n, dev)
+    n -= 1
     prefix = (0, 0, 0, 0, 0, 0)
     if group_starts is not None:
         if prefix_pages is None or prefix_lens is None:
             raise BBError("group_starts without prefix_pages and prefix_lens")
-        gs = _ints(group_starts, "group_starts", None, dev)
-        groups = group_starts.shape[0] - 1
+        groups = _ranges(group_starts, "group_starts")
+        gs = _ints(group_starts, "group_starts", groups, dev)
+        groups -= 1
         prefix = (*_table(prefix_pages, "prefix_pages", groups, dev), _ints(prefix_lens, "prefix_lens", groups, dev), gs, groups)
     elif prefix_pages is not None or prefix_lens is not None:
         raise BBError("prefix_pages or prefix_lens without group_starts")

@@ -56,7 +56,6 @@ struct KvArgs {
     float* part_o; float2* part_ml;                                     // [part][token][head]: unscaled output; maximum (times log2(e)) and sum.  Null: a single part
 };
 #define KV_LEAST_TILES 2                // of 64 keys, a part of a row tile's keys
-#define KV_MOST_PARTS 32
 #define KV_ROWS 128                     // rows (tokens x heads of a group) of a workgroup
 
 // Sums over the lanes up to each (in the row's order: within rows of 16, then across them).
@@ -393,6 +392,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
     __shared__ long places[4][32];                          // where a wave's rows go (-1: nowhere)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h2 = lane >> 5, half = HALVES == 1 ? 0 : wave >> 2, w4 = HALVES == 1 ? wave : wave & 3;
 
+    warm_arguments<sizeof(KvArgs)>();
     // Which item: kv head fastest, then the parts of the keys, so that the row tiles of a part of a head's keys go to one XCD (workgroups go to them round robin) wherever their
     // number is a multiple of eight, and share an L2; last row tiles, which see the most keys, first.
     int lin = blockIdx.x;
@@ -460,7 +460,9 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
 
     const unsigned base = lds_offset(lds);
     const char *kb = a.k + ((long)kvh * a.k_hs + first * a.k_ts) * 2, *vb = a.v + ((long)kvh * a.v_hs + first * a.v_ts) * 2;
-    const int n_tiles = (n_prefix + 63) / 64 + (tile_limit + 63) / 64, t0 = split == 1 ? 0 : (int)((long)n_tiles * piece / split), t1 = split == 1 ? n_tiles : (int)((long)n_tiles * (piece + 1) / split);
+    const int n_tiles = (n_prefix + 63) / 64 + (tile_limit + 63) / 64;      // (below 2^25, parts at most 32)
+    auto part_from = [&](int of) { return prefix ? a.by_prefix_split(n_tiles * of) : a.by_own_split(n_tiles * of); };
+    const int t0 = part_from(piece), t1 = part_from(piece + 1);
     const int whole = n_prefix / 64 + (n_prefix % 64 ? 0 : all_limit / 64);     // tiles that every row sees whole, from the first on
     // The queries have to be there before the loop: left to it, their wait would be one for the fetches that are on their way there, too.
     auto have_queries = [&]() {

@@ -36,6 +36,15 @@ static __device__ __forceinline__ void wave_lds_order() {
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
+// A kernel's arguments into the scalar cache, all lines at once: where they are loaded as they are needed, each line not yet touched is a miss of its own in the chain of a workgroup's
+// first instructions.
+template <int BYTES> static __device__ __forceinline__ void warm_arguments() {
+    const __attribute__((address_space(4))) int* line = (const __attribute__((address_space(4))) int*)__builtin_amdgcn_kernarg_segment_ptr();
+    int any = 0;
+#pragma unroll
+    for (int at = 0; at < BYTES; at += 64) any |= line[at / 4];
+    asm volatile("" ::"s"(any));
+}
 static __device__ __forceinline__ unsigned lds_offset(const void* p) {
     return (unsigned)(size_t)(__attribute__((address_space(3))) const void*)p;
 }
