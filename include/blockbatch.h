@@ -384,8 +384,9 @@ int bb_rope_append(const bb_rope_append_args* args_host, void* hip_stream);
  * (starts [sequences + 1], ascending).  Query heads h * heads / kv_heads .. use kv head h.  out = softmax(scale q k^T) v over the keys that a query sees: query i of n
  * stands at key position p = m - n + i of the m keys and sees all of them (block == 0), or those before the end of its block, j < (p / block + 1) * block, none if
  * p < 0 (block == 1: causal).  A query that sees no key gives zeros.  Tokens outside every sequence are left as they were.  lse (may be NULL):
- * [q_tokens][heads] fp32, contiguous, the natural logarithm of the sum of exp(scale q k) (-inf where no key is seen), for joining partial results.
- * type BB_BF16 or BB_F16; head_dim 64 or 128; scale > 0; all pointers of heads 16-byte aligned and their strides multiples of 8 elements, those between tokens of k and v at most 2^23.
+ * [q_tokens][heads] fp32, contiguous, the natural logarithm of the sum of exp(scale q k) (-inf where no key is seen), for joining partial results.  Equal calls give equal bits; a row's may
+ * differ in their last places between calls of other sizes, as its keys are summed in other parts.
+ * type BB_BF16 or BB_F16; head_dim 64 or 128; scale > 0; q_tokens * heads below 2^31; all pointers of heads 16-byte aligned and their strides multiples of 8 elements, those between tokens of k and v at most 2^23.
  * NaN and infinities in keys and values that a query does not see do not reach it.
  * workspace_dev: at least bb_attention_workspace_bytes() of the same sizes (it looks at no pointer, stride, block or scale), 256-byte aligned (may be NULL if that is 0), used by this call
  * alone until its work is done. */
@@ -401,7 +402,7 @@ int bb_attention(const bb_attention_args* args_host, void* workspace_dev, size_t
 /* Attention of branches over a paged cache, the prefix that a group of them shares read once for all.  Branch b has the queries q_starts[b] .. q_starts[b + 1] - 1, own_lens[b]
  * keys of its own in the pages own_pages[b * own_ld + 0 ..] and belongs to group g if group_starts[g] <= b < group_starts[g + 1]; the group's prefix is prefix_lens[g] keys in the
  * pages prefix_pages[g * prefix_ld + 0 ..].  A query sees its whole prefix, and of its branch's m own keys those that bb_attention describes (block counted from the
- * first own key).  own_width, prefix_width: columns of the tables, at most that many pages count.  groups == 0: no prefix (pointers ignored): plain attention over pages.
+ * first own key).  own_width, prefix_width: columns of the tables (at most BB_MAX_TOKENS / BB_PAGE_TOKENS), at most that many pages count.  groups == 0: no prefix (pointers ignored): plain attention over pages.
  * Both lengths may end inside a page; what lies behind them is not read.  Branches outside every group have no prefix; starts and group_starts ascend.  The rest as in bb_attention. */
 typedef struct {
     const void* q; long q_token, q_head; const int32_t* q_starts; long branches, q_tokens;
@@ -413,6 +414,12 @@ typedef struct {
 } bb_shared_attention_args;
 size_t bb_shared_attention_workspace_bytes(const bb_shared_attention_args* args_host);
 int bb_shared_attention(const bb_shared_attention_args* args_host, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* Tests: the two with a plan of the caller's choice: 1 or 2 halves of a workgroup that share its keys, the keys cut into 1 .. 32 parts, a group's prefix into as many (0: taken by every
+ * branch before its own keys).  More than one part in all: at least (parts * q_tokens * heads * (head_dim * 4 + 8) + 512) bytes of workspace (BB_ENOMEM). */
+int bb_debug_attention(const bb_attention_args* args_host, int halves, int parts, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+int bb_debug_shared_attention(const bb_shared_attention_args* args_host, int halves, int own_parts, int prefix_parts, void* workspace_dev, size_t workspace_bytes,
+                              void* hip_stream);
 
 /* Tests: on != 0 makes every later forward also store the fp32 logits of the rows that receive them (view's
  * logits_dev); off (the default) the logits exist only in the registers of the LM-head GEMM. */

@@ -10,7 +10,7 @@
 //   S^T[key][row]  = K[key][:] . Q[row][:]       A = K from LDS, B = Q in registers
 //   O^T[d][row]   += V^T[d][key] . P^T[key][row] A = V^T by transposing LDS reads, B = P out of S^T's own registers: a lane holds keys
 //                                                4 h + {0..3} and 8 + 4 h + {0..3} of every 16 (h = lane / 32), and V^T is read in that order
-// P is rounded to the operands' type (bf16: 2^-9 of each weight at most, of random sign), as the matrix cores take it; the sum of weights is not.
+// P is rounded to the operands' type (off by 2^-8 of a weight at most in bf16, 2^-11 in fp16, of random sign), as the matrix cores take it; the sum of weights is not.
 #include "heads.h"
 #include "lds.h"
 #include "sched.h"
@@ -56,6 +56,8 @@ struct KvArgs {
     float* part_o; float2* part_ml;                                     // [part][token][head]: unscaled output; maximum (times log2(e)) and sum.  Null: a single part
 };
 #define KV_LEAST_TILES 2                // of 64 keys, a part of a row tile's keys
+#define KV_MOST_PARTS 32
+#define KV_MOST_COLUMNS (BB_MAX_TOKENS / BB_PAGE_TOKENS)
 #define KV_ROWS 128                     // rows (tokens x heads of a group) of a workgroup
 
 // Sums over the lanes up to each (in the row's order: within rows of 16, then across them).
@@ -112,7 +114,7 @@ static __device__ __forceinline__ int find_group(const KvArgs& a, int seq) {
     }
     return -1;
 }
-static __device__ __forceinline__ int paged_keys(int n, int width) { return min(max(n, 0), (int)min((long)width * BB_PAGE_TOKENS, 0x3FFFFFC0L)); }
+static __device__ __forceinline__ int paged_keys(int n, int width) { return min(max(n, 0), width * BB_PAGE_TOKENS); }
 
 // Keys in tiles of KEYS tokens: packed, or pages, those of a prefix before those of its own (a tile never holds both).  The ids of 64 pages at a time stand in a register's
 // lanes: a load per tile would have to be waited for, and with it every fetch on its way.  A tile past the end, or of a page that is not in the cache, has no keys (n = 0).
@@ -703,14 +705,16 @@ template <bool PAGED> static void launch_kv(const KvArgs& a, int type, int head_
 
 static bool refuse_attention(long q_tokens, long n_seq, long heads, long kv_heads, long head_dim, long type, long block, double scale) {
     return (type != BB_BF16 && type != BB_F16) || (head_dim != 64 && head_dim != 128) || q_tokens < 0 || q_tokens > BB_MAX_TOKENS || n_seq < 0 || n_seq > BB_MAX_TOKENS || heads < 1 ||
-           heads > BB_MAX_HEADS || kv_heads < 1 || heads % kv_heads || block < 0 || block > 0x7FFFFFFF || !((float)scale > 0) || !((float)scale * 1.45f < INFINITY);
+           heads > BB_MAX_HEADS || kv_heads < 1 || heads % kv_heads || q_tokens * heads > 0x7FFFFFFF || block < 0 || block > 0x7FFFFFFF || !((float)scale > 0) || !((float)scale * 1.45f < INFINITY);
 }
+// A plan: halves of a workgroup, parts of a branch's keys, of a group's prefix (0: taken by the branches before their own).
+struct KvPlan { int halves, own_parts, prefix_parts; };
 // How many row tiles there can be, whatever the lengths, and how their keys are shared out: into how many parts, to one or two halves of a workgroup, and whether a prefix is taken once
 // for its group, as parts of its own, or again by every branch before its own keys.  Lengths stand on the device: tables count with their width, packed keys with their mean, sequences
 // as equally long, the longest somewhat longer.  The least of a rough account of the time, us, whose constants were fitted to 38 shapes with up to 50 plans each (what it picks is 1 % slower
 // than the best of them in the mean, 11 % at most): FIRST for the first loads and the launch, ITEM for a workgroup's own, 64 keys of a row tile ALONE on a CU or with another workgroup's
 // (BOTH, 512 at once), or 128 by two HALVES; FEW: times that for tiles of up to 32 rows; the join's launch, and its bytes per us.
-static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim) {
+static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim, const KvPlan* given) {
     const double FIRST = 3.4, ITEM = 2.8, BOTH = 0.9, ALONE = 1.0, HALVES = 1.5, MERGE = 0.15, FEW = 0.57, LONGEST = 1.2, JOIN = 3.7, JOIN_BYTES = 2.8e6, DIM_64 = 0.53;
     static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
     const long rows = (long)a.q_tokens * a.each;
@@ -735,7 +739,11 @@ static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim)
                 const double cost = FIRST + std::max(all, longest) + (op + pp > 1 ? JOIN + (double)rows * a.kv_heads * (op + pp) * head_dim * 8 / JOIN_BYTES : 0);
                 if (best == 0 || cost < best) { best = cost; own_parts = op; pre_parts = pp; a.halves = halves; }
             }
-    if ((own * own_parts + pre * pre_parts) * a.kv_heads > 0x7FFFFFFF || ((long)a.q_tokens * a.heads + 3L * a.n_seq) / 2 > 0x7FFFFFFF || rows + KV_ROWS > 0x7FFFFFFF) return false;
+    if (given) {
+        if (given->halves < 1 || given->halves > 2 || given->own_parts < 1 || given->own_parts > KV_MOST_PARTS || given->prefix_parts < 0 || given->prefix_parts > KV_MOST_PARTS) return false;
+        a.halves = given->halves; own_parts = given->own_parts; pre_parts = pre ? given->prefix_parts : 0;
+    }
+    if ((own * own_parts + pre * pre_parts) * a.kv_heads > 0x7FFFFFFF || (long)a.q_tokens * a.heads + 3L * a.n_seq > 0x7FFFFFFF || rows + KV_ROWS > 0x7FFFFFFF) return false;
     a.own_tiles = (int)own; a.own_split = (int)own_parts; a.prefix_tiles = pre_parts ? (int)pre : 0; a.prefix_split = (int)pre_parts;
     a.by_kv_heads = Divide::by(a.kv_heads); a.by_each = Divide::by(a.each); a.by_block = Divide::by(std::max(a.block, 1)); a.by_own_split = Divide::by(a.own_split);
     a.by_prefix_split = Divide::by(std::max(a.prefix_split, 1));
@@ -763,26 +771,27 @@ static bool refuse_ints(const void* p) { return !p || (uintptr_t)p % 4; }
 static bool refuse_sizes(const bb_attention_args* x) {
     return !x || refuse_attention(x->q_tokens, x->sequences, x->heads, x->kv_heads, x->head_dim, x->type, x->block, x->scale) || x->k_tokens < 0 || x->k_tokens > BB_MAX_TOKENS;
 }
-static bool plan(KvArgs& a, const bb_attention_args* x) {
+static bool plan(KvArgs& a, const bb_attention_args* x, const KvPlan* given = nullptr) {
     a.n_seq = (int)x->sequences; a.q_tokens = (int)x->q_tokens; a.k_tokens = (int)x->k_tokens; a.heads = (int)x->heads; a.kv_heads = (int)x->kv_heads; a.each = a.heads / a.kv_heads;
     a.block = (int)x->block; a.scale = (float)x->scale * 1.44269504089f;
-    return plan_parts(a, x->k_tokens / x->sequences, 0, (int)x->head_dim);
+    return plan_parts(a, x->k_tokens / x->sequences, 0, (int)x->head_dim, given);
 }
 extern "C" size_t bb_attention_workspace_bytes(const bb_attention_args* x) {
     KvArgs a{};
     return refuse_sizes(x) || x->q_tokens == 0 || x->sequences == 0 || !plan(a, x) ? 0 : parts_bytes(a, (int)x->head_dim);
 }
-extern "C" int bb_attention(const bb_attention_args* x, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+static int attention(const bb_attention_args* x, const KvPlan* given, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
     if (refuse_sizes(x)) return BB_EINVAL;
     if (x->q_tokens == 0 || x->sequences == 0) return BB_OK;
     if (refuse_ints(x->q_starts) || refuse_ints(x->k_starts) || (uintptr_t)x->lse % 4) return BB_EINVAL;
     const int heads = (int)x->heads, kv_heads = (int)x->kv_heads, dim = (int)x->head_dim;
     const HeadView q = heads_view(x->q, x->q_tokens, x->q_token, heads, x->q_head, dim, 2), o = heads_view(x->out, x->q_tokens, x->o_token, heads, x->o_head, dim, 2);
     const HeadView k = heads_view(x->k, x->k_tokens, x->k_token, kv_heads, x->k_head, dim, 2), v = heads_view(x->v, x->k_tokens, x->v_token, kv_heads, x->v_head, dim, 2);
-    if (refuse_view(q) || refuse_pieces(q) || refuse_out_view(o) || refuse_pieces(o) || overlap(o, q)) return BB_EINVAL;
-    if (x->k_tokens > 0 && (refuse_view(k) || refuse_pieces(k) || refuse_view(v) || refuse_pieces(v) || far_rows(k.s[0]) || far_rows(v.s[0]) || overlap(o, k) || overlap(o, v))) return BB_EINVAL;
+    const HeadView l = heads_view(x->lse, x->q_tokens, heads, heads, 1, 1, 4);
+    if (refuse_view(q) || refuse_pieces(q) || refuse_out_view(o) || refuse_pieces(o) || overlap(o, q) || (x->lse && (overlap(l, o) || overlap(l, q)))) return BB_EINVAL;
+    if (x->k_tokens > 0 && (refuse_view(k) || refuse_pieces(k) || refuse_view(v) || refuse_pieces(v) || far_rows(k.s[0]) || far_rows(v.s[0]) || overlap(o, k) || overlap(o, v) || (x->lse && (overlap(l, k) || overlap(l, v))))) return BB_EINVAL;
     KvArgs a{};
-    if (!plan(a, x)) return BB_EINVAL;
+    if (!plan(a, x, given)) return BB_EINVAL;
     // (strides as the views have them: none over a single token or head)
     a.q = (const char*)x->q; a.q_ts = q.s[0]; a.q_hs = q.s[1]; a.k = (const char*)x->k; a.k_ts = k.s[0]; a.k_hs = k.s[1]; a.v = (const char*)x->v; a.v_ts = v.s[0]; a.v_hs = v.s[1];
     a.out = (char*)x->out; a.o_ts = o.s[0]; a.o_hs = o.s[1]; a.lse = x->lse; a.q_starts = x->q_starts; a.k_starts = x->k_starts;
@@ -791,19 +800,19 @@ extern "C" int bb_attention(const bb_attention_args* x, void* workspace_dev, siz
 
 static bool refuse_sizes(const bb_shared_attention_args* x) {
     return !x || refuse_attention(x->q_tokens, x->branches, x->heads, x->kv_heads, x->head_dim, x->type, x->block, x->scale) || x->groups < 0 || x->groups > BB_MAX_TOKENS ||
-           x->own_width < 0 || x->own_width > BB_MAX_PAGES || (x->groups > 0 && (x->prefix_width < 0 || x->prefix_width > BB_MAX_PAGES));
+           x->own_width < 0 || x->own_width > KV_MOST_COLUMNS || (x->groups > 0 && (x->prefix_width < 0 || x->prefix_width > KV_MOST_COLUMNS));
 }
-static bool plan(KvArgs& a, const bb_shared_attention_args* x) {
+static bool plan(KvArgs& a, const bb_shared_attention_args* x, const KvPlan* given = nullptr) {
     a.n_seq = (int)x->branches; a.q_tokens = (int)x->q_tokens; a.heads = (int)x->heads; a.kv_heads = (int)x->kv_heads; a.each = a.heads / a.kv_heads;
     a.block = (int)x->block; a.scale = (float)x->scale * 1.44269504089f;
     a.own_width = (int)x->own_width; a.n_groups = (int)x->groups; a.prefix_width = x->groups ? (int)x->prefix_width : 0;
-    return plan_parts(a, 64L * a.own_width, 64L * a.prefix_width, (int)x->head_dim);
+    return plan_parts(a, 64L * a.own_width, 64L * a.prefix_width, (int)x->head_dim, given);
 }
 extern "C" size_t bb_shared_attention_workspace_bytes(const bb_shared_attention_args* x) {
     KvArgs a{};
     return refuse_sizes(x) || x->q_tokens == 0 || x->branches == 0 || !plan(a, x) ? 0 : parts_bytes(a, (int)x->head_dim);
 }
-extern "C" int bb_shared_attention(const bb_shared_attention_args* x, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+static int shared_attention(const bb_shared_attention_args* x, const KvPlan* given, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
     if (refuse_sizes(x) || x->pages < 1 || x->pages > BB_MAX_PAGES || (x->branches > 1 && x->own_ld < 0) || (x->groups > 1 && x->prefix_ld < 0) ||
         x->own_ld > HEADS_MAX_STRIDE || (x->groups > 0 && x->prefix_ld > HEADS_MAX_STRIDE)) return BB_EINVAL;
     if (x->q_tokens == 0 || x->branches == 0) return BB_OK;
@@ -811,14 +820,33 @@ extern "C" int bb_shared_attention(const bb_shared_attention_args* x, void* work
     if (x->groups > 0 && (refuse_ints(x->prefix_lens) || refuse_ints(x->group_starts) || (x->prefix_width > 0 && refuse_ints(x->prefix_pages)))) return BB_EINVAL;
     const int heads = (int)x->heads, kv_heads = (int)x->kv_heads, dim = (int)x->head_dim;
     const HeadView q = heads_view(x->q, x->q_tokens, x->q_token, heads, x->q_head, dim, 2), o = heads_view(x->out, x->q_tokens, x->o_token, heads, x->o_head, dim, 2);
+    const HeadView l = heads_view(x->lse, x->q_tokens, heads, heads, 1, 1, 4);
     const HeadView k = pages_view(x->k_cache, x->pages, x->kc_page, kv_heads, x->kc_head, x->kc_token, dim, 2), v = pages_view(x->v_cache, x->pages, x->vc_page, kv_heads, x->vc_head, x->vc_token, dim, 2);
     if (refuse_view(q) || refuse_pieces(q) || refuse_out_view(o) || refuse_pieces(o) || refuse_view(k) || refuse_pieces(k) || refuse_view(v) || refuse_pieces(v) ||
-        far_rows(x->kc_token) || far_rows(x->vc_token) || overlap(o, q) || overlap(o, k) || overlap(o, v)) return BB_EINVAL;
+        far_rows(x->kc_token) || far_rows(x->vc_token) || overlap(o, q) || overlap(o, k) || overlap(o, v) ||
+        (x->lse && (overlap(l, o) || overlap(l, q) || overlap(l, k) || overlap(l, v)))) return BB_EINVAL;
     KvArgs a{};
-    if (!plan(a, x)) return BB_EINVAL;
+    if (!plan(a, x, given)) return BB_EINVAL;
     a.q = (const char*)x->q; a.q_ts = q.s[0]; a.q_hs = q.s[1]; a.k = (const char*)x->k_cache; a.k_ps = k.s[0]; a.k_hs = k.s[1]; a.k_ts = k.s[2];
     a.v = (const char*)x->v_cache; a.v_ps = v.s[0]; a.v_hs = v.s[1]; a.v_ts = v.s[2]; a.out = (char*)x->out; a.o_ts = o.s[0]; a.o_hs = o.s[1]; a.lse = x->lse;
     a.q_starts = x->q_starts; a.own_pages = x->own_pages; a.own_ld = x->branches > 1 ? x->own_ld : 0; a.own_lens = x->own_lens;
     a.prefix_pages = x->prefix_pages; a.prefix_ld = x->groups > 1 ? x->prefix_ld : 0; a.prefix_lens = x->prefix_lens; a.group_starts = x->group_starts; a.n_pages = (int)x->pages;
     return run_kv<true>(a, (int)x->type, dim, workspace_dev, workspace_bytes, hip_stream);
+}
+
+extern "C" int bb_attention(const bb_attention_args* x, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    return attention(x, nullptr, workspace_dev, workspace_bytes, hip_stream);
+}
+extern "C" int bb_shared_attention(const bb_shared_attention_args* x, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    return shared_attention(x, nullptr, workspace_dev, workspace_bytes, hip_stream);
+}
+
+// ---- tests ------------------------------------------------------------------------------------------------------------------------------------
+extern "C" int bb_debug_attention(const bb_attention_args* x, int halves, int parts, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    const KvPlan given{halves, parts, 0};
+    return attention(x, &given, workspace_dev, workspace_bytes, hip_stream);
+}
+extern "C" int bb_debug_shared_attention(const bb_shared_attention_args* x, int halves, int own_parts, int prefix_parts, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    const KvPlan given{halves, own_parts, prefix_parts};
+    return shared_attention(x, &given, workspace_dev, workspace_bytes, hip_stream);
 }

@@ -425,6 +425,97 @@ def test_argument_structs_are_packed_as_the_header_has_them():
         assert packed.size == 8 * len(kinds)
 
 
+def heads_of(t):
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def run_plan(q, k, v, ql, kl, block, halves, parts):
+    """bb_attention with a plan of the test's choice."""
+    d = [t.to(DEV) for t in (q, k, v)]
+    qs, ks = starts(ql).to(DEV), starts(kl).to(DEV)
+    out, lse = torch.full(q.shape, 9.0, dtype=q.dtype, device=DEV), torch.full(q.shape[:2], 9.0, device=DEV)
+    tokens, heads, dim = q.shape
+    args = binding.ATTENTION_ARGS.pack(*(x for t in d for x in heads_of(t)), qs.data_ptr(), ks.data_ptr(), len(ql), tokens, k.shape[0], heads, k.shape[1], dim,
+                                       {torch.bfloat16: 1, torch.float16: 2}[q.dtype], block, dim ** -0.5, *heads_of(out), lse.data_ptr())
+    ws = torch.full((parts * tokens * heads * (dim * 4 + 8) + 512,), 255, dtype=torch.uint8, device=DEV)       # (NaN wherever nothing is written)
+    assert bb.load_library().bb_debug_attention(args, halves, parts, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    return out, lse
+
+
+def run_shared_plan(q, rows, k, v, op, own, pp, prefixes, groups, block, halves, own_parts, prefix_parts):
+    d = [t.to(DEV) for t in (q, k, v, op, pp, ints(own), ints(prefixes), ints(groups), starts(rows))]
+    dq, dk, dv, do, dp, ol, pl, gs, qs = d
+    out, lse = torch.full(q.shape, 9.0, dtype=q.dtype, device=DEV), torch.full(q.shape[:2], 9.0, device=DEV)
+    tokens, heads, dim = q.shape
+
+    def cache(t):
+        return t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)
+
+    args = binding.SHARED_ATTENTION_ARGS.pack(*heads_of(dq), qs.data_ptr(), len(rows), tokens, *cache(dk), *cache(dv), k.shape[0], do.data_ptr(), do.stride(0), do.shape[1], ol.data_ptr(),
+                                              dp.data_ptr(), dp.stride(0), dp.shape[1], pl.data_ptr(), gs.data_ptr(), len(prefixes), heads, k.shape[1], dim,
+                                              {torch.bfloat16: 1, torch.float16: 2}[q.dtype], block, dim ** -0.5, *heads_of(out), lse.data_ptr())
+    ws = torch.full(((own_parts + prefix_parts) * tokens * heads * (dim * 4 + 8) + 512,), 255, dtype=torch.uint8, device=DEV)
+    rc = bb.load_library().bb_debug_shared_attention(args, halves, own_parts, prefix_parts, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    torch.cuda.synchronize()
+    return out, lse
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(6, 2, 128), (7, 1, 64)])
+@pytest.mark.parametrize("block", [0, 1, 32])
+@pytest.mark.parametrize("ql,kl", [([130, 0, 33, 1, 5], [130, 7, 300, 70, 2]), ([9, 60], [700, 33]), ([300], [641])])
+def test_every_plan_of_packed_sequences(ql, kl, block, heads, kv_heads, dim, dtype):
+    """One and two halves, the keys in one part up to more than there are tiles: each against the definition."""
+    q, k, v = inputs(dim + block, ql, kl, heads, kv_heads, dim, dtype, 2.0)
+    want = attention(q, k, v, ql, kl, block, dim ** -0.5)
+    for halves in (1, 2):
+        for parts in (1, 2, 3, 7, 32):
+            check(*run_plan(q, k, v, ql, kl, block, halves, parts), want, q.dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(6, 2, 128), (7, 1, 64)])
+@pytest.mark.parametrize("block", [0, 1])
+@pytest.mark.parametrize("rows,own,prefixes,groups", BRANCHES + [([1, 2], [4500, 70], [5000], [0, 2]), ([50, 40], [100, 64], [4480, 130], [0, 1, 2])])
+def test_every_plan_of_shared_prefixes(rows, own, prefixes, groups, block, heads, kv_heads, dim, dtype):
+    """Prefixes taken by every branch, or by the group in one part and in many; own keys in one and many; a page that is not there among them."""
+    q, k, v, op, pp = branches(dim + len(rows), rows, own, prefixes, heads, kv_heads, dim, dtype)
+    pp = pp.clone()
+    if prefixes[0] > 128:
+        pp[0, 1] = k.shape[0]
+    want = shared(q, rows, k, v, op, own, pp, prefixes, groups, block, dim ** -0.5)
+    for halves in (1, 2):
+        for own_parts, prefix_parts in ((1, 0), (3, 0), (32, 0), (1, 1), (2, 3), (1, 32)):
+            check(*run_shared_plan(q, rows, k, v, op, own, pp, prefixes, groups, block, halves, own_parts, prefix_parts), want, q.dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,at", [(140, 75), (9, 4), (300, 250)])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_unseen_values_under_every_plan(bad, dim, n, at):
+    """Garbage behind token `at` of a causal prompt, and one value that later rows do see, in tiles of few and of many rows."""
+    q, k, v = inputs(7, [n], [n], 2, 1, dim, "bf16")
+    k2, v2 = k.clone(), v.clone()
+    k2[at:], v2[at:] = bad, bad
+    v3 = v.clone()
+    v3[at, 0, 3] = bad
+    hit = torch.zeros(n, 2, dim, dtype=torch.bool)
+    hit[at:, :, 3] = True
+    for halves in (1, 2):
+        for parts in (1, 3):
+            out, _ = run_plan(q, k, v, [n], [n], 1, halves, parts)
+            got, _ = run_plan(q, k2, v2, [n], [n], 1, halves, parts)
+            assert torch.equal(got[:at], out[:at])
+            got, _ = run_plan(q, k, v3, [n], [n], 1, halves, parts)
+            assert torch.equal(got.cpu()[~hit], out.cpu()[~hit])
+            assert torch.isnan(got.cpu()[hit]).all() if bad != bad else (got.cpu()[hit] == bad).all()
+
+
 def test_c_entries_refuse_before_touching_a_device():
     """Every call below is refused on the host (the pointers are never followed)."""
     lib = bb.load_library()
@@ -439,8 +530,12 @@ def test_c_entries_refuse_before_touching_a_device():
     for bad in (dict(q=0), dict(q=p + 2), dict(qt=250), dict(qh=4), dict(k=0), dict(k=2 * p + 8), dict(kt=1 << 24), dict(v=0), dict(vh=65), dict(qs=0), dict(ks=0),
                 dict(qs=4 * p + 1), dict(n=-1), dict(qn=-1), dict(kn=-1), dict(qn=1 << 31), dict(n=1 << 33), dict(heads=3), dict(heads=0), dict(kv=0), dict(heads=4096, kv=2), dict(dim=96),
                 dict(dim=0), dict(type=0), dict(type=7), dict(block=-1), dict(block=1 << 31), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
-                dict(scale=1e39), dict(scale=1e-60), dict(o=0), dict(ot=128), dict(oh=0), dict(o=p), dict(o=2 * p), dict(o=3 * p + 128), dict(lse=6), dict(qt=-8), dict(qt=1 << 50)):
+                dict(scale=1e39), dict(scale=1e-60), dict(lse=p + 4), dict(lse=2 * p), dict(heads=1024, kv=1024, qn=1 << 24), dict(o=0), dict(ot=128), dict(oh=0), dict(o=p), dict(o=2 * p), dict(o=3 * p + 128), dict(lse=6), dict(qt=-8), dict(qt=1 << 50)):
         assert call(**bad) == -1, bad
+    args = binding.ATTENTION_ARGS.pack(*good.values())
+    for halves, parts in ((0, 1), (3, 1), (1, 0), (1, 33), (1, -1)):
+        assert lib.bb_debug_attention(args, halves, parts, None, 0, None) == -1
+    assert lib.bb_debug_attention(args, 1, 2, None, 0, None) == -3
     # work that wants its keys in parts wants a workspace for them
     large = dict(good, qn=16, kn=100000, n=1, k=1 << 32, v=1 << 33)
     args = binding.ATTENTION_ARGS.pack(*large.values())
