@@ -317,27 +317,25 @@ template <class E, int D> static __device__ __forceinline__ typename Half<E>::x8
     __builtin_memcpy(&v, f, 16);
     return v;
 }
-// Whether a tile of V holds an infinity or a NaN.
-template <class E, int D, int NK> static __device__ __forceinline__ bool any_infinite(unsigned at) {
+// Whether N KiB of LDS, every STEP-th, hold an infinity or a NaN.
+template <class E, int N, int STEP> static __device__ __forceinline__ bool any_infinite(unsigned at) {
     unsigned bad = 0;
 #pragma unroll
-    for (int i = 0; i < NK * D / 16; ++i) {
-        const u32x4 x = lds_at<u32x4>(at + i * 1024 + (threadIdx.x & 63) * 16);
+    for (int i = 0; i < N; ++i) {
+        const u32x4 x = lds_at<u32x4>(at + i * STEP * 1024 + (threadIdx.x & 63) * 16);
 #pragma unroll
         for (int j = 0; j < 4; ++j) bad |= (x[j] & Half<E>::exponent) + Half<E>::one;
         if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);          // (no more registers than that)
     }
     return __ballot((bad & 0x80008000u) != 0) != 0;
 }
-// O^T += V^T P^T.  Weight 0 does not hide an infinity or a NaN that a row must not see from the product: in a tile that not every row sees whole (PART) and that holds any,
+// O^T += V^T P^T.  Weight 0 does not hide an infinity or a NaN that a row must not see from the product: in a tile that not every row sees whole (PART) and that holds any (bad),
 // the product is made without them, and the rows that see them get them added, key by key (tile: the LDS offset of the tile as a whole).
 template <class E, int D, int NK, bool PART>
-static __device__ __forceinline__ void weigh(RowState<D>& r, unsigned vp, unsigned at, const typename Half<E>::x8 (&p)[2 * NK], int seen, unsigned tile) {
+static __device__ __forceinline__ void weigh(RowState<D>& r, unsigned vp, unsigned at, const typename Half<E>::x8 (&p)[2 * NK], int seen, unsigned tile, bool bad) {
     typedef typename Half<E>::x8 x8;
     constexpr int OT = D / 32, STEPS = 2 * NK * OT;
     asm volatile("" : "+v"(vp));
-    bool bad = false;
-    if constexpr (PART) bad = any_infinite<E, D, NK>(tile);
     x8 ring[AHEAD];
 #pragma unroll
     for (int n = 0; n < AHEAD; ++n) ring[n] = values<E, D>(vp, at, n / OT, n % OT);
@@ -391,6 +389,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
     constexpr int STAGE = 2 * 64 * D * 2, ST = D / 16, OT = D / 32, WAVES = 4 * HALVES;
     __shared__ __attribute__((aligned(1024))) char lds[HALVES * 2 * STAGE];
     __shared__ float2 ends[WAVES][32];                      // the waves' maxima and sums
+    __shared__ __attribute__((aligned(16))) int bad_values[2][WAVES];      // of a stage's V, whether the share that a wave fetched holds an infinity or a NaN
     __shared__ long places[4][32];                          // where a wave's rows go (-1: nowhere)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h2 = lane >> 5, half = HALVES == 1 ? 0 : wave >> 2, w4 = HALVES == 1 ? wave : wave & 3;
 
@@ -491,6 +490,10 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
         auto round = [&](auto part, int stage) {
             constexpr bool PART = decltype(part)::value;
             wait_loads<0>();
+            if (PART && cur.n) {
+                const bool bad = any_infinite<E, N, 4>(to + stage * STAGE + STAGE / 2 + w4 * 1024);
+                if (lane == 0) bad_values[stage][wave] = bad;
+            }
             __syncthreads();                                    // the round's tiles are there, and all have left those before them: the next on their way into their place
             nxt = keys.tile(a, t0 + half + (i + 1) * HALVES, t1);
             fetch(nxt, 1 - stage);
@@ -498,10 +501,14 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
                 const unsigned at = to + stage * STAGE;
                 f32x16 s[2];
                 x8 p[4];
-                if (!PART) st.met = true;
+                int bad = 0;
+                if constexpr (PART) {
+                    const u32x4 b = *reinterpret_cast<const u32x4*>(&bad_values[stage][half * 4]);
+                    bad = __builtin_amdgcn_readfirstlane(b[0] | b[1] | b[2] | b[3]);
+                } else st.met = true;
                 scores<E, D, 2>(kp, at, qf, s);
                 weights<E, D, 2, PART>(st, s, a.scale, seen(cur), p);
-                weigh<E, D, 2, PART>(st, vp, at + STAGE / 2, p, seen(cur), at + STAGE / 2);
+                weigh<E, D, 2, PART>(st, vp, at + STAGE / 2, p, seen(cur), at + STAGE / 2, bad);
             }
             cur = nxt;
             ++i;
@@ -563,7 +570,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
             if (nxt.n) fetch_k(nxt.k, nxt.n, 32, to, 0);
             weights<E, D, 1, PART>(st, s, a.scale, seen(cur), p);
             if (nxt.n) wait_loads<N>(); else wait_loads<0>();
-            weigh<E, D, 1, PART>(st, vp, to + STAGE / 4, p, seen(cur), to + STAGE / 4);
+            weigh<E, D, 1, PART>(st, vp, to + STAGE / 4, p, seen(cur), to + STAGE / 4, PART && any_infinite<E, N, 1>(to + STAGE / 4));
             wait_lds();
             if (nxt.n) fetch_v(nxt.v, nxt.n, 32, to + STAGE / 4, 0);
             cur = nxt;
