@@ -401,10 +401,20 @@ def _table(t, what, rows, index):
 
 def _ranges(t, what):
     """Elements of a vector of starts, one more than it has ranges."""
-    n = len(t)
-    if n < 1:
-        raise BBError(f"{what}: expected (ranges + 1,) starts, got {tuple(t.shape)}")
-    return n
+    shape = t.shape
+    if len(shape) != 1 or shape[0] < 1:
+        raise BBError(f"{what}: expected (ranges + 1,) starts, got {tuple(shape)}")
+    return shape[0]
+
+
+_TURN = "interleaved and magnitude: expected a flag and a number, got {!r} and {!r}"
+
+
+def _half(freqs):
+    shape = freqs.shape
+    if len(shape) != 1:
+        raise BBError(f"freqs: expected (rot / 2,), got {tuple(shape)}")
+    return shape[0]
 
 
 def _three(t, what):
@@ -438,10 +448,14 @@ def rope(q, k, positions, freqs, interleaved=False, magnitude=1.0, q_out=None, k
         ks, kos = _heads(k, "k", dtype, kv, dev), _heads(k_out, "k_out", dtype, kv, dev)
     elif k_out is not None:
         raise BBError("k_out without k")
-    half = len(freqs)
-    rc = _LIB.bb_rope(ROPE_ARGS.pack(*_heads(q, "q", dtype, shape, dev), *_heads(q_out, "q_out", dtype, shape, dev), heads, *ks, *kos, kv_heads,
-                                     _ints(positions, "positions", tokens, dev), _ints(freqs, "freqs", half, dev, _F64), 2 * half, interleaved, magnitude, tokens, dim,
-                                     _type(dtype, "q")), _raw_stream(dev))
+    half = _half(freqs)
+    rows = (*_heads(q, "q", dtype, shape, dev), *_heads(q_out, "q_out", dtype, shape, dev), heads, *ks, *kos, kv_heads, _ints(positions, "positions", tokens, dev),
+            _ints(freqs, "freqs", half, dev, _F64), 2 * half)
+    try:
+        args = ROPE_ARGS.pack(*rows, interleaved, magnitude, tokens, dim, _type(dtype, "q"))
+    except struct.error:
+        raise BBError(_TURN.format(interleaved, magnitude)) from None
+    rc = _LIB.bb_rope(args, _raw_stream(dev))
     if rc:
         _done(rc, "bb_rope")
     return q_out, k_out
@@ -463,12 +477,15 @@ def rope_append(q, k, v, positions, freqs, k_cache, v_cache, slots, interleaved=
         q_out = q
     pages, kv_heads = k_cache.shape[0] if k_cache.dim() else 0, kv[1]
     cache = (pages, kv_heads, PAGE_TOKENS, dim)
-    half = len(freqs)
-    rc = _LIB.bb_rope_append(ROPE_APPEND_ARGS.pack(*_heads(q, "q", dtype, shape, dev), *_heads(q_out, "q_out", dtype, shape, dev), heads, *_heads(k, "k", dtype, kv, dev),
-                                                   *_heads(v, "v", dtype, kv, dev), kv_heads, _ints(positions, "positions", tokens, dev),
-                                                   _ints(freqs, "freqs", half, dev, _F64), 2 * half, interleaved, magnitude, _ints(slots, "slots", tokens, dev),
-                                                   *_cache(k_cache, "k_cache", dtype, cache, dev), *_cache(v_cache, "v_cache", dtype, cache, dev), pages, tokens, dim,
-                                                   _type(dtype, "q")), _raw_stream(dev))
+    half = _half(freqs)
+    rows = (*_heads(q, "q", dtype, shape, dev), *_heads(q_out, "q_out", dtype, shape, dev), heads, *_heads(k, "k", dtype, kv, dev), *_heads(v, "v", dtype, kv, dev), kv_heads,
+            _ints(positions, "positions", tokens, dev), _ints(freqs, "freqs", half, dev, _F64), 2 * half)
+    places = (_ints(slots, "slots", tokens, dev), *_cache(k_cache, "k_cache", dtype, cache, dev), *_cache(v_cache, "v_cache", dtype, cache, dev), pages)
+    try:
+        args = ROPE_APPEND_ARGS.pack(*rows, interleaved, magnitude, *places, tokens, dim, _type(dtype, "q"))
+    except struct.error:
+        raise BBError(_TURN.format(interleaved, magnitude)) from None
+    rc = _LIB.bb_rope_append(args, _raw_stream(dev))
     if rc:
         _done(rc, "bb_rope_append")
     return q_out
@@ -484,6 +501,9 @@ def _attention_outputs(q, shape, out, lse, dev):
             raise BBError(f"lse: expected contiguous torch.float32 {tuple(shape[:2])} on cuda:{dev}, got {lse.dtype} {tuple(lse.shape)} on {lse.device}")
         pl = lse.data_ptr()
     return out, (*_heads(out, "out", q.dtype, shape, dev), pl)
+
+
+_NUMBERS = "block and scale: expected an integer of 64 bits and a number, got {!r} and {!r}"
 
 
 def _attend(call, workspace_bytes, args, dev, what):
@@ -515,8 +535,11 @@ def attention(q, k, v, q_starts, k_starts=None, block=0, scale=None, out=None, l
     n = _ranges(q_starts, "q_starts")
     qs = _ints(q_starts, "q_starts", n, dev)
     ks = qs if k_starts is None else _ints(k_starts, "k_starts", n, dev)
-    args = ATTENTION_ARGS.pack(*_heads(q, "q", dtype, shape, dev), *_heads(k, "k", dtype, kv, dev), *_heads(v, "v", dtype, kv, dev), qs, ks, n - 1, tokens, kv[0], heads, kv[1], dim,
-                               _type(dtype, "q"), block, dim ** -0.5 if scale is None else scale, *outs)
+    heads_of = (*_heads(q, "q", dtype, shape, dev), *_heads(k, "k", dtype, kv, dev), *_heads(v, "v", dtype, kv, dev))
+    try:
+        args = ATTENTION_ARGS.pack(*heads_of, qs, ks, n - 1, tokens, kv[0], heads, kv[1], dim, _type(dtype, "q"), block, dim ** -0.5 if scale is None else scale, *outs)
+    except struct.error:
+        raise BBError(_NUMBERS.format(block, scale)) from None
     _attend(_LIB.bb_attention, _LIB.bb_attention_workspace_bytes, args, dev, "bb_attention")
     return out
 
@@ -552,9 +575,12 @@ def shared_attention(q, q_starts, k_cache, v_cache, own_pages, own_lens, prefix_
         prefix = (*_table(prefix_pages, "prefix_pages", groups, dev), _ints(prefix_lens, "prefix_lens", groups, dev), gs, groups)
     elif prefix_pages is not None or prefix_lens is not None:
         raise BBError("prefix_pages or prefix_lens without group_starts")
-    args = SHARED_ATTENTION_ARGS.pack(*_heads(q, "q", dtype, shape, dev), qs, n, tokens, *_cache(k_cache, "k_cache", dtype, cache, dev),
-                                      *_cache(v_cache, "v_cache", dtype, cache, dev), cache[0], *_table(own_pages, "own_pages", n, dev), _ints(own_lens, "own_lens", n, dev),
-                                      *prefix, heads, cache[1], dim, _type(dtype, "q"), block, dim ** -0.5 if scale is None else scale, *outs)
+    branches = (*_heads(q, "q", dtype, shape, dev), qs, n, tokens, *_cache(k_cache, "k_cache", dtype, cache, dev), *_cache(v_cache, "v_cache", dtype, cache, dev), cache[0],
+                *_table(own_pages, "own_pages", n, dev), _ints(own_lens, "own_lens", n, dev), *prefix)
+    try:
+        args = SHARED_ATTENTION_ARGS.pack(*branches, heads, cache[1], dim, _type(dtype, "q"), block, dim ** -0.5 if scale is None else scale, *outs)
+    except struct.error:
+        raise BBError(_NUMBERS.format(block, scale)) from None
     _attend(_LIB.bb_shared_attention, _LIB.bb_shared_attention_workspace_bytes, args, dev, "bb_shared_attention")
     return out
 

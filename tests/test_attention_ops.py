@@ -494,7 +494,7 @@ def test_every_plan_of_shared_prefixes(rows, own, prefixes, groups, block, heads
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("n,at", [(140, 75), (9, 4), (300, 250)])
+@pytest.mark.parametrize("n,at", [(140, 75), (140, 66), (140, 69), (140, 94), (9, 4), (300, 250)])
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_unseen_values_under_every_plan(bad, dim, n, at):
@@ -576,7 +576,10 @@ def test_python_refuses_on_the_device():
            lambda: bb.attention(x, x, x, s, scale=0.0), lambda: bb.attention(x[0], x, x, s), lambda: bb.attention(x, x, x, s.cpu()),
            lambda: bb.shared_attention(x, s, c, c[:, :2], op, ol), lambda: bb.shared_attention(x, s, c[0], c[0], op, ol), lambda: bb.shared_attention(x, s, c, c, op[0], ol),
            lambda: bb.shared_attention(x, s, c, c, op, ol.long()), lambda: bb.shared_attention(x, s, c, c, op, ol, op, ol), lambda: bb.shared_attention(x, s, c, c, op, ol, group_starts=ints([0, 1]).to(DEV)),
-           lambda: bb.shared_attention(x, s, c[:, :, :32], c[:, :, :32], op, ol), lambda: bb.shared_attention(x, s, c, c, op, ol, out=x)]
+           lambda: bb.shared_attention(x, s, c[:, :, :32], c[:, :, :32], op, ol), lambda: bb.shared_attention(x, s, c, c, op, ol, out=x),
+           lambda: bb.attention(x, x, x, s[0]), lambda: bb.attention(x, x, x, s, s[0]), lambda: bb.attention(x, x, x, s, block=1.5), lambda: bb.attention(x, x, x, s, block=1 << 70),
+           lambda: bb.attention(x, x, x, s, scale="1"), lambda: bb.shared_attention(x, s[0], c, c, op, ol), lambda: bb.shared_attention(x, s, c, c, op, ol[0]),
+           lambda: bb.shared_attention(x, s, c, c, op, ol, op, ol, s[0]), lambda: bb.shared_attention(x, s, c, c, op, ol, block="1")]
     for i, call in enumerate(bad):
         with pytest.raises(BBError):
             call()

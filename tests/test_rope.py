@@ -202,7 +202,9 @@ def test_python_refuses_on_the_device():
            lambda: bb.rope(x, x, pos, f), lambda: bb.rope(x[:, :, :32], None, pos, f[:16], q_out=x[:, :, 16:48]),
            lambda: bb.rope_append(x, x.clone(), x, pos, f, c, c, pos), lambda: bb.rope_append(x, x.clone(), x, pos, f, c, c[:, :2], pos),
            lambda: bb.rope_append(x, x.clone(), x, pos, f, c, c.float(), pos), lambda: bb.rope_append(x, x.clone(), x, pos, f, c, c.clone(), pos.long()),
-           lambda: bb.rope(x.expand(3, 4, 64), None, pos, f, q_out=x[:1].expand(3, 4, 64))]
+           lambda: bb.rope(x.expand(3, 4, 64), None, pos, f, q_out=x[:1].expand(3, 4, 64)),
+           lambda: bb.rope(x, None, pos, f[0]), lambda: bb.rope(x, None, pos[0], f), lambda: bb.rope(x, None, pos, f, magnitude="1"), lambda: bb.rope(x, None, pos, f, interleaved=0.5),
+           lambda: bb.rope_append(x, x.clone(), x, pos, f[0], c, c.clone(), pos), lambda: bb.rope_append(x, x.clone(), x, pos, f, c[0, 0, 0, 0], c.clone(), pos)]
     for i, call in enumerate(bad):
         with pytest.raises(BBError):
             call()
