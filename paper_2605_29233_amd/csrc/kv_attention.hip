@@ -56,7 +56,8 @@ struct KvArgs {
     float* part_o; float2* part_ml;                                     // [part][token][head]: unscaled output; maximum (times log2(e)) and sum.  Null: a single part
 };
 #define KV_LEAST_TILES 2                // of 64 keys, a part of a row tile's keys
-#define KV_MOST_PARTS 32
+#define KV_MOST_PARTS 32                // of a branch's own keys, of a prefix
+#define KV_FEW_PARTS 6                  // from there on the join takes them four ways
 #define KV_MOST_COLUMNS (BB_MAX_TOKENS / BB_PAGE_TOKENS)
 #define KV_ROWS 128                     // rows (tokens x heads of a group) of a workgroup
 
@@ -657,40 +658,63 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
     else through([&](char* at, float x, float y, float z, float w) { *reinterpret_cast<x4*>(at) = x4{(E)(x * inv), (E)(y * inv), (E)(z * inv), (E)(w * inv)}; }, IC(2));
 }
 
-// The parts of every row, joined: a group of D / 4 lanes takes each WAYS-th of them, and the groups are joined in order.  (Four ways for many parts, which a row's chain of loads
-// would be long for; one, and more rows a workgroup, for few.)
+// The parts of every row, joined: a group of D / 4 lanes takes each WAYS-th of them, AT_ONCE loads on their way while the group's lanes see to the parts' maxima and sums, a part a
+// lane; the groups are joined in order.  (Four ways for many parts, which a row's chain of loads would be long for; one, and more rows a workgroup, for few.)
 template <class E, int D, int WAYS> __global__ __launch_bounds__(256) void kv_join_kernel(KvArgs a) {
     typedef E x4 __attribute__((ext_vector_type(4)));
-    constexpr int LANES = D / 4, ROWS = 256 / LANES / WAYS;
+    constexpr int LANES = D / 4, ROWS = 256 / LANES / WAYS, AT_ONCE = WAYS == 1 ? KV_FEW_PARTS - 1 : 8, PER_LANE = 2 * KV_MOST_PARTS / LANES;
     __shared__ float4 outs[WAYS][ROWS][LANES];
-    __shared__ float sums[WAYS][ROWS];
     RowTile r;
     if (!find_tile(a, nullptr, a.n_seq, blockIdx.x, a.heads, ROWS, r, [](int, int&, int&) {})) return;
     const int rows = r.n * a.heads, n_parts = a.prefix_split + a.own_split;
     const int l = threadIdx.x % LANES, i = threadIdx.x / LANES % ROWS, way = threadIdx.x / LANES / ROWS, row = r.tile * ROWS + i;
     const long parts = (long)a.q_tokens * a.heads, at = (long)r.q0 * a.heads + min(row, rows - 1);
+    float2 ml[PER_LANE];
+#pragma unroll
+    for (int n = 0; n < PER_LANE; ++n) ml[n] = l + n * LANES < n_parts ? a.part_ml[(l + n * LANES) * parts + at] : make_float2(-INFINITY, 0.f);
+    float4 x[AT_ONCE];
+    auto load = [&](int from) {
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+            if (from + u * WAYS < n_parts) x[u] = *reinterpret_cast<const float4*>(a.part_o + ((from + u * WAYS) * parts + at) * D + 4 * l);
+    };
+    load(way);
     float top = -INFINITY, sum = 0.f;
-#pragma unroll 4
-    for (int p = 0; p < n_parts; ++p) top = fmaxf(top, a.part_ml[p * parts + at].x);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int p = way; p < n_parts; p += WAYS) {
-        const float2 ml = a.part_ml[p * parts + at];
-        if (no_key(ml.x, ml.y)) continue;                       // (its output was not written)
-        const float keep = rescale(ml.x, top);
-        const float4 x = *reinterpret_cast<const float4*>(a.part_o + (p * parts + at) * D + 4 * l);
-        sum += ml.y * keep;
-        o.x += x.x * keep; o.y += x.y * keep; o.z += x.z * keep; o.w += x.w * keep;
+#pragma unroll
+    for (int n = 0; n < PER_LANE; ++n) top = fmaxf(top, ml[n].x);
+#pragma unroll
+    for (int d = 1; d < LANES; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    float keep[PER_LANE];                                       // -1: no key, its output was not written
+#pragma unroll
+    for (int n = 0; n < PER_LANE; ++n) {
+        const bool none = no_key(ml[n].x, ml[n].y);
+        keep[n] = none ? -1.f : rescale(ml[n].x, top);
+        sum += none ? 0.f : ml[n].y * keep[n];
     }
-    outs[way][i][l] = o;
-    if (l == 0) sums[way][i] = sum;
-    __syncthreads();
+#pragma unroll
+    for (int d = 1; d < LANES; d *= 2) sum += __shfl_xor(sum, d);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int from = way; from < n_parts; from += AT_ONCE * WAYS) {
+        if (from != way) load(from);
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int p = from + u * WAYS;
+            float k = keep[0];
+#pragma unroll
+            for (int n = 1; n < PER_LANE; ++n) k = p / LANES == n ? keep[n] : k;
+            k = __shfl(k, p, LANES);
+            if (p < n_parts && k >= 0.f) { o.x += x[u].x * k; o.y += x[u].y * k; o.z += x[u].z * k; o.w += x[u].w * k; }
+        }
+    }
+    if (WAYS > 1) {
+        outs[way][i][l] = o;
+        __syncthreads();
+    }
     if (way || row >= rows) return;
 #pragma unroll
     for (int w = 1; w < WAYS; ++w) {
-        const float4 x = outs[w][i][l];
-        o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
-        sum += sums[w][i];
+        const float4 y = outs[w][i][l];
+        o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
     }
     const float inv = no_key(top, sum) ? 0.f : 1.f / sum;
     const int token = row / a.heads, head = row - token * a.heads;
@@ -703,7 +727,7 @@ template <class E, int D, bool PAGED> static void launch_kv(const KvArgs& a, hip
     if (a.halves == 2) kv_attention_kernel<E, D, PAGED, 2><<<grid, 512, 0, s>>>(a); else kv_attention_kernel<E, D, PAGED, 1><<<grid, 256, 0, s>>>(a);
     auto groups = [&](int rows) { return (unsigned)(((long)a.q_tokens * a.heads + (rows - 1) * (long)a.n_seq) / rows); };
     if (!a.part_o) return;
-    if (a.own_split + a.prefix_split >= 6) kv_join_kernel<E, D, 4><<<groups(64 / (D / 4)), 256, 0, s>>>(a); else kv_join_kernel<E, D, 1><<<groups(256 / (D / 4)), 256, 0, s>>>(a);
+    if (a.own_split + a.prefix_split >= KV_FEW_PARTS) kv_join_kernel<E, D, 4><<<groups(64 / (D / 4)), 256, 0, s>>>(a); else kv_join_kernel<E, D, 1><<<groups(256 / (D / 4)), 256, 0, s>>>(a);
 }
 template <bool PAGED> static void launch_kv(const KvArgs& a, int type, int head_dim, hipStream_t s) {
     if (type == BB_BF16) head_dim == 128 ? launch_kv<__bf16, 128, PAGED>(a, s) : launch_kv<__bf16, 64, PAGED>(a, s);
