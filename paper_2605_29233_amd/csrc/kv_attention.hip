@@ -10,7 +10,8 @@
 //   S^T[key][row]  = K[key][:] . Q[row][:]       A = K from LDS, B = Q in registers
 //   O^T[d][row]   += V^T[d][key] . P^T[key][row] A = V^T by transposing LDS reads, B = P out of S^T's own registers: a lane holds keys
 //                                                4 h + {0..3} and 8 + 4 h + {0..3} of every 16 (h = lane / 32), and V^T is read in that order
-// P is rounded to the operands' type (off by 2^-8 of a weight at most in bf16, 2^-11 in fp16, of random sign), as the matrix cores take it; the sum of weights is not.
+// P is rounded to the operands' type (off by 2^-8 of a weight at most in bf16, 2^-11 in fp16, or 2^-25 of weight 1
+// where it is below 2^-14; of random sign), as the matrix cores take it; the sum of weights is not.
 #include "heads.h"
 #include "lds.h"
 #include "sched.h"
@@ -382,7 +383,15 @@ static __device__ __forceinline__ void weigh(RowState<D>& r, unsigned vp, unsign
 // Up to 32 rows: every wave has all of them and takes each 4 HALVES-th tile of 32 keys through a slice of LDS of its own (K of the next while it works on V of the last),
 // without barriers.  The waves of the same rows are joined at the end, in order.
 // One half, two workgroups a CU: where there are items enough (each runs on while the other waits at its barrier).  Two halves, one workgroup a CU: where there are few, so that
-// fewer parts of the keys have to be joined through memory.
+// fewer parts of the keys have to be joined through memory (four branches of 120 rows in all on 512 shared and 104 to 128 own keys, 32 heads: 16.7 us, 18.1 with one half).
+//
+// What bounds it.  16384 causal tokens of 32 heads of 128: 1960 to 2060 us, 1.07 to 1.12 PFLOP/s (a library product of 8192^3 on the same card 1.39): the clock is down to 1.9 GHz for
+// power, the matrix pipes are busy for 0.51 of the time and the vector pipes, with the exponentials, conversions and maxima, for 0.52; without the fetches it would take 0.88 of the time, without the
+// products 0.65.  The two pipes overlap no better whichever way their instructions are laid out (two tiles of scores at once, halves of a tile by turns, priorities: the same within 1 %, or slower).  Short prompts (sixteen of 1 to 1008 tokens, 28 heads on 4: 78 us, 0.6 PFLOP/s) are bound by an item's own time, 11600 cycles besides its tiles: 1700 until its
+// sequence is found, 2000 until the first fetch is on its way, the fetch, the join or the barrier, 3300 for its rows' way out.
+//
+// Why 128 rows by 64 keys: a wave's 32 rows keep queries, weights, scores and output in registers (227 of 256, so two waves a SIMD), K,V of 64 keys come into LDS once for four waves, twice over
+// (64 KiB, two workgroups a CU), and a page is one tile.  K Q^T rather than Q K^T, so that a lane's weights are what the second product takes from it, without a way through LDS.
 template <class E, int D, bool PAGED, int HALVES>
 __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a) {
     typedef typename Half<E>::x8 x8;
@@ -632,8 +641,8 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
             }
         return;
     }
-    // 32 rows a wave, through its slice of LDS, so that whole rows are stored at once (8 bytes of each of 64 rows at a time: 2.2 us instead of
-    // less than one).  Piece c of row r lies at c ^ r.
+    // 32 rows a wave, through its slice of LDS, so that whole rows are stored at once (8 bytes of each of 64 rows at a time took an item 2.2 us
+    // instead of less than one).  Piece c of row r lies at c ^ r.
     if (HALVES == 1) __syncthreads();                           // (all have left the stages; after the halves' join they have)
     if (h2 == 0) places[w4][lane] = store ? place : -1;
     auto through = [&](auto put, auto bytes_of) {
@@ -660,6 +669,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
 
 // The parts of every row, joined: a group of D / 4 lanes takes each WAYS-th of them, AT_ONCE loads on their way while the group's lanes see to the parts' maxima and sums, a part a
 // lane; the groups are joined in order.  (Four ways for many parts, which a row's chain of loads would be long for; one, and more rows a workgroup, for few.)
+// Memory bounds it: 14000 rows of 128 in four parts 7.7 us (33 MB, 4.2 TB/s); 1792 rows in 25 parts 6.4 us (23 MB), 9.0 with a load after the other.
 template <class E, int D, int WAYS> __global__ __launch_bounds__(256) void kv_join_kernel(KvArgs a) {
     typedef E x4 __attribute__((ext_vector_type(4)));
     constexpr int LANES = D / 4, ROWS = 256 / LANES / WAYS, AT_ONCE = WAYS == 1 ? KV_FEW_PARTS - 1 : 8, PER_LANE = 2 * KV_MOST_PARTS / LANES;

@@ -36,6 +36,8 @@ static __device__ __forceinline__ RopePlace place_of(const RopeArgs& a, long t) 
 
 // Rows of 16-byte pieces.  A unit is a piece and the one it is turned with (half: half the turned range further on; interleaved: a piece holds its pairs), or a piece of what is
 // not turned; values move in the same units.  A thread takes units of all its workgroup's tokens' heads, its loads on their way while the angles are made.
+// Memory bounds it where there is much: 20480 tokens of 32 heads of 128 bf16 into a cache 191 us, 5.3 TB/s of 1.0 GB (a copy of 1 GiB runs at 5.1; element by element,
+// as below, 466 us).  Little (one token 2.7 us, 112 of 28 heads 3.3) is a launch, the position's load and its angles' 64-bit product behind one another.
 template <class E, bool INTER> __global__ __launch_bounds__(256) void rope_pieces_kernel(RopeArgs a) {
     constexpr int VEC = 16 / sizeof(E), AT_ONCE = 4;
     typedef E vec __attribute__((ext_vector_type(VEC)));
