@@ -386,7 +386,8 @@ int bb_rope_append(const bb_rope_append_args* args_host, void* hip_stream);
  * p < 0 (block == 1: causal).  A query that sees no key gives zeros.  Tokens outside every sequence are left as they were.  lse (may be NULL):
  * [q_tokens][heads] fp32, contiguous, the natural logarithm of the sum of exp(scale q k) (-inf where no key is seen), for joining partial results.  Equal calls give equal bits; a row's may
  * differ in their last places between calls of other sizes, as its keys are summed in other parts.
- * type BB_BF16 or BB_F16; head_dim 64 or 128; scale > 0; q_tokens * heads below 2^31; all pointers of heads 16-byte aligned and their strides multiples of 8 elements, those between tokens of k and v at most 2^23.
+ * type BB_BF16 or BB_F16; head_dim 64 or 128; scale > 0; q_tokens * heads at most 2^30, q_tokens * heads / 128 + kv_heads * sequences
+ * below 2^24; all pointers of heads 16-byte aligned and their strides multiples of 8 elements, those between tokens of k and v at most 2^23.
  * NaN and infinities in keys and values that a query does not see do not reach it.
  * workspace_dev: at least bb_attention_workspace_bytes() of the same sizes (it looks at no pointer, stride, block or scale), 256-byte aligned (may be NULL if that is 0), used by this call
  * alone until its work is done. */

@@ -746,7 +746,7 @@ template <bool PAGED> static void launch_kv(const KvArgs& a, int type, int head_
 
 static bool refuse_attention(long q_tokens, long n_seq, long heads, long kv_heads, long head_dim, long type, long block, double scale) {
     return (type != BB_BF16 && type != BB_F16) || (head_dim != 64 && head_dim != 128) || q_tokens < 0 || q_tokens > BB_MAX_TOKENS || n_seq < 0 || n_seq > BB_MAX_TOKENS || heads < 1 ||
-           heads > BB_MAX_HEADS || kv_heads < 1 || heads % kv_heads || q_tokens * heads > 0x7FFFFFFF || block < 0 || block > 0x7FFFFFFF || !((float)scale > 0) || !((float)scale * 1.45f < INFINITY);
+           heads > BB_MAX_HEADS || kv_heads < 1 || heads % kv_heads || q_tokens * heads > 1L << 30 || block < 0 || block > 0x7FFFFFFF || !((float)scale > 0) || !((float)scale * 1.45f < INFINITY);
 }
 // A plan: halves of a workgroup, parts of a branch's keys, of a group's prefix (0: taken by the branches before their own).
 struct KvPlan { int halves, own_parts, prefix_parts; };
@@ -763,8 +763,11 @@ static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim,
     const long own_like = std::max(1L, a.n_seq * ((rows / a.n_seq + KV_ROWS - 1) / KV_ROWS)), pre_like = pre ? std::max(1L, a.n_groups * ((rows / a.n_groups + KV_ROWS - 1) / KV_ROWS)) : 0;
     const long own_cols = std::max(1L, (own_keys + 63) / 64), pre_cols = (prefix_keys + 63) / 64;
     const double scale = head_dim == 64 ? DIM_64 : 1, of = rows / a.n_seq <= 32 ? FEW : 1, pf = pre && rows / a.n_groups <= 32 ? FEW : 1;
+    // Launches of less than 2^32 threads (the join's workgroups have two rows at least).
+    auto fits = [&](int halves, long op, long pp) { return (own * op + pre * pp) * a.kv_heads < (1L << 24) / halves && (op + pp == 1 || (long)a.q_tokens * a.heads + 7L * a.n_seq < 1L << 25); };
     long own_parts = 1, pre_parts = 0;
     double best = 0;
+    a.halves = 1;
     for (int apart = 0; apart <= (pre ? 1 : 0); ++apart)
         for (int halves = 1; halves <= 2; ++halves)
             for (int parts : counts) {
@@ -772,6 +775,7 @@ static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim,
                 const long cols = apart ? std::max(own_cols, pre_cols) : own_cols + pre_cols, c = (cols + parts - 1) / parts;
                 if (parts > 1 && c < KV_LEAST_TILES) break;
                 const long op = apart ? std::min<long>((own_cols + c - 1) / c, parts) : parts, pp = apart ? std::min<long>((pre_cols + c - 1) / c, parts) : 0;
+                if (!fits(halves, op, pp)) continue;
                 auto rounds = [&](long n, long in) { return (double)(((n + in - 1) / in + halves - 1) / halves); };
                 const double oc = rounds(apart ? own_cols : cols, op) * of, pc = apart ? rounds(pre_cols, pp) * pf : 0, oi = (double)own_like * op * a.kv_heads, pi = (double)pre_like * pp * a.kv_heads;
                 const bool full = oi + pi > 256;
@@ -784,7 +788,7 @@ static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim,
         if (given->halves < 1 || given->halves > 2 || given->own_parts < 1 || given->own_parts > KV_MOST_PARTS || given->prefix_parts < 0 || given->prefix_parts > KV_MOST_PARTS) return false;
         a.halves = given->halves; own_parts = given->own_parts; pre_parts = pre ? given->prefix_parts : 0;
     }
-    if ((own * own_parts + pre * pre_parts) * a.kv_heads > 0x7FFFFFFF || (long)a.q_tokens * a.heads + 3L * a.n_seq > 0x7FFFFFFF || rows + KV_ROWS > 0x7FFFFFFF) return false;
+    if (!fits(a.halves, own_parts, pre_parts)) return false;
     a.own_tiles = (int)own; a.own_split = (int)own_parts; a.prefix_tiles = pre_parts ? (int)pre : 0; a.prefix_split = (int)pre_parts;
     a.by_kv_heads = Divide::by(a.kv_heads); a.by_each = Divide::by(a.each); a.by_block = Divide::by(std::max(a.block, 1)); a.by_own_split = Divide::by(a.own_split);
     a.by_prefix_split = Divide::by(std::max(a.prefix_split, 1));

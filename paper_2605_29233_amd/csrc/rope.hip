@@ -143,6 +143,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 
 // Units are numbered below 2^16, so that a product with 2^32 / n rounded up divides them by n exactly (n up to 2^16).
 #define ROPE_MOST_UNITS 65536
+#define ROPE_MOST_GROUPS (1 << 20)          // of tokens, a launch (one of 2^24 workgroups of 256 threads would be refused)
 template <class E> static void launch_rope(RopeArgs& a, hipStream_t s) {
     constexpr int VEC = 16 / sizeof(E);
     const int turned = a.interleaved ? a.rot / VEC : a.rot / 2 / VEC, rest = (a.dim - a.rot) / VEC, heads = a.q_heads + a.k_heads * (a.vo ? 2 : 1);
@@ -155,15 +156,23 @@ template <class E> static void launch_rope(RopeArgs& a, hipStream_t s) {
         // one thread a unit while there are few; four, or more, where the chip is full
         a.head_units = turned + rest; a.units = (int)units;
         a.per_group = (int)std::max(1L, std::min<long>(256 / units, a.rot ? ROPE_TURNS / (a.rot / 2) : 256));
-        const long groups = (a.tokens + a.per_group - 1) / a.per_group, in_group = a.per_group * units;
+        const long at_once = (long)ROPE_MOST_GROUPS * a.per_group, groups = (std::min(a.tokens, at_once) + a.per_group - 1) / a.per_group, in_group = a.per_group * units;
         const long slices = std::max(1L, std::min((in_group + 255) / 256, 1024 / groups));
         a.per_slice = (int)((in_group + slices - 1) / slices + 255) / 256 * 256;
         a.by_units = units > 1 ? (unsigned)((0x100000000ull + units - 1) / units) : 0;
         a.by_head = a.head_units > 1 ? (unsigned)((0x100000000ull + a.head_units - 1) / a.head_units) : 0;
-        if (units > 1 && a.head_units > 1 && groups <= 0x7FFFFFFF) {
-            const dim3 grid((unsigned)groups, (unsigned)((in_group + a.per_slice - 1) / a.per_slice));
-            if (a.interleaved) rope_pieces_kernel<E, true><<<grid, 256, 0, s>>>(a); else rope_pieces_kernel<E, false><<<grid, 256, 0, s>>>(a);
-            return;
+        if (units > 1 && a.head_units > 1) {
+            const long all = a.tokens;
+            for (long t = 0; t < all; t += at_once) {
+                a.tokens = std::min(all - t, at_once);
+                const dim3 grid((unsigned)((a.tokens + a.per_group - 1) / a.per_group), (unsigned)((in_group + a.per_slice - 1) / a.per_slice));
+                if (a.interleaved) rope_pieces_kernel<E, true><<<grid, 256, 0, s>>>(a); else rope_pieces_kernel<E, false><<<grid, 256, 0, s>>>(a);
+                if (all - t <= at_once) return;
+                const long bytes = at_once * (long)sizeof(E);
+                a.q += a.q_ts * bytes; a.qo += a.qo_ts * bytes; a.k += a.k_ts * bytes; a.v += a.v_ts * bytes;
+                a.positions += at_once;
+                if (a.slots) a.slots += at_once; else a.ko += a.ko_ts * bytes;
+            }
         }
     }
     rope_kernel<E><<<(unsigned)std::min<long>(a.tokens, 1 << 20), 256, 0, s>>>(a);

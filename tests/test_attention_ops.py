@@ -530,7 +530,7 @@ def test_c_entries_refuse_before_touching_a_device():
     for bad in (dict(q=0), dict(q=p + 2), dict(qt=250), dict(qh=4), dict(k=0), dict(k=2 * p + 8), dict(kt=1 << 24), dict(v=0), dict(vh=65), dict(qs=0), dict(ks=0),
                 dict(qs=4 * p + 1), dict(n=-1), dict(qn=-1), dict(kn=-1), dict(qn=1 << 31), dict(n=1 << 33), dict(heads=3), dict(heads=0), dict(kv=0), dict(heads=4096, kv=2), dict(dim=96),
                 dict(dim=0), dict(type=0), dict(type=7), dict(block=-1), dict(block=1 << 31), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
-                dict(scale=1e39), dict(scale=1e-60), dict(lse=p + 4), dict(lse=2 * p), dict(heads=1024, kv=1024, qn=1 << 24), dict(o=0), dict(ot=128), dict(oh=0), dict(o=p), dict(o=2 * p), dict(o=3 * p + 128), dict(lse=6), dict(qt=-8), dict(qt=1 << 50)):
+                dict(scale=1e39), dict(scale=1e-60), dict(lse=p + 4), dict(lse=2 * p), dict(n=1 << 24), dict(heads=1024, kv=4, qn=(1 << 20) + 1), dict(heads=1024, kv=1024, qn=1 << 24), dict(o=0), dict(ot=128), dict(oh=0), dict(o=p), dict(o=2 * p), dict(o=3 * p + 128), dict(lse=6), dict(qt=-8), dict(qt=1 << 50)):
         assert call(**bad) == -1, bad
     args = binding.ATTENTION_ARGS.pack(*good.values())
     for halves, parts in ((0, 1), (3, 1), (1, 0), (1, 33), (1, -1)):

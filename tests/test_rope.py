@@ -132,6 +132,32 @@ def test_cache_beyond_32_bits():
 
 
 @pytest.mark.gpu
+def test_more_tokens_than_a_launch_takes():
+    """A workgroup for every token, and more of them than a launch has: rows on both sides of the border, and the last."""
+    tokens, heads, kv_heads, dim = (1 << 20) + 3, 40, 8, 64
+    q = torch.zeros(tokens, heads, dim, dtype=torch.bfloat16, device=DEV)
+    kv = torch.zeros(tokens, 2 * kv_heads, dim, dtype=torch.bfloat16, device=DEV)
+    cache = torch.zeros(2, tokens // PAGE + 1, kv_heads, PAGE, dim, dtype=torch.bfloat16, device=DEV)
+    at = torch.tensor([0, 1, (1 << 20) - 1, 1 << 20, tokens - 1])
+    x, y = rnd(1, len(at), heads, dim), rnd(2, len(at), 2 * kv_heads, dim)
+    q[at.to(DEV)], kv[at.to(DEV)] = x.to(DEV), y.to(DEV)
+    pos = torch.arange(tokens, dtype=torch.int32).flip(0)
+    slots = torch.arange(tokens, dtype=torch.int32) ^ 1                     # (an odd number of tokens: the last one's slot is one further)
+    f = freqs_of(dim)
+    wq, wk = turned(x, pos[at], f, False), turned(y[:, :kv_heads], pos[at], f, False)
+    k0 = kv[:, :kv_heads].clone()
+    bb.rope_append(q, k0, kv[:, kv_heads:], pos.to(DEV), f.to(DEV), cache[0], cache[1], slots.to(DEV))
+    close(q[at.to(DEV)], *wq, torch.bfloat16)
+    s = slots[at].long().to(DEV)
+    close(cache[0][s // PAGE, :, s % PAGE], *wk, torch.bfloat16)
+    assert torch.equal(cache[1][s // PAGE, :, s % PAGE].cpu(), y[:, kv_heads:])
+    r, k = bb.rope(q, k0, (-pos).to(DEV), f.to(DEV))                        # back, in place
+    w = turned(x, pos[at], f, False)
+    assert r is q and k is k0 and float((r[at.to(DEV)].cpu().double() - x.double()).abs().max()) <= float(2 ** -6 * w[0].abs().max())
+    assert float(q[7].abs().max()) == 0
+
+
+@pytest.mark.gpu
 def test_not_a_number_stays_in_its_pair():
     x = rnd(1, 2, 2, 64, dtype="fp16")
     x[0, 1, 5], x[1, 0, 40] = float("nan"), float("inf")
