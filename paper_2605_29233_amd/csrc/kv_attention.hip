@@ -72,49 +72,86 @@ static __device__ __forceinline__ int lane_sums(int x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);     // row_bcast:31 into rows 2 and 3
     return x;
 }
-// Of the sequences' row tiles the t-th: which sequence (range i of starts[step[i]] .., step null: i), its first token, its tokens, which of its tiles.  Starts are
-// taken as they come but never outside 0 .. q_tokens.  extra(i, x, y): two more values of the sequence, loaded with the starts.
+// The sequences' row tiles have numbers.  Up to KV_SUMMED sequences: one after the other, found by sums over the sequences, 64 at a look.  More: sequence i (starts[i] .., or with steps
+// starts[step[i]] ..) has those from starts[i] * each / ROWS + i on, which leaves it room for all its tiles and now and then one that is none; 64 equal shares of the sequences at a look,
+// and on in the last that begins at the number or before.  (A token each of 128, 256, 1024, 4096 branches on 64 keys, 28 heads on 4: sums 8.6, 16.8, 67.5, 526 us, shares 11.9, 18.4, 50.6, 209.)
+#define KV_SUMMED 512
+// How many numbers there may be.
+static long tile_numbers(long rows, long sequences, int rows_per_tile) {
+    return sequences <= KV_SUMMED ? (rows + (rows_per_tile - 1) * sequences) / rows_per_tile : (rows + rows_per_tile - 1) / rows_per_tile + sequences - 1;
+}
+// Of number t: which sequence, its first token, its tokens, which of its tiles; false: none.  Starts are taken as they come but never outside 0 .. q_tokens.  extra(i, x, y): two
+// more values of the sequence, loaded with the starts.
 struct RowTile { int seq, q0, n, tile, x, y; };
-template <class F>
-static __device__ __forceinline__ bool find_tile(const KvArgs& a, const int* __restrict__ step, int ranges, int t, int each, int rows_per_tile, RowTile& r, F&& extra) {
+template <int ROWS, class F>
+static __device__ __forceinline__ bool find_tile(const KvArgs& a, const int* __restrict__ step, int ranges, int t, int each, RowTile& r, F&& extra) {
     const int lane = threadIdx.x & 63;
-    for (int b = 0; b < ranges; b += 64) {
-        const int i = b + lane;
-        int s0 = 0, n = 0, x = 0, y = 0;
-        if (i < ranges) {
-            int i0 = i, i1 = i + 1;
-            if (step) { i0 = min(max(step[i], 0), a.n_seq); i1 = min(max(step[i + 1], i0), a.n_seq); }
-            extra(i, x, y);
-            s0 = min(max(a.q_starts[i0], 0), a.q_tokens);
-            n = min(max(a.q_starts[i1], s0), a.q_tokens) - s0;
+    auto start_at = [&](int i) { return min(max(a.q_starts[i], 0), a.q_tokens); };
+    auto range = [&](int i, int& s0, int& n, int& x, int& y) {
+        int i0 = i, i1 = i + 1;
+        if (step) { i0 = min(max(step[i], 0), a.n_seq); i1 = min(max(step[i + 1], i0), a.n_seq); }
+        extra(i, x, y);
+        s0 = start_at(i0);
+        n = max(start_at(i1), s0) - s0;
+    };
+    auto found = [&](int seq, int l, int s0, int n, int x, int y, int first) {
+        r.seq = seq;
+        r.q0 = __builtin_amdgcn_readlane(s0, l);
+        r.n = __builtin_amdgcn_readlane(n, l);
+        r.x = __builtin_amdgcn_readlane(x, l);
+        r.y = __builtin_amdgcn_readlane(y, l);
+        r.tile = t - __builtin_amdgcn_readlane(first, l);
+    };
+    auto tiles_of = [&](int n) { return (int)(((unsigned)n * (unsigned)each + ROWS - 1) / ROWS); };
+    if (ranges <= KV_SUMMED) {
+        for (int b = 0; b < ranges; b += 64) {
+            const int i = b + lane;
+            int s0 = 0, n = 0, x = 0, y = 0;
+            if (i < ranges) range(i, s0, n, x, y);
+            const int mine = tiles_of(n), upto = lane_sums(mine);
+            const unsigned long long hit = __ballot(upto > t);
+            if (hit) {
+                const int l = __builtin_ctzll(hit);
+                found(b + l, l, s0, n, x, y, upto - mine);
+                return true;
+            }
+            t -= __builtin_amdgcn_readlane(upto, 63);
         }
-        const int mine = (int)(((long)n * each + rows_per_tile - 1) / rows_per_tile);
-        const int upto = lane_sums(mine);
-        const unsigned long long hit = __ballot(upto > t);
-        if (hit) {
-            const int l = __builtin_ctzll(hit);
-            r.seq = b + l;
-            r.q0 = __builtin_amdgcn_readlane(s0, l);
-            r.n = __builtin_amdgcn_readlane(n, l);
-            r.x = __builtin_amdgcn_readlane(x, l);
-            r.y = __builtin_amdgcn_readlane(y, l);
-            r.tile = t - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));
-            return true;
-        }
-        t -= __builtin_amdgcn_readlane(upto, 63);
+        return false;
     }
-    return false;
+    auto number = [&](int start, int i) { return (int)((unsigned)start * (unsigned)each / ROWS) + i; };
+    int b = 0, left = ranges;
+    while (left > 64) {
+        const int share = (left + 63) / 64, i = lane * share;
+        int at = b + min(i, left - 1);
+        if (step) at = min(max(step[at], 0), a.n_seq);
+        const int k = __builtin_popcountll(__ballot(i < left && number(start_at(at), b + i) <= t));
+        if (k == 0) return false;
+        b += (k - 1) * share;
+        left = min(share, left - (k - 1) * share);
+    }
+    int s0 = 0, n = 0, x = 0, y = 0;
+    if (lane < left) range(b + lane, s0, n, x, y);
+    const int first = number(s0, b + lane), l = __builtin_popcountll(__ballot(lane < left && first <= t)) - 1;
+    if (l < 0) return false;
+    found(b + l, l, s0, n, x, y, first);
+    return r.tile >= 0 && r.tile < tiles_of(r.n);
 }
 
 // The group a branch belongs to, -1: none.
 static __device__ __forceinline__ int find_group(const KvArgs& a, int seq) {
     const int lane = threadIdx.x & 63;
-    for (int b = 0; b < a.n_groups; b += 64) {
-        const int i = b + lane;
-        const unsigned long long hit = __ballot(i < a.n_groups && a.group_starts[i] <= seq && seq < a.group_starts[i + 1]);
-        if (hit) return b + __builtin_ctzll(hit);
+    int b = 0, n = a.n_groups;
+    while (n > 64) {                                            // (they ascend: 64 equal shares, and on in the last that starts at the branch or before)
+        const int share = (n + 63) / 64, i = lane * share;
+        const int k = __builtin_popcountll(__ballot(i < n && a.group_starts[b + i] <= seq));
+        if (k == 0) return -1;
+        b += (k - 1) * share;
+        n = min(share, n - (k - 1) * share);
     }
-    return -1;
+    const int i = b + lane;
+    const unsigned long long hit = __ballot(lane < n && a.group_starts[i] <= seq && seq < a.group_starts[i + 1]);
+    return hit ? b + __builtin_ctzll(hit) : -1;
 }
 static __device__ __forceinline__ int paged_keys(int n, int width) { return min(max(n, 0), width * BB_PAGE_TOKENS); }
 
@@ -414,7 +451,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
     const int piece = j - from_last * split;
     RowTile r;
     const int* lens = PAGED ? prefix ? a.prefix_lens : a.own_lens : a.k_starts;
-    if (!find_tile(a, prefix ? a.group_starts : nullptr, prefix ? a.n_groups : a.n_seq, (prefix ? a.prefix_tiles : a.own_tiles) - 1 - from_last, a.each, KV_ROWS, r,
+    if (!find_tile<KV_ROWS>(a, prefix ? a.group_starts : nullptr, prefix ? a.n_groups : a.n_seq, (prefix ? a.prefix_tiles : a.own_tiles) - 1 - from_last, a.each, r,
                    [&](int i, int& x, int& y) { x = lens[i]; if (!PAGED) y = lens[i + 1]; }))
         return;
 
@@ -675,7 +712,7 @@ template <class E, int D, int WAYS> __global__ __launch_bounds__(256) void kv_jo
     constexpr int LANES = D / 4, ROWS = 256 / LANES / WAYS, AT_ONCE = WAYS == 1 ? KV_FEW_PARTS - 1 : 8, PER_LANE = 2 * KV_MOST_PARTS / LANES;
     __shared__ float4 outs[WAYS][ROWS][LANES];
     RowTile r;
-    if (!find_tile(a, nullptr, a.n_seq, blockIdx.x, a.heads, ROWS, r, [](int, int&, int&) {})) return;
+    if (!find_tile<ROWS>(a, nullptr, a.n_seq, blockIdx.x, a.heads, r, [](int, int&, int&) {})) return;
     const int rows = r.n * a.heads, n_parts = a.prefix_split + a.own_split;
     const int l = threadIdx.x % LANES, i = threadIdx.x / LANES % ROWS, way = threadIdx.x / LANES / ROWS, row = r.tile * ROWS + i;
     const long parts = (long)a.q_tokens * a.heads, at = (long)r.q0 * a.heads + min(row, rows - 1);
@@ -735,7 +772,7 @@ template <class E, int D, int WAYS> __global__ __launch_bounds__(256) void kv_jo
 template <class E, int D, bool PAGED> static void launch_kv(const KvArgs& a, hipStream_t s) {
     const unsigned grid = (unsigned)((a.prefix_tiles * (long)a.prefix_split + a.own_tiles * (long)a.own_split) * a.kv_heads);
     if (a.halves == 2) kv_attention_kernel<E, D, PAGED, 2><<<grid, 512, 0, s>>>(a); else kv_attention_kernel<E, D, PAGED, 1><<<grid, 256, 0, s>>>(a);
-    auto groups = [&](int rows) { return (unsigned)(((long)a.q_tokens * a.heads + (rows - 1) * (long)a.n_seq) / rows); };
+    auto groups = [&](int rows) { return (unsigned)tile_numbers((long)a.q_tokens * a.heads, a.n_seq, rows); };
     if (!a.part_o) return;
     if (a.own_split + a.prefix_split >= KV_FEW_PARTS) kv_join_kernel<E, D, 4><<<groups(64 / (D / 4)), 256, 0, s>>>(a); else kv_join_kernel<E, D, 1><<<groups(256 / (D / 4)), 256, 0, s>>>(a);
 }
@@ -759,12 +796,12 @@ static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim,
     const double FIRST = 3.4, ITEM = 2.8, BOTH = 0.9, ALONE = 1.0, HALVES = 1.5, MERGE = 0.15, FEW = 0.57, LONGEST = 1.2, JOIN = 3.7, JOIN_BYTES = 2.8e6, DIM_64 = 0.53;
     static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
     const long rows = (long)a.q_tokens * a.each;
-    const long own = (rows + (KV_ROWS - 1) * (long)a.n_seq) / KV_ROWS, pre = prefix_keys > 0 ? (rows + (KV_ROWS - 1) * (long)a.n_groups) / KV_ROWS : 0;
+    const long own = tile_numbers(rows, a.n_seq, KV_ROWS), pre = prefix_keys > 0 ? tile_numbers(rows, a.n_groups, KV_ROWS) : 0;
     const long own_like = std::max(1L, a.n_seq * ((rows / a.n_seq + KV_ROWS - 1) / KV_ROWS)), pre_like = pre ? std::max(1L, a.n_groups * ((rows / a.n_groups + KV_ROWS - 1) / KV_ROWS)) : 0;
     const long own_cols = std::max(1L, (own_keys + 63) / 64), pre_cols = (prefix_keys + 63) / 64;
     const double scale = head_dim == 64 ? DIM_64 : 1, of = rows / a.n_seq <= 32 ? FEW : 1, pf = pre && rows / a.n_groups <= 32 ? FEW : 1;
     // Launches of less than 2^32 threads (the join's workgroups have two rows at least).
-    auto fits = [&](int halves, long op, long pp) { return (own * op + pre * pp) * a.kv_heads < (1L << 24) / halves && (op + pp == 1 || (long)a.q_tokens * a.heads + 7L * a.n_seq < 1L << 25); };
+    auto fits = [&](int halves, long op, long pp) { return (own * op + pre * pp) * a.kv_heads < (1L << 24) / halves && (op + pp == 1 || (long)a.q_tokens * a.heads + 2L * a.n_seq < 1L << 25); };
     long own_parts = 1, pre_parts = 0;
     double best = 0;
     a.halves = 1;

@@ -493,6 +493,68 @@ def test_every_plan_of_shared_prefixes(rows, own, prefixes, groups, block, heads
             check(*run_shared_plan(q, rows, k, v, op, own, pp, prefixes, groups, block, halves, own_parts, prefix_parts), want, q.dtype)
 
 
+def many(n, seed):
+    """Lengths of n sequences: tokens by ones and twos, some empty, a few of more than a tile, the first and the last among them."""
+    g = torch.Generator().manual_seed(seed)
+    lens = torch.randint(0, 3, (n,), generator=g)
+    lens[torch.randint(0, n, (6,), generator=g)] = 131
+    lens[0], lens[-1] = 140, 133
+    return lens.tolist()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads,kv_heads", [(4, 2), (1, 1)])
+@pytest.mark.parametrize("n", [64, 65, 72, 511, 513, 576, 577, 1100, 3000])
+def test_many_sequences(n, heads, kv_heads):
+    """More sequences than a wave has lanes, and than it looks over at once; in one part and in parts that are joined."""
+    ql = many(n, n)
+    kl = [m + 3 * (i % 2) for i, m in enumerate(ql)]
+    q, k, v = inputs(n, ql, kl, heads, kv_heads, 64, "bf16", 2.0)
+    want = attention(q, k, v, ql, kl, 1, 0.125)
+    check(*run(q, k, v, ql, kl, 1, 0.125), want, q.dtype)
+    for parts in (3, 7):
+        check(*run_plan(q, k, v, ql, kl, 1, 1, parts), want, q.dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [64, 65, 127, 128, 129, 600, 4100])
+def test_many_groups(n):
+    """Groups of none to three branches, some branches outside the first and the last; prefixes once a group, and again by every branch."""
+    g = torch.Generator().manual_seed(n)
+    edges = [2]
+    for c in torch.randint(0, 4, (n,), generator=g).tolist():
+        edges.append(edges[-1] + c)
+    branches_n = edges[-1] + 3
+    rows = torch.randint(0, 3, (branches_n,), generator=g).tolist()
+    own = torch.randint(1, 9, (branches_n,), generator=g).tolist()
+    prefixes = torch.randint(0, 70, (n,), generator=g).tolist()
+    q, k, v, op, pp = branches(n, rows, own, prefixes, 2, 1, 64, "bf16")
+    want = shared(q, rows, k, v, op, own, pp, prefixes, edges, 1, 0.125)
+    check(*run_shared(q, rows, k, v, op, own, pp, prefixes, edges, 1), want, q.dtype)
+    for plan in ((1, 1, 0), (1, 1, 1), (2, 2, 0)):
+        check(*run_shared_plan(q, rows, k, v, op, own, pp, prefixes, edges, 1, *plan), want, q.dtype)
+
+
+@pytest.mark.gpu
+def test_starts_of_many_that_do_not_ascend():
+    """Garbage among thousands of starts, lengths and groups: nothing out of range is read or written, and what lies outside stays as it is."""
+    g = torch.Generator().manual_seed(3)
+    n, tokens = 2000, 300
+    q, k = (torch.zeros(tokens, 2, 64, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    room = torch.full((tokens + 20, 2, 64), 9.0, dtype=torch.bfloat16, device=DEV)
+    c = torch.zeros(4, 2, PAGE, 64, dtype=torch.bfloat16, device=DEV)
+
+    def noise(*shape):
+        return torch.randint(-2 ** 31, 2 ** 31 - 1, shape, generator=g).to(torch.int32)
+
+    for qs in (noise(n + 1), noise(n + 1) % 400, torch.tensor([0, 2 ** 30] * (n // 2) + [0], dtype=torch.int32)):
+        qs = qs.to(DEV)
+        bb.attention(q, k, k, qs, noise(n + 1).to(DEV), block=1, out=room[10:-10])
+        bb.shared_attention(q, qs, c, c, noise(n, 2).to(DEV), noise(n).to(DEV), noise(700, 3).to(DEV), noise(700).to(DEV), (noise(701) % 2500).to(DEV), block=1, out=room[10:-10])
+        torch.cuda.synchronize()
+        assert (room[:10] == 9).all() and (room[-10:] == 9).all()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("n,at", [(140, 75), (140, 66), (140, 69), (140, 94), (9, 4), (300, 250)])
 @pytest.mark.parametrize("dim", [64, 128])
