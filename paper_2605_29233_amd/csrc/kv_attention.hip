@@ -50,17 +50,19 @@ struct KvArgs {
     long own_ld, prefix_ld;
     int q_tokens, k_tokens, n_seq, n_groups, n_pages, own_width, prefix_width;
     int heads, kv_heads, each, block;
-    float scale;                                                        // times log2(e)
+    float scale, lag;                                                   // scale times log2(e); KV_LAG / that
     int own_tiles, own_split, prefix_tiles, prefix_split, halves;       // row tiles that the branches (groups) may have, parts that their keys are cut into.  No prefix tiles: a
                                                                         // branch's items take its group's prefix before its own keys
     Divide by_kv_heads, by_each, by_block, by_own_split, by_prefix_split;
-    float* part_o; float2* part_ml;                                     // [part][token][head]: unscaled output; maximum (times log2(e)) and sum.  Null: a single part
+    float* part_o; float2* part_ml;                                     // [part][token][head]: unscaled output; maximum before scale and sum.  Null: a single part
 };
 #define KV_LEAST_TILES 2                // of 64 keys, a part of a row tile's keys
 #define KV_MOST_PARTS 32                // of a branch's own keys, of a prefix
 #define KV_FEW_PARTS 6                  // from there on the join takes them four ways
 #define KV_MOST_COLUMNS (BB_MAX_TOKENS / BB_PAGE_TOKENS)
 #define KV_ROWS 128                     // rows (tokens x heads of a group) of a workgroup
+#define KV_LAG 8                        // a row's running maximum is at most 2^KV_LAG behind
+#define KV_LARGE 1024.f                 // where products with scale stop being what exponents start from
 
 // Sums over the lanes up to each (in the row's order: within rows of 16, then across them).
 static __device__ __forceinline__ int lane_sums(int x) {
@@ -255,15 +257,16 @@ static __device__ __forceinline__ float sum_halves(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Parts of a row: maximum and sum.  A part without a key: (-inf, 0).  One whose scores were all -inf has a finite maximum, so that 0 / 0 comes out as the definition's NaN.
+// Parts of a row: maximum (of the scores before scale) and sum.  A part without a key: (-inf, 0).  One whose scores were all -inf has a finite maximum, so that 0 / 0 comes out as the definition's NaN.
 static __device__ __forceinline__ bool no_key(float top, float sum) { return top == -INFINITY && sum == 0.f; }
-static __device__ __forceinline__ float rescale(float top, float to) { return top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - to); }
-static __device__ __forceinline__ float log_sum(float top, float sum) { return no_key(top, sum) ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.69314718056f; }
+static __device__ __forceinline__ float rescale(float top, float to, float scale) { return top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - to) * scale); }
+static __device__ __forceinline__ float log_sum(float top, float sum, float scale) { return no_key(top, sum) ? -INFINITY : (top * scale + __builtin_amdgcn_logf(sum)) * 0.69314718056f; }
 
-// What a lane keeps of its row: the running maximum (times scale), its half of the sum, its half of the output, whether a key was seen.
-template <int D> struct RowState { f32x16 o[D / 32]; float top, sum; bool met; };
+// What a lane keeps of its row: the running maximum, what its weights' exponents start from and the score above which the maximum follows (see follow()), its half of the sum, its half
+// of the output, whether a key was seen.
+template <int D> struct RowState { f32x16 o[D / 32]; float top, from, bar, sum; bool met; };
 template <int D> static __device__ __forceinline__ void finish(RowState<D>& r) {
-    if (r.met && r.top == -INFINITY && r.sum == 0.f) r.top = -3e38f;
+    if (r.met && r.top == -INFINITY && r.sum == 0.f) r.top = -3.402823e38f;
 }
 
 // LDS by its byte offset.
@@ -297,9 +300,13 @@ template <class E, int D, int NK> static __device__ __forceinline__ void scores(
         __builtin_amdgcn_sched_barrier(0);
     }
 }
-// The rows' maxima follow a tile's scores.  PART: not every row sees all of the tile's keys; seen: how many of them the lane's row does.
-// They follow only by more than 8 (of 2^8): a weight is then at most that, of no less precision, and the output is seldom scaled.
-template <int D, int NK, bool PART> static __device__ __forceinline__ void follow(RowState<D>& r, f32x16 (&s)[NK], float scale, int seen) {
+// The rows' maxima follow a tile's scores, each by itself.  PART: not every row sees all of the tile's keys; seen: how many of them the lane's row does.
+// One follows only by more than KV_LAG (of 2^KV_LAG), so the output is seldom scaled: a weight is then at most that, of no fewer bits.  (The largest is 1 only where the maximum has just followed; elsewhere
+// it is rounded as any other.)
+// Weights are exp2(s * by - from).  From is the maximum times scale, rounded: what the rounding is off by, 2^-25 of it, all weights have in common, but from some 2^27 on it leaves the range of 16-bit
+// weights, and then of fp32.  Beyond KV_LARGE a row's exponents are (s - maximum) * scale instead, its maximum follows every tile, and the two agree within 2^-15 where a row has both (a score's own
+// rounding is off by as much).
+template <int D, int NK, bool PART> static __device__ __forceinline__ void follow(RowState<D>& r, f32x16 (&s)[NK], float scale, float lag, int seen, float& by, float& from) {
     const int h2 = (threadIdx.x & 63) >> 5;
     if (PART) {
         r.met |= seen > 0;
@@ -314,37 +321,50 @@ template <int D, int NK, bool PART> static __device__ __forceinline__ void follo
     for (int i = 0; i < NK; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) best = fmaxf(best, s[i][e]);
-    best = max_halves(best) * scale;
-    if (__ballot(best > r.top + 8.f)) {
-        best = fmaxf(best, r.top);
+    best = max_halves(best);
+    by = scale;
+    if (__ballot(best > r.bar)) {
+        const float to = best > r.bar ? fmaxf(best, r.top) : r.top;
         // (not quite 0: an infinity in the output stays one)
-        const float keep = fmaxf(__builtin_amdgcn_exp2f(r.top - best), 1.2e-38f);
+        const float keep = fmaxf(__builtin_amdgcn_exp2f((r.top - to) * scale), 1.2e-38f);
         r.sum *= keep;
 #pragma unroll
         for (int t = 0; t < D / 32; ++t)
 #pragma unroll
             for (int e = 0; e < 16; ++e) r.o[t][e] *= keep;
-        r.top = best;
+        const bool none = to == -INFINITY, large = !none && fabsf(to * scale) >= KV_LARGE;
+        r.top = to;
+        r.from = none || large ? 0.f : to * scale;
+        r.bar = none || large ? -INFINITY : to + lag;
+        if (__ballot(large)) {
+            const float less = large ? to : 0.f;
+#pragma unroll
+            for (int i = 0; i < NK; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[i][e] = __builtin_fmaf(s[i][e] - less, scale, -r.from);
+            by = 1.f;
+            from = 0.f;
+            return;
+        }
     }
+    from = r.from;
 }
-// What the exponents start from (-inf: no key seen yet, or only scores of -inf: every weight 0).
-template <int D> static __device__ __forceinline__ float from_of(const RowState<D>& r) { return r.top == -INFINITY ? 0.f : r.top; }
 // Scores -> weights p in the operands' type, elements FROM to TO of all 16 NK.
 template <class E, int NK, int FROM, int TO>
-static __device__ __forceinline__ void weights(const f32x16 (&s)[NK], float scale, float from, float (&sum)[2], typename Half<E>::x8 (&p)[2 * NK]) {
+static __device__ __forceinline__ void weights(const f32x16 (&s)[NK], float by, float from, float (&sum)[2], typename Half<E>::x8 (&p)[2 * NK]) {
 #pragma unroll
     for (int n = FROM; n < TO; ++n) {
         const int i = n >> 4, e = n & 15;
-        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], scale, -from));
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], by, -from));
         sum[n & 1] += w;
         p[n >> 3][n & 7] = (E)w;
     }
 }
 template <class E, int D, int NK, bool PART>
-static __device__ __forceinline__ void weights(RowState<D>& r, f32x16 (&s)[NK], float scale, int seen, typename Half<E>::x8 (&p)[2 * NK]) {
-    follow<D, NK, PART>(r, s, scale, seen);
-    float sum[2] = {0.f, 0.f};
-    weights<E, NK, 0, 16 * NK>(s, scale, from_of(r), sum, p);
+static __device__ __forceinline__ void weights(RowState<D>& r, f32x16 (&s)[NK], float scale, float lag, int seen, typename Half<E>::x8 (&p)[2 * NK]) {
+    float by, from, sum[2] = {0.f, 0.f};
+    follow<D, NK, PART>(r, s, scale, lag, seen, by, from);
+    weights<E, NK, 0, 16 * NK>(s, by, from, sum, p);
     r.sum += sum[0] + sum[1];
 }
 // V^T of 16 keys (from 16 st on) and 32 d (from 32 t on), in the order of the weights.  vp: v_piece.
@@ -504,7 +524,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
     for (int t = 0; t < OT; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) st.o[t][e] = 0.f;
-    st.top = -INFINITY; st.sum = 0.f; st.met = false;
+    st.top = st.bar = -INFINITY; st.from = st.sum = 0.f; st.met = false;
 
     const unsigned base = lds_offset(lds);
     const char *kb = a.k + ((long)kvh * a.k_hs + first * a.k_ts) * 2, *vb = a.v + ((long)kvh * a.v_hs + first * a.v_ts) * 2;
@@ -554,7 +574,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
                     bad = __builtin_amdgcn_readfirstlane(b[0] | b[1] | b[2] | b[3]);
                 } else st.met = true;
                 scores<E, D, 2>(kp, at, qf, s);
-                weights<E, D, 2, PART>(st, s, a.scale, seen(cur), p);
+                weights<E, D, 2, PART>(st, s, a.scale, a.lag, seen(cur), p);
                 weigh<E, D, 2, PART>(st, vp, at + STAGE / 2, p, seen(cur), at + STAGE / 2, bad);
             }
             cur = nxt;
@@ -576,7 +596,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
             __syncthreads();
             if (half) return;
             const float2 theirs = ends[wave + 4][lane & 31];
-            const float top = fmaxf(st.top, theirs.x), keep = rescale(st.top, top), take = rescale(theirs.x, top);
+            const float top = fmaxf(st.top, theirs.x), keep = rescale(st.top, top, a.scale), take = rescale(theirs.x, top, a.scale);
 #pragma unroll
             for (int e = 0; e < 4 * OT; ++e) {
                 const float4 x = other[e * 64 + lane];
@@ -615,7 +635,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
             scores<E, D, 1>(kp, to, qf, s);
             wait_lds();
             if (nxt.n) fetch_k(nxt.k, nxt.n, 32, to, 0);
-            weights<E, D, 1, PART>(st, s, a.scale, seen(cur), p);
+            weights<E, D, 1, PART>(st, s, a.scale, a.lag, seen(cur), p);
             if (nxt.n) wait_loads<N>(); else wait_loads<0>();
             weigh<E, D, 1, PART>(st, vp, to + STAGE / 4, p, seen(cur), to + STAGE / 4, PART && any_infinite<E, N, 1>(to + STAGE / 4));
             wait_lds();
@@ -633,8 +653,8 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) top = fmaxf(top, ends[w][lane & 31].x);
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) sum += ends[w][lane & 31].y * rescale(ends[w][lane & 31].x, top);
-        const float keep = rescale(st.top, top);
+        for (int w = 0; w < WAVES; ++w) sum += ends[w][lane & 31].y * rescale(ends[w][lane & 31].x, top, a.scale);
+        const float keep = rescale(st.top, top, a.scale);
         float* all = (float*)lds;
 #pragma unroll
         for (int e = 0; e < 16 * OT; ++e) all[(wave * OT * 16 + e) * 64 + lane] = st.o[e >> 4][e & 15] * keep;
@@ -656,7 +676,7 @@ __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a)
     const long at_row = (long)(r.q0 + token) * a.heads + head, parts = (long)a.q_tokens * a.heads, slot = prefix ? piece : a.prefix_split + piece;
     if (mine && h2 == 0 && (!few || wave == 0)) {
         if (!a.part_o) {
-            if (a.lse) a.lse[at_row] = log_sum(st.top, st.sum);
+            if (a.lse) a.lse[at_row] = log_sum(st.top, st.sum, a.scale);
         } else {
             a.part_ml[slot * parts + at_row] = make_float2(st.top, st.sum);
             if (alone)                                          // a branch outside every group: nobody else writes what its prefix would give
@@ -735,7 +755,7 @@ template <class E, int D, int WAYS> __global__ __launch_bounds__(256) void kv_jo
 #pragma unroll
     for (int n = 0; n < PER_LANE; ++n) {
         const bool none = no_key(ml[n].x, ml[n].y);
-        keep[n] = none ? -1.f : rescale(ml[n].x, top);
+        keep[n] = none ? -1.f : rescale(ml[n].x, top, a.scale);
         sum += none ? 0.f : ml[n].y * keep[n];
     }
 #pragma unroll
@@ -766,7 +786,7 @@ template <class E, int D, int WAYS> __global__ __launch_bounds__(256) void kv_jo
     const float inv = no_key(top, sum) ? 0.f : 1.f / sum;
     const int token = row / a.heads, head = row - token * a.heads;
     *reinterpret_cast<x4*>(a.out + ((long)(r.q0 + token) * a.o_ts + (long)head * a.o_hs + 4 * l) * 2) = x4{(E)(o.x * inv), (E)(o.y * inv), (E)(o.z * inv), (E)(o.w * inv)};
-    if (a.lse && l == 0) a.lse[at] = log_sum(top, sum);
+    if (a.lse && l == 0) a.lse[at] = log_sum(top, sum, a.scale);
 }
 
 template <class E, int D, bool PAGED> static void launch_kv(const KvArgs& a, hipStream_t s) {
@@ -855,7 +875,7 @@ static bool refuse_sizes(const bb_attention_args* x) {
 }
 static bool plan(KvArgs& a, const bb_attention_args* x, const KvPlan* given = nullptr) {
     a.n_seq = (int)x->sequences; a.q_tokens = (int)x->q_tokens; a.k_tokens = (int)x->k_tokens; a.heads = (int)x->heads; a.kv_heads = (int)x->kv_heads; a.each = a.heads / a.kv_heads;
-    a.block = (int)x->block; a.scale = (float)x->scale * 1.44269504089f;
+    a.block = (int)x->block; a.scale = (float)x->scale * 1.44269504089f; a.lag = KV_LAG / a.scale;
     return plan_parts(a, x->k_tokens / x->sequences, 0, (int)x->head_dim, given);
 }
 extern "C" size_t bb_attention_workspace_bytes(const bb_attention_args* x) {
@@ -886,7 +906,7 @@ static bool refuse_sizes(const bb_shared_attention_args* x) {
 }
 static bool plan(KvArgs& a, const bb_shared_attention_args* x, const KvPlan* given = nullptr) {
     a.n_seq = (int)x->branches; a.q_tokens = (int)x->q_tokens; a.heads = (int)x->heads; a.kv_heads = (int)x->kv_heads; a.each = a.heads / a.kv_heads;
-    a.block = (int)x->block; a.scale = (float)x->scale * 1.44269504089f;
+    a.block = (int)x->block; a.scale = (float)x->scale * 1.44269504089f; a.lag = KV_LAG / a.scale;
     a.own_width = (int)x->own_width; a.n_groups = (int)x->groups; a.prefix_width = x->groups ? (int)x->prefix_width : 0;
     return plan_parts(a, 64L * a.own_width, 64L * a.prefix_width, (int)x->head_dim, given);
 }
