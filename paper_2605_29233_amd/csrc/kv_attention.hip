@@ -801,10 +801,13 @@ template <bool PAGED> static void launch_kv(const KvArgs& a, int type, int head_
     else head_dim == 128 ? launch_kv<half_t, 128, PAGED>(a, s) : launch_kv<half_t, 64, PAGED>(a, s);
 }
 
-static bool refuse_attention(long q_tokens, long n_seq, long heads, long kv_heads, long head_dim, long type, long block, double scale) {
+// What a plan, and with it the size of a workspace, depends on.
+static bool refuse_common_sizes(long q_tokens, long n_seq, long heads, long kv_heads, long head_dim, long type) {
     return (type != BB_BF16 && type != BB_F16) || (head_dim != 64 && head_dim != 128) || q_tokens < 0 || q_tokens > BB_MAX_TOKENS || n_seq < 0 || n_seq > BB_MAX_TOKENS || heads < 1 ||
-           heads > BB_MAX_HEADS || kv_heads < 1 || heads % kv_heads || q_tokens * heads > 1L << 30 || block < 0 || block > 0x7FFFFFFF || !((float)scale > 0) || !((float)scale * 1.45f < INFINITY);
+           heads > BB_MAX_HEADS || kv_heads < 1 || heads % kv_heads || q_tokens * heads > 1L << 30;
 }
+// What it does not.
+static bool refuse_mask(long block, double scale) { return block < 0 || block > 0x7FFFFFFF || !((float)scale > 0) || !((float)scale * 1.45f < INFINITY); }
 // A plan: halves of a workgroup, parts of a branch's keys, of a group's prefix (0: taken by the branches before their own).
 struct KvPlan { int halves, own_parts, prefix_parts; };
 // How many row tiles there can be, whatever the lengths, and how their keys are shared out: into how many parts, to one or two halves of a workgroup, and whether a prefix is taken once
@@ -871,7 +874,7 @@ static bool far_rows(long ts) { return ts > 1 << 23; }
 static bool refuse_ints(const void* p) { return !p || (uintptr_t)p % 4; }
 
 static bool refuse_sizes(const bb_attention_args* x) {
-    return !x || refuse_attention(x->q_tokens, x->sequences, x->heads, x->kv_heads, x->head_dim, x->type, x->block, x->scale) || x->k_tokens < 0 || x->k_tokens > BB_MAX_TOKENS;
+    return !x || refuse_common_sizes(x->q_tokens, x->sequences, x->heads, x->kv_heads, x->head_dim, x->type) || x->k_tokens < 0 || x->k_tokens > BB_MAX_TOKENS;
 }
 static bool plan(KvArgs& a, const bb_attention_args* x, const KvPlan* given = nullptr) {
     a.n_seq = (int)x->sequences; a.q_tokens = (int)x->q_tokens; a.k_tokens = (int)x->k_tokens; a.heads = (int)x->heads; a.kv_heads = (int)x->kv_heads; a.each = a.heads / a.kv_heads;
@@ -883,7 +886,7 @@ extern "C" size_t bb_attention_workspace_bytes(const bb_attention_args* x) {
     return refuse_sizes(x) || x->q_tokens == 0 || x->sequences == 0 || !plan(a, x) ? 0 : parts_bytes(a, (int)x->head_dim);
 }
 static int attention(const bb_attention_args* x, const KvPlan* given, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
-    if (refuse_sizes(x)) return BB_EINVAL;
+    if (refuse_sizes(x) || refuse_mask(x->block, x->scale)) return BB_EINVAL;
     if (x->q_tokens == 0 || x->sequences == 0) return BB_OK;
     if (refuse_ints(x->q_starts) || refuse_ints(x->k_starts) || (uintptr_t)x->lse % 4) return BB_EINVAL;
     const int heads = (int)x->heads, kv_heads = (int)x->kv_heads, dim = (int)x->head_dim;
@@ -901,7 +904,7 @@ static int attention(const bb_attention_args* x, const KvPlan* given, void* work
 }
 
 static bool refuse_sizes(const bb_shared_attention_args* x) {
-    return !x || refuse_attention(x->q_tokens, x->branches, x->heads, x->kv_heads, x->head_dim, x->type, x->block, x->scale) || x->groups < 0 || x->groups > BB_MAX_TOKENS ||
+    return !x || refuse_common_sizes(x->q_tokens, x->branches, x->heads, x->kv_heads, x->head_dim, x->type) || x->groups < 0 || x->groups > BB_MAX_TOKENS ||
            x->own_width < 0 || x->own_width > KV_MOST_COLUMNS || (x->groups > 0 && (x->prefix_width < 0 || x->prefix_width > KV_MOST_COLUMNS));
 }
 static bool plan(KvArgs& a, const bb_shared_attention_args* x, const KvPlan* given = nullptr) {
@@ -915,7 +918,7 @@ extern "C" size_t bb_shared_attention_workspace_bytes(const bb_shared_attention_
     return refuse_sizes(x) || x->q_tokens == 0 || x->branches == 0 || !plan(a, x) ? 0 : parts_bytes(a, (int)x->head_dim);
 }
 static int shared_attention(const bb_shared_attention_args* x, const KvPlan* given, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
-    if (refuse_sizes(x) || x->pages < 1 || x->pages > BB_MAX_PAGES || (x->branches > 1 && x->own_ld < 0) || (x->groups > 1 && x->prefix_ld < 0) ||
+    if (refuse_sizes(x) || refuse_mask(x->block, x->scale) || x->pages < 1 || x->pages > BB_MAX_PAGES || (x->branches > 1 && x->own_ld < 0) || (x->groups > 1 && x->prefix_ld < 0) ||
         x->own_ld > HEADS_MAX_STRIDE || (x->groups > 0 && x->prefix_ld > HEADS_MAX_STRIDE)) return BB_EINVAL;
     if (x->q_tokens == 0 || x->branches == 0) return BB_OK;
     if (refuse_ints(x->q_starts) || refuse_ints(x->own_lens) || (x->own_width > 0 && refuse_ints(x->own_pages)) || (uintptr_t)x->lse % 4) return BB_EINVAL;
