@@ -182,17 +182,18 @@ def gemm_int8_plan(M, N, K):
 # ---- 8-bit integer operators --------------------------------------------------------------------
 # (what these calls do on the host counts where a kernel takes a few microseconds: no objects made, nothing looked up twice)
 _TYPES = {}             # torch dtype -> BB_F32, BB_BF16, BB_F16
-_torch = _here = _raw_stream = _I8 = _I32 = _F32 = _F64 = None
+_torch = _here = _raw_stream = _I8 = _I32 = _F32 = _F64 = _grads = _written = None
 
 
 def _ready():
     """What the calls below use of torch (imported with the first of them)."""
-    global _torch, _here, _raw_stream, _I8, _I32, _F32, _F64
+    global _torch, _here, _raw_stream, _I8, _I32, _F32, _F64, _grads, _written
     import torch
     load_library()
     _TYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
     _I8, _I32, _F32, _F64, _here = torch.int8, torch.int32, torch.float32, torch.float64, torch.cuda.current_device
     _raw_stream = torch._C._cuda_getCurrentRawStream        # (torch.cuda.current_stream without its 2 us)
+    _grads, _written = torch.is_grad_enabled, torch.autograd.graph.increment_version
     _torch = torch
 
 
@@ -362,6 +363,12 @@ ATTENTION_ARGS = struct.Struct("9q2q8qd3qq")
 SHARED_ATTENTION_ARGS = struct.Struct("6q9q4q6q5qd3qq")
 
 
+# None of them has a backward pass.  Tensors that require a gradient are refused while gradients are recorded; what a call writes gets another version, as by torch's own operators, so that autograd
+# finds out if it has kept the rows from before.
+def _recorded(what):
+    raise BBError(f"{what} requires a gradient, and this call has no backward pass: call it under torch.no_grad() or with {what}.detach()")
+
+
 def _heads(t, what, dtype, shape, index):
     """Address and strides (between tokens, between heads) of rows of heads [tokens][heads][dim] on GPU `index`."""
     if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
@@ -369,6 +376,8 @@ def _heads(t, what, dtype, shape, index):
     ts, hs, step = t.stride()
     if step != 1 and shape[2] > 1:
         raise BBError(f"{what}: the elements of a head must be contiguous")
+    if t.requires_grad and _grads():
+        _recorded(what)
     return t.data_ptr(), ts, hs
 
 
@@ -379,6 +388,8 @@ def _cache(t, what, dtype, shape, index):
     ps, hs, ts, step = t.stride()
     if step != 1 and shape[3] > 1:
         raise BBError(f"{what}: the elements of a head must be contiguous")
+    if t.requires_grad and _grads():
+        _recorded(what)
     return t.data_ptr(), ps, hs, ts
 
 
@@ -386,6 +397,8 @@ def _ints(t, what, n, index, dtype=None):
     """Address of a contiguous vector of n elements."""
     if t.dtype is not (dtype or _I32) or t.shape != (n,) or t.get_device() != index or not t.is_contiguous():
         raise BBError(f"{what}: expected contiguous {dtype or _I32} ({n},) on cuda:{index}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.requires_grad and _grads():        # (frequencies)
+        _recorded(what)
     return t.data_ptr()
 
 
@@ -427,7 +440,7 @@ def _three(t, what):
 def rope(q, k, positions, freqs, interleaved=False, magnitude=1.0, q_out=None, k_out=None, stream=None):
     """bb_rope on torch CUDA tensors: q [tokens][heads][dim] and k [tokens][kv heads][dim] (None: no keys) fp32, bf16 or fp16 turned by positions (int32 [tokens]) *
     freqs (fp64 [rot / 2], see rope_frequencies; the heads' first rot elements); written to q_out and k_out (default: in place).  Returns (q_out, k_out).
-    Stream as in quantize_rows."""
+    Stream as in quantize_rows.  No backward pass: tensors that require a gradient are refused unless gradients are off."""
     if _torch is None:
         _ready()
     dev = q.get_device()
@@ -458,12 +471,14 @@ def rope(q, k, positions, freqs, interleaved=False, magnitude=1.0, q_out=None, k
     rc = _LIB.bb_rope(args, _raw_stream(dev))
     if rc:
         _done(rc, "bb_rope")
+    _written(q_out if k is None else (q_out, k_out))
     return q_out, k_out
 
 
 def rope_append(q, k, v, positions, freqs, k_cache, v_cache, slots, interleaved=False, magnitude=1.0, q_out=None, stream=None):
     """bb_rope_append: q turned into q_out (default: in place) as by rope, the turned k and v written to k_cache and v_cache [pages][kv heads][PAGE_TOKENS][dim] at
-    slots (int32 [tokens], page * PAGE_TOKENS + token in the page; a negative one keeps its token out).  Returns q_out.  Stream as in quantize_rows."""
+    slots (int32 [tokens], page * PAGE_TOKENS + token in the page; a negative one keeps its token out).  Returns q_out.  Stream as in quantize_rows,
+    gradients as in rope."""
     if _torch is None:
         _ready()
     dev = q.get_device()
@@ -488,6 +503,7 @@ def rope_append(q, k, v, positions, freqs, k_cache, v_cache, slots, interleaved=
     rc = _LIB.bb_rope_append(args, _raw_stream(dev))
     if rc:
         _done(rc, "bb_rope_append")
+    _written((q_out, k_cache, v_cache))
     return q_out
 
 
@@ -499,6 +515,8 @@ def _attention_outputs(q, shape, out, lse, dev):
     if lse is not None:
         if lse.dtype is not _F32 or lse.shape != shape[:2] or lse.get_device() != dev or not lse.is_contiguous():
             raise BBError(f"lse: expected contiguous torch.float32 {tuple(shape[:2])} on cuda:{dev}, got {lse.dtype} {tuple(lse.shape)} on {lse.device}")
+        if lse.requires_grad and _grads():
+            _recorded("lse")
         pl = lse.data_ptr()
     return out, (*_heads(out, "out", q.dtype, shape, dev), pl)
 
@@ -521,7 +539,7 @@ def attention(q, k, v, q_starts, k_starts=None, block=0, scale=None, out=None, l
     """bb_attention on torch CUDA tensors: packed sequences of queries [tokens][heads][dim] on keys and values [tokens][kv heads][dim], bf16 or fp16; sequence s is
     rows q_starts[s] .. q_starts[s + 1] - 1 of q and k_starts[s] .. (default: the same) of k and v (int32 [sequences + 1]).  block 0: every query sees all its keys, 1: causal, b:
     keys before the end of its own block of b.  scale: default dim^-0.5.  Written to out [tokens][heads][dim] (made here where not given) and lse (fp32 [tokens][heads], where
-    given); returns out.  Stream as in quantize_rows; a workspace, where the call needs one, is allocated on it for this call alone."""
+    given); returns out.  Stream as in quantize_rows; a workspace, where the call needs one, is allocated on it for this call alone.  Gradients as in rope."""
     if _torch is None:
         _ready()
     dev = q.get_device()
@@ -541,6 +559,7 @@ def attention(q, k, v, q_starts, k_starts=None, block=0, scale=None, out=None, l
     except struct.error:
         raise BBError(_NUMBERS.format(block, scale)) from None
     _attend(_LIB.bb_attention, _LIB.bb_attention_workspace_bytes, args, dev, "bb_attention")
+    _written(out if lse is None else (out, lse))
     return out
 
 
@@ -549,7 +568,7 @@ def shared_attention(q, q_starts, k_cache, v_cache, own_pages, own_lens, prefix_
     """bb_shared_attention: queries [tokens][heads][dim] of branches (branch b: rows q_starts[b] .. q_starts[b + 1] - 1) over caches [pages][kv heads][PAGE_TOKENS][dim]:
     the prefix of the branch's group (branches group_starts[g] .. group_starts[g + 1] - 1; prefix_lens[g] keys in the pages prefix_pages[g]), read once for all of
     them, and the branch's own_lens[b] keys in the pages own_pages[b].  Tables, lengths and starts are int32 tensors of the device; without a prefix it is plain attention over pages.
-    block, scale, out, lse, stream and workspace as in attention (block counts from the first own key)."""
+    block, scale, out, lse, stream, workspace and gradients as in attention (block counts from the first own key)."""
     if _torch is None:
         _ready()
     dev = q.get_device()
@@ -582,6 +601,7 @@ def shared_attention(q, q_starts, k_cache, v_cache, own_pages, own_lens, prefix_
     except struct.error:
         raise BBError(_NUMBERS.format(block, scale)) from None
     _attend(_LIB.bb_shared_attention, _LIB.bb_shared_attention_workspace_bytes, args, dev, "bb_shared_attention")
+    _written(out if lse is None else (out, lse))
     return out
 
 

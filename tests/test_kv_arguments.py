@@ -25,3 +25,60 @@ def test_workspace_bytes_look_at_sizes_alone(struct, good, size):
         assert size(struct.pack(*dict(good, **other).values())) == need, other
     for bad in (dict(n=-1), dict(qn=-1), dict(heads=3), dict(heads=0), dict(kv=0), dict(dim=96), dict(type=0), dict(type=7)):
         assert size(struct.pack(*dict(good, **bad).values())) == 0, bad
+
+
+def operands():
+    """Of every operator around K,V: (call, its float inputs, its outputs), by names of the call's arguments."""
+    def x(seed, *shape):
+        return rnd(seed, *shape).to(DEV)
+
+    pos, f, s = ints([1, 2, 3]).to(DEV), bb.rope_frequencies(64, device=DEV), starts([3]).to(DEV)
+    table, lens, slots = ints([[1]]).to(DEV), ints([3]).to(DEV), ints([5, 6, 7]).to(DEV)
+    return [
+        (bb.rope, dict(positions=pos, freqs=f), dict(q=x(1, 3, 4, 64), k=x(2, 3, 2, 64)), dict(q_out=x(3, 3, 4, 64), k_out=x(4, 3, 2, 64))),
+        (bb.rope_append, dict(positions=pos, freqs=f, slots=slots), dict(q=x(1, 3, 4, 64), k=x(2, 3, 2, 64), v=x(5, 3, 2, 64)),
+         dict(k_cache=x(6, 2, 2, PAGE, 64), v_cache=x(7, 2, 2, PAGE, 64), q_out=x(3, 3, 4, 64))),
+        (bb.attention, dict(q_starts=s), dict(q=x(1, 3, 4, 64), k=x(2, 3, 2, 64), v=x(5, 3, 2, 64)), dict(out=x(3, 3, 4, 64), lse=torch.zeros(3, 4, device=DEV))),
+        (bb.shared_attention, dict(q_starts=s, own_pages=table, own_lens=lens), dict(q=x(1, 3, 4, 64), k_cache=x(6, 2, 2, PAGE, 64), v_cache=x(7, 2, 2, PAGE, 64)),
+         dict(out=x(3, 3, 4, 64), lse=torch.zeros(3, 4, device=DEV))),
+    ]
+
+
+@pytest.mark.gpu
+def test_tensors_that_require_a_gradient_are_refused():
+    """There is no backward pass: with gradients recorded such a tensor, read or written, is refused and stays as it is; without, or detached, the call runs."""
+    for call, others, inputs, outputs in operands():
+        for name, t in {**inputs, **outputs}.items():
+            leaf = t.clone().requires_grad_()
+            for graded in (leaf, leaf * 1):             # (one that autograd would refuse to overwrite, and one that it would let be)
+                args = {**others, **inputs, **outputs, name: graded}
+                before = [a.detach().clone() for a in (*inputs.values(), *outputs.values())]
+                with pytest.raises(BBError, match=f"{name}.*gradient"):
+                    call(**args)
+                assert all(torch.equal(a, b) for a, b in zip((*inputs.values(), *outputs.values()), before))
+                with torch.no_grad():
+                    call(**args)
+            call(**{**others, **inputs, **outputs, name: leaf.detach()})
+
+
+@pytest.mark.gpu
+def test_outputs_count_as_written():
+    """What a call writes has another version afterwards, in place or not, so that autograd finds a tensor changed that it kept; what it reads has not.  Inference tensors, which have none, are taken too."""
+    for call, others, inputs, outputs in operands():
+        seen = {n: t._version for n, t in {**inputs, **outputs}.items()}
+        call(**others, **inputs, **outputs)
+        assert all(t._version == seen[n] for n, t in inputs.items())
+        assert all(t._version > seen[n] for n, t in outputs.items())
+        with torch.inference_mode():
+            call(**others, **inputs, **{n: t.clone() for n, t in outputs.items()})
+    call, others, inputs, _ = operands()[0]
+    q, k = (inputs[n].float() for n in "qk")
+    seen = q._version, k._version
+    call(q, k, **others)
+    assert q._version > seen[0] and k._version > seen[1]
+    # a product that has kept q: its gradient would be taken with the turned rows
+    w = torch.ones_like(q, requires_grad=True)
+    y = (q * w).sum()
+    call(q, None, **others)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
