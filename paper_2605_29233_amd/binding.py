@@ -466,7 +466,7 @@ def rope(q, k, positions, freqs, interleaved=False, magnitude=1.0, q_out=None, k
             _ints(freqs, "freqs", half, dev, _F64), 2 * half)
     try:
         args = ROPE_ARGS.pack(*rows, interleaved, magnitude, tokens, dim, _type(dtype, "q"))
-    except struct.error:
+    except (struct.error, OverflowError):
         raise BBError(_TURN.format(interleaved, magnitude)) from None
     rc = _LIB.bb_rope(args, _raw_stream(dev))
     if rc:
@@ -498,7 +498,7 @@ def rope_append(q, k, v, positions, freqs, k_cache, v_cache, slots, interleaved=
     places = (_ints(slots, "slots", tokens, dev), *_cache(k_cache, "k_cache", dtype, cache, dev), *_cache(v_cache, "v_cache", dtype, cache, dev), pages)
     try:
         args = ROPE_APPEND_ARGS.pack(*rows, interleaved, magnitude, *places, tokens, dim, _type(dtype, "q"))
-    except struct.error:
+    except (struct.error, OverflowError):
         raise BBError(_TURN.format(interleaved, magnitude)) from None
     rc = _LIB.bb_rope_append(args, _raw_stream(dev))
     if rc:
@@ -555,8 +555,8 @@ def attention(q, k, v, q_starts, k_starts=None, block=0, scale=None, out=None, l
     ks = qs if k_starts is None else _ints(k_starts, "k_starts", n, dev)
     heads_of = (*_heads(q, "q", dtype, shape, dev), *_heads(k, "k", dtype, kv, dev), *_heads(v, "v", dtype, kv, dev))
     try:
-        args = ATTENTION_ARGS.pack(*heads_of, qs, ks, n - 1, tokens, kv[0], heads, kv[1], dim, _type(dtype, "q"), block, dim ** -0.5 if scale is None else scale, *outs)
-    except struct.error:
+        args = ATTENTION_ARGS.pack(*heads_of, qs, ks, n - 1, tokens, kv[0], heads, kv[1], dim, _type(dtype, "q"), block, (dim and dim ** -0.5) if scale is None else scale, *outs)
+    except (struct.error, OverflowError):
         raise BBError(_NUMBERS.format(block, scale)) from None
     _attend(_LIB.bb_attention, _LIB.bb_attention_workspace_bytes, args, dev, "bb_attention")
     _written(out if lse is None else (out, lse))
@@ -597,8 +597,8 @@ def shared_attention(q, q_starts, k_cache, v_cache, own_pages, own_lens, prefix_
     branches = (*_heads(q, "q", dtype, shape, dev), qs, n, tokens, *_cache(k_cache, "k_cache", dtype, cache, dev), *_cache(v_cache, "v_cache", dtype, cache, dev), cache[0],
                 *_table(own_pages, "own_pages", n, dev), _ints(own_lens, "own_lens", n, dev), *prefix)
     try:
-        args = SHARED_ATTENTION_ARGS.pack(*branches, heads, cache[1], dim, _type(dtype, "q"), block, dim ** -0.5 if scale is None else scale, *outs)
-    except struct.error:
+        args = SHARED_ATTENTION_ARGS.pack(*branches, heads, cache[1], dim, _type(dtype, "q"), block, (dim and dim ** -0.5) if scale is None else scale, *outs)
+    except (struct.error, OverflowError):
         raise BBError(_NUMBERS.format(block, scale)) from None
     _attend(_LIB.bb_shared_attention, _LIB.bb_shared_attention_workspace_bytes, args, dev, "bb_shared_attention")
     _written(out if lse is None else (out, lse))

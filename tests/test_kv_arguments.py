@@ -82,3 +82,17 @@ def test_outputs_count_as_written():
     call(q, None, **others)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.backward()
+
+
+@pytest.mark.gpu
+def test_head_of_no_elements_and_numbers_that_no_field_holds():
+    x, s = rnd(1, 3, 4, 64).to(DEV), starts([3]).to(DEV)
+    c, table, lens = rnd(2, 2, 4, PAGE, 64).to(DEV), ints([[1]]).to(DEV), ints([3]).to(DEV)
+    pos, f = ints([1, 2, 3]).to(DEV), bb.rope_frequencies(64, device=DEV)
+    e, ec = x[:, :, :0], c[:, :, :, :0]
+    huge = 10 ** 400
+    for call in (lambda: bb.attention(e, e, e, s), lambda: bb.shared_attention(e, s, ec, ec, table, lens), lambda: bb.attention(x, x, x, s, scale=huge),
+                 lambda: bb.shared_attention(x, s, c, c, table, lens, scale=huge), lambda: bb.rope(x.clone(), None, pos, f, magnitude=huge),
+                 lambda: bb.rope_append(x.clone(), x, x, pos, f, c.clone(), c.clone(), pos, magnitude=huge), lambda: bb.rope(e, None, pos, f[:0])):
+        with pytest.raises(BBError):
+            call()
