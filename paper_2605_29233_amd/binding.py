@@ -341,14 +341,15 @@ def gemm_int8(a, a_scale, w, w_scale, bias=None, out=None, dtype=None, stream=No
 
 # ---- operators around K,V ------------------------------------------------------------------------
 PAGE_TOKENS = 64
+MAX_ROT = 1024          # (the C entry takes an int, which ctypes would cut a larger number down to)
 
 
 def rope_frequencies(rot, base=10000.0, factor=1.0, context=0, low=1.0, high=4.0, device="cuda:0"):
     """bb_rope_frequencies as a tensor of `device`: fp64 [rot / 2], base^(-2 j / rot), scaled for contexts `factor` times as long: all divided by it, or, of a
     model trained on `context` tokens, those that turn at most `low` times over it, those that turn `high` times or more not at all."""
     import torch
-    if rot < 2 or rot % 2:
-        raise BBError(f"rot: expected an even number of elements, at least 2, got {rot}")
+    if rot < 2 or rot % 2 or rot > MAX_ROT:
+        raise BBError(f"rot: expected an even number of elements, 2 .. {MAX_ROT}, got {rot}")
     f = torch.empty(rot // 2, dtype=torch.float64)
     rc = load_library().bb_rope_frequencies(f.data_ptr(), int(rot), float(base), float(factor), float(context), float(low), float(high))
     if rc:

@@ -96,3 +96,10 @@ def test_head_of_no_elements_and_numbers_that_no_field_holds():
                  lambda: bb.rope_append(x.clone(), x, x, pos, f, c.clone(), c.clone(), pos, magnitude=huge), lambda: bb.rope(e, None, pos, f[:0])):
         with pytest.raises(BBError):
             call()
+
+
+def test_frequencies_of_more_pairs_than_a_head_has():
+    """2^32 + 64 elements are not 64 (the C entry's int)."""
+    for rot in (2 ** 32 + 64, 1026, 2 ** 80):
+        with pytest.raises(BBError):
+            bb.rope_frequencies(rot, device="cpu")
