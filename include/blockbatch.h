@@ -388,7 +388,9 @@ int bb_rope_append(const bb_rope_append_args* args_host, void* hip_stream);
  * differ in their last places between calls of other sizes, as its keys are summed in other parts.
  * type BB_BF16 or BB_F16; head_dim 64 or 128; scale > 0; q_tokens * heads at most 2^30, q_tokens * heads / 128 + kv_heads * sequences
  * below 2^24; all pointers of heads 16-byte aligned and their strides multiples of 8 elements, those between tokens of k and v at most 2^23.
- * NaN and infinities in keys and values that a query does not see do not reach it.
+ * NaN and infinities in keys and values that a query does not see do not reach it; an infinite value that it sees gives
+ * an infinity, or a NaN where its weight is too small for the operands' type.  Outputs are summed in fp32 before they are divided, with weights of up to 2^8: bf16 values are to stay below 2^120 / keys in magnitude
+ * (fp16 values always do), finite ones beyond may give an infinity.
  * workspace_dev: at least bb_attention_workspace_bytes() of the same sizes (it looks at no pointer, stride, block or scale), 256-byte aligned (may be NULL if that is 0), used by this call
  * alone until its work is done. */
 typedef struct {

@@ -97,3 +97,20 @@ def test_large_operands_pick_the_largest(n, dtype):
         assert torch.equal(out.cpu()[clear], v[best.indices[:, 0]][clear])
         assert ((lse.cpu()[:, 0].double() - best.values[:, 0] * 0.125).abs() <= off * 0.125 + 2.0 ** -21 * best.values[:, 0].abs())[clear].all()
     assert seen > 10 * n
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [5, 60])
+def test_values_up_to_the_documented_limit(n):
+    """bf16 values just below 2^120 / keys, on scores that the running maximum does not follow (weights of 2^7.93): their mean, not an infinity."""
+    keys, dim, t = 256, 64, torch.bfloat16
+    q, k = torch.zeros(n, 1, dim, dtype=t), torch.zeros(keys, 1, dim, dtype=t)
+    q[:, :, 0], k[64:, :, 0] = 1, 44                    # (44 / 8 log2(e) = 7.93)
+    v = (rnd(1, keys, 1, dim).double().abs().clamp(0.25, 1.0) * 2.0 ** 112 * (1 - 2.0 ** -8)).to(t)
+    assert float(v.double().max()) < 2.0 ** 120 / keys
+    s = (q[:, 0].double() @ k[:, 0].double().t()) * 0.125
+    want = weighed(s, v[:, 0].double(), t)
+    for halves in (1, 2):
+        for parts in (1, 2, 4):
+            got = run_plan(q, k, v, [n], [keys], 0, halves, parts)
+            check(*got, want, t)
