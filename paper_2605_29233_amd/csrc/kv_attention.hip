@@ -325,13 +325,18 @@ template <int D, int NK, bool PART> static __device__ __forceinline__ void follo
     by = scale;
     if (__ballot(best > r.bar)) {
         const float to = best > r.bar ? fmaxf(best, r.top) : r.top;
-        // (not quite 0: an infinity in the output stays one)
-        const float keep = fmaxf(__builtin_amdgcn_exp2f((r.top - to) * scale), 1.2e-38f);
-        r.sum *= keep;
+        // by 2^126 at most at a time (twice where it is more), so that an infinity in the output stays one
+        const float power = (r.top - to) * scale;
+        auto scale_by = [&](float keep) {
+            r.sum *= keep;
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t)
+            for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) r.o[t][e] *= keep;
+                for (int e = 0; e < 16; ++e) r.o[t][e] *= keep;
+        };
+        const bool more = power < -126.f && r.sum > 0.f;
+        scale_by(__builtin_amdgcn_exp2f(fmaxf(power, -126.f)));
+        if (__ballot(more)) scale_by(__builtin_amdgcn_exp2f(more ? fmaxf(power + 126.f, -126.f) : 0.f));
         const bool none = to == -INFINITY, large = !none && fabsf(to * scale) >= KV_LARGE;
         r.top = to;
         r.from = none || large ? 0.f : to * scale;

@@ -114,3 +114,23 @@ def test_values_up_to_the_documented_limit(n):
         for parts in (1, 2, 4):
             got = run_plan(q, k, v, [n], [keys], 0, halves, parts)
             check(*got, want, t)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [5, 60])
+@pytest.mark.parametrize("rise", [680, 1112, 2048])
+def test_large_values_that_later_scores_leave_behind(n, rise):
+    """64 values of 2^113 (below 2^120 / keys), then one key whose score is 2^122 to 2^369 of weight higher, of value 2^-20: nothing of the first is left but what its weight gives (at 2^-126, 2^-7 of them would)."""
+    keys, dim, t = 65, 64, torch.bfloat16
+    q, k = torch.zeros(n, 1, dim, dtype=t), torch.zeros(keys, 1, dim, dtype=t)
+    q[:, :, 0], k[64, :, 0] = 1, rise
+    v = torch.full((keys, 1, dim), 2.0 ** -20, dtype=t)
+    v[:64] = 2.0 ** 113
+    s = (q[:, 0].double() @ k[:, 0].double().t()) * 0.125
+    want = weighed(s, v[:, 0].double(), t)
+    for halves in (1, 2):
+        for parts in (1, 2):
+            check(*run_plan(q, k, v, [n], [keys], 0, halves, parts), want, t)
+    v[3, 0, 7] = float("inf")
+    out, _ = run_plan(q, k, v, [n], [keys], 0, 1, 1)
+    assert not torch.isfinite(out[:, :, 7]).any() and torch.isfinite(out[:, :, :7]).all()
