@@ -336,11 +336,13 @@ int bb_debug_panel_quantize(const float* x_dev, int rows, int cols, void* panel_
 /* ---- operators around K,V ------------------------------------------------------------------------------
  * Rotary positions, attention over packed prompts, attention of branches that share a prefix over a paged cache.  As with the 8-bit operators no context is
  * needed, all work is enqueued on hip_stream (of the current device), nothing is allocated, memset or synchronised, and every call may be captured into a
- * graph.  Arguments come in a struct that the call reads before it returns; the pointers in it are device memory.  Malformed arguments: BB_EINVAL; too little workspace: BB_ENOMEM; a HIP error: BB_EHIP.
+ * graph.  Arguments come in a struct that the call reads before it returns; the pointers in it are device memory.  Malformed arguments: BB_EINVAL; too little workspace:
+ * BB_ENOMEM; a HIP error: BB_EHIP.
  *
  * Rows of heads: element d of head h of token t lies at data[t * x_token + h * x_head + d]; strides in elements, not negative (that over a single token or head is
  * ignored).  Strides of an output are such that no element lies twice (the larger at least what the smaller spans), and it shares no element with another tensor of the
- * call: it lies apart from it, or both are column ranges of rows at one distance (the parts of one projection's output); anything else is refused.
+ * call: it lies apart from it, or both are column ranges of token rows at one distance (the parts of one projection's output); anything else is refused, among it caches of keys and of values whose
+ * pages take turns in one allocation (either's pages in one run each are fine).
  * A cache is pages of BB_PAGE_TOKENS tokens: element d of token t of page p and kv head h at data[p * x_page + h * x_head + t * x_token + d].
  *
  * What stands on the device (starts, lengths, page tables, slots) is read by the kernels and may change between a graph's replays; values that
@@ -388,9 +390,9 @@ int bb_rope_append(const bb_rope_append_args* args_host, void* hip_stream);
  * differ in their last places between calls of other sizes, as its keys are summed in other parts.
  * type BB_BF16 or BB_F16; head_dim 64 or 128; scale > 0; q_tokens * heads at most 2^30, q_tokens * heads / 128 + kv_heads * sequences
  * below 2^24; all pointers of heads 16-byte aligned and their strides multiples of 8 elements, those between tokens of k and v at most 2^23.
- * NaN and infinities in keys and values that a query does not see do not reach it; an infinite value that it sees gives
- * an infinity, or a NaN where its weight is too small for the operands' type.  Outputs are summed in fp32 before they are divided, with weights of up to 2^8: bf16 values are to stay below 2^120 / keys in magnitude
- * (fp16 values always do), finite ones beyond may give an infinity.
+ * NaN and infinities in keys and values that a query does not see do not reach it; an infinite value that it sees gives an infinity, or a NaN where
+ * its weight is too small for the operands' type.  Scores may have any size that fp32 holds; weights below 2^-126 count as none.  Outputs are summed in fp32 before they are divided, with weights of
+ * up to 2^8: bf16 values are to stay below 2^120 / keys in magnitude (fp16 values always do), finite ones beyond may give an infinity.
  * workspace_dev: at least bb_attention_workspace_bytes() of the same sizes (it looks at no pointer, stride, block or scale), 256-byte aligned (may be NULL if that is 0), used by this call
  * alone until its work is done. */
 typedef struct {
@@ -405,7 +407,8 @@ int bb_attention(const bb_attention_args* args_host, void* workspace_dev, size_t
 /* Attention of branches over a paged cache, the prefix that a group of them shares read once for all.  Branch b has the queries q_starts[b] .. q_starts[b + 1] - 1, own_lens[b]
  * keys of its own in the pages own_pages[b * own_ld + 0 ..] and belongs to group g if group_starts[g] <= b < group_starts[g + 1]; the group's prefix is prefix_lens[g] keys in the
  * pages prefix_pages[g * prefix_ld + 0 ..].  A query sees its whole prefix, and of its branch's m own keys those that bb_attention describes (block counted from the
- * first own key).  own_width, prefix_width: columns of the tables (at most BB_MAX_TOKENS / BB_PAGE_TOKENS), at most that many pages count.  groups == 0: no prefix (pointers ignored): plain attention over pages.
+ * first own key).  own_width, prefix_width: columns of the tables (at most BB_MAX_TOKENS / BB_PAGE_TOKENS), at most that many pages count, and
+ * work is shared out for lengths of that many pages: columns that no length reaches cost time (own_ld, prefix_ld may be larger).  groups == 0: no prefix (pointers ignored): plain attention over pages.
  * Both lengths may end inside a page; what lies behind them is not read.  Branches outside every group have no prefix; starts and group_starts ascend.  The rest as in bb_attention. */
 typedef struct {
     const void* q; long q_token, q_head; const int32_t* q_starts; long branches, q_tokens;

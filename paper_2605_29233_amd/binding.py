@@ -539,8 +539,8 @@ def _attend(call, workspace_bytes, args, dev, what):
 def attention(q, k, v, q_starts, k_starts=None, block=0, scale=None, out=None, lse=None, stream=None):
     """bb_attention on torch CUDA tensors: packed sequences of queries [tokens][heads][dim] on keys and values [tokens][kv heads][dim], bf16 or fp16; sequence s is
     rows q_starts[s] .. q_starts[s + 1] - 1 of q and k_starts[s] .. (default: the same) of k and v (int32 [sequences + 1]).  block 0: every query sees all its keys, 1: causal, b:
-    keys before the end of its own block of b.  scale: default dim^-0.5.  Written to out [tokens][heads][dim] (made here where not given) and lse (fp32 [tokens][heads], where
-    given); returns out.  Stream as in quantize_rows; a workspace, where the call needs one, is allocated on it for this call alone.  Gradients as in rope."""
+    keys before the end of its own block of b.  scale: default dim^-0.5.  Written to out [tokens][heads][dim] (made here where not given: rows of no sequence then hold
+    anything) and lse (fp32 [tokens][heads], where given); returns out.  Stream as in quantize_rows; a workspace, where the call needs one, is allocated on it for this call alone.  Gradients as in rope."""
     if _torch is None:
         _ready()
     dev = q.get_device()
@@ -569,6 +569,7 @@ def shared_attention(q, q_starts, k_cache, v_cache, own_pages, own_lens, prefix_
     """bb_shared_attention: queries [tokens][heads][dim] of branches (branch b: rows q_starts[b] .. q_starts[b + 1] - 1) over caches [pages][kv heads][PAGE_TOKENS][dim]:
     the prefix of the branch's group (branches group_starts[g] .. group_starts[g + 1] - 1; prefix_lens[g] keys in the pages prefix_pages[g]), read once for all of
     them, and the branch's own_lens[b] keys in the pages own_pages[b].  Tables, lengths and starts are int32 tensors of the device; without a prefix it is plain attention over pages.
+    Work is shared out for lengths of as many pages as the tables have columns: of wide tables pass those in use, table[:, :n].
     block, scale, out, lse, stream, workspace and gradients as in attention (block counts from the first own key)."""
     if _torch is None:
         _ready()

@@ -56,7 +56,7 @@ struct KvArgs {
     Divide by_kv_heads, by_each, by_block, by_own_split, by_prefix_split;
     float* part_o; float2* part_ml;                                     // [part][token][head]: unscaled output; maximum before scale and sum.  Null: a single part
 };
-#define KV_LEAST_TILES 2                // of 64 keys, a part of a row tile's keys
+#define KV_LEAST_TILES 2                // of 64 keys, a part of as many keys as the plan counts with (a row tile may have fewer)
 #define KV_MOST_PARTS 32                // of a branch's own keys, of a prefix
 #define KV_FEW_PARTS 6                  // from there on the join takes them four ways
 #define KV_MOST_COLUMNS (BB_MAX_TOKENS / BB_PAGE_TOKENS)
@@ -303,9 +303,9 @@ template <class E, int D, int NK> static __device__ __forceinline__ void scores(
 // The rows' maxima follow a tile's scores, each by itself.  PART: not every row sees all of the tile's keys; seen: how many of them the lane's row does.
 // One follows only by more than KV_LAG (of 2^KV_LAG), so the output is seldom scaled: a weight is then at most that, of no fewer bits.  (The largest is 1 only where the maximum has just followed; elsewhere
 // it is rounded as any other.)
-// Weights are exp2(s * by - from).  From is the maximum times scale, rounded: what the rounding is off by, 2^-25 of it, all weights have in common, but from some 2^27 on it leaves the range of 16-bit
-// weights, and then of fp32.  Beyond KV_LARGE a row's exponents are (s - maximum) * scale instead, its maximum follows every tile, and the two agree within 2^-15 where a row has both (a score's own
-// rounding is off by as much).
+// Weights are exp2(s * by - from).  From is the maximum times scale, rounded: what the rounding is off by, 2^-25 of it, all weights have in common, but from some 2^27 on it leaves the range of
+// 16-bit weights, and then of fp32.  Beyond KV_LARGE a row's exponents are (s - maximum) * scale instead, its maximum follows every tile, and the two agree within 2^-15 where a row has both (a
+// score's own rounding is off by as much).
 template <int D, int NK, bool PART> static __device__ __forceinline__ void follow(RowState<D>& r, f32x16 (&s)[NK], float scale, float lag, int seen, float& by, float& from) {
     const int h2 = (threadIdx.x & 63) >> 5;
     if (PART) {
@@ -447,13 +447,14 @@ static __device__ __forceinline__ void weigh(RowState<D>& r, unsigned vp, unsign
 // One half, two workgroups a CU: where there are items enough (each runs on while the other waits at its barrier).  Two halves, one workgroup a CU: where there are few, so that
 // fewer parts of the keys have to be joined through memory (four branches of 120 rows in all on 512 shared and 104 to 128 own keys, 32 heads: 16.7 us, 18.1 with one half).
 //
-// What bounds it.  16384 causal tokens of 32 heads of 128: 1960 to 2060 us, 1.07 to 1.12 PFLOP/s (a library product of 8192^3 on the same card 1.39): the clock is down to 1.9 GHz for
+// What bounds it.  16384 causal tokens of 32 heads of 128: 1920 to 2060 us, 1.07 to 1.15 PFLOP/s (a library product of 8192^3 on the same card 1.39): the clock is down to 1.9 GHz for
 // power, the matrix pipes are busy for 0.51 of the time and the vector pipes, with the exponentials, conversions and maxima, for 0.52; without the fetches it would take 0.88 of the time, without the
-// products 0.65.  The two pipes overlap no better whichever way their instructions are laid out (two tiles of scores at once, halves of a tile by turns, priorities: the same within 1 %, or slower).  Short prompts (sixteen of 1 to 1008 tokens, 28 heads on 4: 78 us, 0.6 PFLOP/s) are bound by an item's own time, 11600 cycles besides its tiles: 1700 until its
-// sequence is found, 2000 until the first fetch is on its way, the fetch, the join or the barrier, 3300 for its rows' way out.
+// products 0.65.  The two pipes overlap no better whichever way their instructions are laid out (two tiles of scores at once, halves of a tile by turns, priorities: the same within 1 %, or
+// slower).  Short prompts (sixteen of 1 to 1008 tokens, 28 heads on 4: 78 us, 0.6 PFLOP/s) are bound by an item's own time, 11600 cycles besides its tiles: 1700 until its sequence is found, 2000 until
+// the first fetch is on its way, the fetch, the join or the barrier, 3300 for its rows' way out.
 //
-// Why 128 rows by 64 keys: a wave's 32 rows keep queries, weights, scores and output in registers (227 of 256, so two waves a SIMD), K,V of 64 keys come into LDS once for four waves, twice over
-// (64 KiB, two workgroups a CU), and a page is one tile.  K Q^T rather than Q K^T, so that a lane's weights are what the second product takes from it, without a way through LDS.
+// Why 128 rows by 64 keys: a wave's 32 rows keep queries, weights, scores and output in registers (233 of 256, 236 with pages, so two waves a SIMD), K,V of 64 keys come into LDS once for four
+// waves, twice over (64 KiB, two workgroups a CU), and a page is one tile.  K Q^T rather than Q K^T, so that a lane's weights are what the second product takes from it, without a way through LDS.
 template <class E, int D, bool PAGED, int HALVES>
 __global__ __launch_bounds__(256 * HALVES, 2) void kv_attention_kernel(KvArgs a) {
     typedef typename Half<E>::x8 x8;
@@ -817,9 +818,12 @@ static bool refuse_mask(long block, double scale) { return block < 0 || block > 
 struct KvPlan { int halves, own_parts, prefix_parts; };
 // How many row tiles there can be, whatever the lengths, and how their keys are shared out: into how many parts, to one or two halves of a workgroup, and whether a prefix is taken once
 // for its group, as parts of its own, or again by every branch before its own keys.  Lengths stand on the device: tables count with their width, packed keys with their mean, sequences
-// as equally long, the longest somewhat longer.  The least of a rough account of the time, us, whose constants were fitted to 38 shapes with up to 50 plans each (what it picks is 1 % slower
-// than the best of them in the mean, 11 % at most): FIRST for the first loads and the launch, ITEM for a workgroup's own, 64 keys of a row tile ALONE on a CU or with another workgroup's
-// (BOTH, 512 at once), or 128 by two HALVES; FEW: times that for tiles of up to 32 rows; the join's launch, and its bytes per us.
+// as equally long, the longest somewhat longer.  Lengths that are not so cost time, never results: four branches of 120 rows on 512 shared and 104 to 128 own keys (32 heads) 16.4 us with tables of
+// their own width, 18.3 with 16 or 64 columns, 25.9 with 512; 64 tokens on 16381 shared keys (28 heads on 4) 36 and, with 512 columns, 90; one query on 16384 packed keys 12.6, with 31 more on 64 each 95.8, as
+// its keys are no longer cut.
+// The least of a rough account of the time, us, whose constants were fitted to 38 shapes with up to 50 plans each (what it picked was 1 % slower than the best of them in the mean, 11 % at
+// most; the join has become a quarter faster since than JOIN and JOIN_BYTES have it): FIRST for the first loads and the launch, ITEM for a workgroup's own, 64 keys of a row tile ALONE on a CU or
+// with another workgroup's (BOTH, 512 at once), or 128 by two HALVES; FEW: times that for tiles of up to 32 rows; the join's launch, and its bytes per us.
 static bool plan_parts(KvArgs& a, long own_keys, long prefix_keys, int head_dim, const KvPlan* given) {
     const double FIRST = 3.4, ITEM = 2.8, BOTH = 0.9, ALONE = 1.0, HALVES = 1.5, MERGE = 0.15, FEW = 0.57, LONGEST = 1.2, JOIN = 3.7, JOIN_BYTES = 2.8e6, DIM_64 = 0.53;
     static const int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
@@ -899,7 +903,10 @@ static int attention(const bb_attention_args* x, const KvPlan* given, void* work
     const HeadView k = heads_view(x->k, x->k_tokens, x->k_token, kv_heads, x->k_head, dim, 2), v = heads_view(x->v, x->k_tokens, x->v_token, kv_heads, x->v_head, dim, 2);
     const HeadView l = heads_view(x->lse, x->q_tokens, heads, heads, 1, 1, 4);
     if (refuse_view(q) || refuse_pieces(q) || refuse_out_view(o) || refuse_pieces(o) || overlap(o, q) || (x->lse && (overlap(l, o) || overlap(l, q)))) return BB_EINVAL;
-    if (x->k_tokens > 0 && (refuse_view(k) || refuse_pieces(k) || refuse_view(v) || refuse_pieces(v) || far_rows(k.s[0]) || far_rows(v.s[0]) || overlap(o, k) || overlap(o, v) || (x->lse && (overlap(l, k) || overlap(l, v))))) return BB_EINVAL;
+    if (x->k_tokens > 0) {
+        if (refuse_view(k) || refuse_pieces(k) || far_rows(k.s[0]) || refuse_view(v) || refuse_pieces(v) || far_rows(v.s[0])) return BB_EINVAL;
+        if (overlap(o, k) || overlap(o, v) || (x->lse && (overlap(l, k) || overlap(l, v)))) return BB_EINVAL;
+    }
     KvArgs a{};
     if (!plan(a, x, given)) return BB_EINVAL;
     // (strides as the views have them: none over a single token or head)
