@@ -103,3 +103,35 @@ def test_frequencies_of_more_pairs_than_a_head_has():
     for rot in (2 ** 32 + 64, 1026, 2 ** 80):
         with pytest.raises(BBError):
             bb.rope_frequencies(rot, device="cpu")
+
+
+@pytest.mark.gpu
+def test_rope_captured_and_replayed_with_other_positions_and_slots():
+    """Both calls in one graph; positions, slots and rows change between replays, eager calls of the same run between them; every replay equals the eager result, and slots of earlier ones stay."""
+    x, f = rnd(1, 9, 8, 64).to(DEV), bb.rope_frequencies(64, device=DEV)
+    pos, slots = ints(range(9)).to(DEV), ints(range(9)).to(DEV)
+    cache = torch.zeros(2, 3, 2, PAGE, 64, dtype=x.dtype, device=DEV)
+    q2, k2, q3 = (torch.empty(9, h, 64, dtype=x.dtype, device=DEV) for h in (4, 2, 4))
+
+    def both(cache, q2, k2, q3):
+        bb.rope(x[:, :4], x[:, 4:6], pos, f, q_out=q2, k_out=k2)
+        bb.rope_append(x[:, :4], x[:, 4:6], x[:, 6:], pos, f, cache[0], cache[1], slots, interleaved=True, q_out=q3)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both(torch.zeros_like(cache), q2, k2, q3)
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        both(cache, q2, k2, q3)
+    other = [torch.zeros_like(cache), torch.empty_like(q2), torch.empty_like(k2), torch.empty_like(q3)]
+    for n in range(4):
+        x.copy_(rnd(10 + n, 9, 8, 64))
+        pos.copy_(torch.randint(-9, 1 << 20, (9,), generator=torch.Generator().manual_seed(n)))
+        slots.copy_(torch.randperm(3 * PAGE, generator=torch.Generator().manual_seed(n))[:9])
+        g.replay()
+        both(*other)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((cache, q2, k2, q3), other)), n
+    assert (cache != 0).any()
